@@ -209,6 +209,104 @@ void ctkvr_free(ctkvr_index *idx);
 /* Thread-local description of the last non-OK return of this library. */
 const char *ctkvr_last_error(void);
 
+/* ---- the paged KV cache itself: append, dense attention, accumulated weights, eviction --------------- */
+/*
+ * What surrounds the index: filling the caller's pages with rotated keys, attending densely with the prompt's chunks and with
+ * single tokens, and keeping a sequence within a budget of tokens by the attention that its keys have had.
+ *
+ * Tokens.  A call serves `batch` sequences with `total` new tokens, sequence after sequence: those of sequence b are cu_new[b] ..
+ * cu_new[b + 1] - 1 (0, 1 or more; cu_new[0] = 0), and cur_lens[b] counts the tokens of b in the cache with the new ones among
+ * them, so that new token i of n_b stands in slot (and, to the masks, at position) cur_lens[b] - n_b + i.  cu_new [batch + 1],
+ * cur_lens [batch] and block_table [batch][max_pages] are DEVICE arrays: captured graphs stay valid as they change.
+ * Outputs of tokens behind cu_new[batch] are left as they were.  A page id outside 0 .. num_pages - 1 (-1, say) is no page: nothing is
+ * written there, and its keys are seen by no token.  Slots of cur_lens[b] beyond max_pages * page_size are no slots.
+ *
+ * Rows of q, k and v may be views of a wider array (a fused projection): *_stride is the distance from a token to the next in
+ * elements, a token's heads are contiguous, and every row begins on a 16-byte boundary; so do pages and outputs.
+ *
+ * Each call is asynchronous on hip_stream, a stream of the device that was current when the handle was made (NULL: that device's default
+ * stream; the calling thread's current device may be another), allocates nothing and can be captured into a HIP graph.
+ * ctkvr_cache_attn uses the handle's workspace: two of its calls on one handle must not overlap, replays of graphs among them.
+ */
+typedef struct ctkvr_cache ctkvr_cache;   /* opaque: geometry, rotary frequencies, workspace */
+
+typedef struct {
+    int32_t batch, n_q_heads, n_kv_heads;
+    int32_t head_dim;            /* must be 128; n_q_heads / n_kv_heads one of 1, 2, 4, 8 */
+    int32_t page_size;           /* a power of two up to 256 */
+    int32_t dtype;               /* ctkvr_dtype of q, k, v, the pages and the attention's output */
+    int32_t num_pages;           /* pages in k_pages and in v_pages */
+    int32_t max_pages;           /* columns of the block table; max_pages * page_size at most 2^20 */
+    int32_t max_new;             /* new tokens of a call, at most (over all sequences) */
+    float   sm_scale;            /* factor of q.k; 0 => 1/sqrt(head_dim) */
+    float   softcap;             /* 0: none; else a score z becomes softcap * tanh(z / softcap) */
+    double  rope_base;           /* frequency of pair i: rope_base^(-2 i / head_dim) */
+    const double *rope_freq;     /* HOST [head_dim / 2] or NULL: these frequencies (radians per position) instead */
+    const uint8_t *rope_axis;    /* HOST [head_dim / 2] or NULL (all 0): the axis, 0 to 2, that turns each pair */
+} ctkvr_cache_params;
+
+/* A handle on the current device; params' arrays are copied.  Errors: EINVAL, EUNSUPPORTED (as the index), ENOMEM. */
+int ctkvr_cache_create(const ctkvr_cache_params *p, ctkvr_cache **out_cache);
+/* Release a handle (NULL is allowed); synchronises its device first, as ctkvr_free does. */
+void ctkvr_cache_free(ctkvr_cache *c);
+
+/*
+ * Rotate new queries and keys to their positions and write keys and values into their slots:
+ *   x'_i = x_i cos a_i - x_{i+64} sin a_i,  x'_{i+64} = x_{i+64} cos a_i + x_i sin a_i,  a_i = position[axis_i] * frequency_i,
+ * in fp32 with angles exact to 2^-32 of a turn at any position, rounded once to `dtype`; values are copied.
+ *   q, q_out   [total][h][128] (q_out contiguous; may be q where q is) or both NULL;  k, v  [total][g][128] or both NULL.
+ *   positions  DEVICE int32 [axes][total], any values, for the axes that rope_axis names (text: the same on all), or NULL:
+ *              the token's slot on every axis.  After an eviction slots are no positions any more.
+ * No two sequences may write into one page's slot.  Errors: EINVAL.
+ */
+int ctkvr_cache_append(ctkvr_cache *c, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                       const int32_t *positions, const int32_t *cu_new, const int32_t *cur_lens, const int32_t *block_table, int32_t total,
+                       void *q_out, void *k_pages, void *v_pages, void *hip_stream);
+
+/*
+ * Attention of the new tokens over the cache (which holds them already): per token and query head softmax(z) V over the keys it sees,
+ *   z = cap(q . k * sm_scale) - slope_h * |pos - t|,
+ * for key t of the token at pos:  first_key <= t < cur_lens[b]  and  (t <= pos or t < prefix_lens[b]).
+ *   q           [total][h][128], rotated.
+ *   slopes      DEVICE fp32 [h] or NULL: a bias by distance.
+ *   prefix_lens DEVICE int32 [batch] or NULL: so many keys at the start are seen by every token, earlier ones too.
+ *   first_key   DEVICE int32 [total] or NULL: where the token's document begins (packed documents), or its window.
+ *   out         [total][h][128] of `dtype`;  out_lse  fp32 [total][h] or NULL, natural log.
+ * A token that sees no key, or none with a score above -infinity, gets zeros and -infinity.  What a token does not see does not touch its result,
+ * infinities and NaN included.  Sums are fp32; with bf16 data the probabilities enter the product with V rounded to bf16.
+ * The same call gives the same result, bit for bit.  Errors: EINVAL.
+ */
+int ctkvr_cache_attn(ctkvr_cache *c, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages, const int32_t *cu_new,
+                     const int32_t *cur_lens, const int32_t *block_table, int32_t total, const float *slopes, const int32_t *prefix_lens,
+                     const int32_t *first_key, void *out, float *out_lse, void *hip_stream);
+
+/*
+ * The attention weight of every key of the batch under the new tokens:
+ *   weights_out[b][kv][t] = decay * weights_in[b][kv][t] + sum over b's new tokens and the KV head's query heads of exp(z - lse)
+ * with ctkvr_cache_attn's scores, masks and out_lse.  A key that the call's own tokens brought has no weight before it.
+ *   lse          fp32 [total][h] of the attention (a row of -infinity adds nothing).
+ *   weights_in   fp32 [batch][g][weights_stride] or NULL (zeros); weights_out likewise, may be weights_in.
+ *                weights_stride >= max_pages * page_size; slots from cur_lens[b] on are left as they were.
+ * With total = 0 the weights decay.  Sums are fp32, in an order of their own: the same result in every call.  Errors: EINVAL.
+ */
+int ctkvr_cache_weights(ctkvr_cache *c, const void *q, int64_t q_stride, const float *lse, const void *k_pages, const int32_t *cu_new,
+                        const int32_t *cur_lens, const int32_t *block_table, int32_t total, const float *slopes, const int32_t *prefix_lens,
+                        const int32_t *first_key, float decay, const float *weights_in, float *weights_out, int32_t weights_stride,
+                        void *hip_stream);
+
+/*
+ * Cut every sequence longer than `budget` down to it: per sequence and KV head the first n_init and the last n_local tokens stay, and
+ * of those in between the budget - n_init - n_local with the largest weights, ties to the lowest slot (-0 equals +0, NaN is below
+ * -infinity).  The kept rows of K and V move to the front in place, in order: slot j then holds what slot out_ids[b][kv][j] held.
+ *   weights_in  as ctkvr_cache_weights leaves them;  weights_out  the same shape or NULL, may be weights_in: the kept weights, moved alike.
+ *   out_ids     int32 [batch][g][budget] ascending, -1 padded;  out_lens  int32 [batch] or NULL: min(cur_lens[b], budget).
+ * Pages that no kept token needs any more are the caller's again; slots from out_lens[b] on hold what they held before or moved rows.  A row whose
+ * old or new page is no page is not moved.  Sequences must not share the pages.  Errors: EINVAL.
+ */
+int ctkvr_cache_evict(ctkvr_cache *c, const float *weights_in, int32_t weights_stride, const int32_t *cur_lens, const int32_t *block_table,
+                      int32_t budget, int32_t n_init, int32_t n_local, void *k_pages, void *v_pages, float *weights_out, int32_t *out_ids,
+                      int32_t *out_lens, void *hip_stream);
+
 /* ---- inspection (tests, tooling); each synchronises ----------------------- */
 typedef struct {
     int32_t batch, n_q_heads, n_kv_heads, head_dim, dtype;

@@ -44,6 +44,14 @@ class _CInfo(ctypes.Structure):
                 ("l_stride", ctypes.c_int32), ("index_bytes", ctypes.c_int64), ("device_bytes", ctypes.c_int64)]
 
 
+class _CCacheParams(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("max_new", ctypes.c_int32),
+                ("sm_scale", ctypes.c_float), ("softcap", ctypes.c_float), ("rope_base", ctypes.c_double),
+                ("rope_freq", ctypes.c_void_p), ("rope_axis", ctypes.c_void_p)]
+
+
 @dataclass
 class Params:
     batch: int
@@ -77,7 +85,8 @@ EXPORTS = ["ctkvr_build_index", "ctkvr_index_load", "ctkvr_decode_step", "ctkvr_
            "ctkvr_index_info", "ctkvr_index_lists", "ctkvr_index_centroids", "ctkvr_index_last_candidates",
            "ctkvr_profile_enable", "ctkvr_profile_collect", "ctkvr_centroid_update", "ctkvr_decode_step_window",
            "ctkvr_selftest_exp", "ctkvr_decode_step_static", "ctkvr_index_set_decode_path", "ctkvr_index_decode_path",
-           "ctkvr_index_check", "ctkvr_profile_phases", "ctkvr_measure_dispatch_floor", "ctkvr_index_build_route", "ctkvr_release_scratch"]
+           "ctkvr_index_check", "ctkvr_profile_phases", "ctkvr_measure_dispatch_floor", "ctkvr_index_build_route", "ctkvr_release_scratch",
+           "ctkvr_cache_create", "ctkvr_cache_free", "ctkvr_cache_append", "ctkvr_cache_attn", "ctkvr_cache_weights", "ctkvr_cache_evict"]
 PATH_AUTO, PATH_STAGED, PATH_FUSED = 0, 1, 2
 N_STAGES = 9
 STAGE_NAMES = ["centroid_cos", "recall_gather", "score", "denom", "keyhist", "classify",
@@ -139,6 +148,19 @@ def load_library() -> ctypes.CDLL:
     L.ctkvr_measure_dispatch_floor.argtypes = [ctypes.c_int32, ctypes.POINTER(ctypes.c_float), vp]
     L.ctkvr_selftest_exp.restype = ctypes.c_int
     L.ctkvr_selftest_exp.argtypes = [ctypes.POINTER(ctypes.c_uint64), vp]
+    i32, i64, f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+    L.ctkvr_cache_create.restype = ctypes.c_int
+    L.ctkvr_cache_create.argtypes = [ctypes.POINTER(_CCacheParams), ctypes.POINTER(ctypes.c_void_p)]
+    L.ctkvr_cache_free.restype = None
+    L.ctkvr_cache_free.argtypes = [vp]
+    L.ctkvr_cache_append.restype = ctypes.c_int
+    L.ctkvr_cache_append.argtypes = [vp, vp, i64, vp, i64, vp, i64, ip, ip, ip, ip, i32, vp, vp, vp, vp]
+    L.ctkvr_cache_attn.restype = ctypes.c_int
+    L.ctkvr_cache_attn.argtypes = [vp, vp, i64, vp, vp, ip, ip, ip, i32, fp, ip, ip, vp, fp, vp]
+    L.ctkvr_cache_weights.restype = ctypes.c_int
+    L.ctkvr_cache_weights.argtypes = [vp, vp, i64, fp, vp, ip, ip, ip, i32, fp, ip, ip, f32, fp, fp, i32, vp]
+    L.ctkvr_cache_evict.restype = ctypes.c_int
+    L.ctkvr_cache_evict.argtypes = [vp, fp, i32, ip, ip, i32, i32, i32, vp, vp, fp, ip, ip, vp]
     _lib = L
     return L
 
@@ -364,3 +386,177 @@ def ctkvr_measure_dispatch_floor(n_launches: int = 200) -> float:
     us = ctypes.c_float(0.0)
     _check(load_library().ctkvr_measure_dispatch_floor(int(n_launches), ctypes.byref(us), _stream()))
     return float(us.value)
+
+
+# ---- the paged KV cache ------------------------------------------------------
+@dataclass
+class CacheParams:
+    """Geometry of a paged KV cache and of the calls on it; ``rope_freq`` (64 float64) and ``rope_axis`` (64 uint8) are
+    host arrays or None."""
+    batch: int
+    n_q_heads: int
+    n_kv_heads: int
+    num_pages: int
+    max_pages: int
+    max_new: int
+    head_dim: int = 128
+    page_size: int = 16
+    dtype: int = BF16
+    sm_scale: float = 0.0
+    softcap: float = 0.0
+    rope_base: float = 10000.0
+    rope_freq: Optional[np.ndarray] = None
+    rope_axis: Optional[np.ndarray] = None
+
+
+class Cache:
+    """Owner of a ``ctkvr_cache*`` on one device; freed on ``ctkvr_cache_free`` or garbage collection."""
+
+    def __init__(self, handle: int, params: CacheParams, device: int):
+        import torch
+        self.handle = handle
+        self.params = params
+        self.device = device
+        self.torch_dtype = _torch_dtype(params.dtype)
+        self.n_axes = 1 if params.rope_axis is None else int(np.max(params.rope_axis)) + 1
+        self._current_stream = torch.cuda.current_stream
+
+    def stream(self) -> int:
+        return self._current_stream(self.device).cuda_stream
+
+    def __del__(self):
+        try:
+            ctkvr_cache_free(self)
+        except Exception:
+            pass
+
+
+def _shape_of(name, t, shape):
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+
+
+def _on(cache: Cache, name, t, dtype, shape):
+    """Device pointer of a contiguous tensor of this type and shape on the cache's device (None passes NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: expected dtype {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        _shape_of(name, t, shape)
+    if not t.is_cuda or t.get_device() != cache.device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor on device {cache.device}")
+    return t.data_ptr()
+
+
+def _rows_on(cache: Cache, name, t, total, heads):
+    """Device pointer and token stride of [total][heads][128], the heads of a token contiguous."""
+    if t is None:
+        return None, 0
+    if t.dtype != cache.torch_dtype:
+        raise ValueError(f"{name}: expected dtype {cache.torch_dtype}, got {t.dtype}")
+    if t.shape != (total, heads, 128):
+        _shape_of(name, t, (total, heads, 128))
+    if not t.is_cuda or t.get_device() != cache.device:
+        raise ValueError(f"{name}: expected a tensor on device {cache.device}")
+    stride = t.stride()
+    if total and (stride[2] != 1 or (heads > 1 and stride[1] != 128)):
+        raise ValueError(f"{name}: a token's heads must be contiguous")
+    return t.data_ptr(), (stride[0] if total > 1 else heads * 128)
+
+
+def _pages_on(cache: Cache, name, t):
+    p = cache.params
+    return _on(cache, name, t, cache.torch_dtype, (p.num_pages, p.n_kv_heads, p.page_size, 128))
+
+
+def _batch_on(cache: Cache, cu_new, cur_lens, block_table):
+    import torch
+    p, i32 = cache.params, torch.int32
+    return (_on(cache, "cu_new", cu_new, i32, (p.batch + 1,)), _on(cache, "cur_lens", cur_lens, i32, (p.batch,)),
+            _on(cache, "block_table", block_table, i32, (p.batch, p.max_pages)))
+
+
+def ctkvr_cache_create(params: CacheParams) -> Cache:
+    import torch
+    L = load_library()
+    freq = None if params.rope_freq is None else np.ascontiguousarray(params.rope_freq, np.float64)
+    axis = None if params.rope_axis is None else np.ascontiguousarray(params.rope_axis, np.uint8)
+    for name, a in (("rope_freq", freq), ("rope_axis", axis)):
+        if a is not None and a.shape != (64,):
+            raise ValueError(f"{name}: expected 64 values, got shape {a.shape}")
+    cp = _CCacheParams(params.batch, params.n_q_heads, params.n_kv_heads, params.head_dim, params.page_size, params.dtype,
+                       params.num_pages, params.max_pages, params.max_new, float(params.sm_scale), float(params.softcap),
+                       float(params.rope_base), None if freq is None else freq.ctypes.data, None if axis is None else axis.ctypes.data)
+    out = ctypes.c_void_p()
+    _check(L.ctkvr_cache_create(ctypes.byref(cp), ctypes.byref(out)))
+    return Cache(out.value, params, torch.cuda.current_device())
+
+
+def ctkvr_cache_free(cache: Optional[Cache]) -> None:
+    if cache is not None and cache.handle:
+        load_library().ctkvr_cache_free(cache.handle)
+        cache.handle = 0
+
+
+def ctkvr_cache_append(cache: Cache, q, k, v, cu_new, cur_lens, block_table, q_out, k_pages, v_pages, positions=None) -> None:
+    """q, k and v may be views of a fused projection; q and q_out, or k and v, may be None."""
+    import torch
+    p = cache.params
+    total = (q if q is not None else k).shape[0]
+    cu, cur, table = _batch_on(cache, cu_new, cur_lens, block_table)
+    (qp, qs), (kp, ks) = _rows_on(cache, "q", q, total, p.n_q_heads), _rows_on(cache, "k", k, total, p.n_kv_heads)
+    vp, vs = _rows_on(cache, "v", v, total, p.n_kv_heads)
+    _check(load_library().ctkvr_cache_append(
+        cache.handle, qp, qs, kp, ks, vp, vs, _on(cache, "positions", positions, torch.int32, (cache.n_axes, total)), cu, cur, table, total,
+        _on(cache, "q_out", q_out, cache.torch_dtype, (total, p.n_q_heads, 128)), _pages_on(cache, "k_pages", k_pages),
+        _pages_on(cache, "v_pages", v_pages), cache.stream()))
+
+
+def _masks_on(cache: Cache, total, slopes, prefix_lens, first_key):
+    import torch
+    return (_on(cache, "slopes", slopes, torch.float32, (cache.params.n_q_heads,)),
+            _on(cache, "prefix_lens", prefix_lens, torch.int32, (cache.params.batch,)),
+            _on(cache, "first_key", first_key, torch.int32, (total,)))
+
+
+def ctkvr_cache_attn(cache: Cache, q, k_pages, v_pages, cu_new, cur_lens, block_table, out, out_lse=None, slopes=None, prefix_lens=None,
+                     first_key=None) -> None:
+    import torch
+    h, total = cache.params.n_q_heads, q.shape[0]
+    cu, cur, table = _batch_on(cache, cu_new, cur_lens, block_table)
+    qp, qs = _rows_on(cache, "q", q, total, h)
+    _check(load_library().ctkvr_cache_attn(
+        cache.handle, qp, qs, _pages_on(cache, "k_pages", k_pages), _pages_on(cache, "v_pages", v_pages), cu, cur, table, total,
+        *_masks_on(cache, total, slopes, prefix_lens, first_key), _on(cache, "out", out, cache.torch_dtype, (total, h, 128)),
+        _on(cache, "out_lse", out_lse, torch.float32, (total, h)), cache.stream()))
+
+
+def ctkvr_cache_weights(cache: Cache, q, lse, k_pages, cu_new, cur_lens, block_table, weights_in, weights_out, decay=1.0, slopes=None,
+                        prefix_lens=None, first_key=None) -> None:
+    """weights_in (None: zeros) and weights_out: fp32 [batch][g][weights_stride]."""
+    import torch
+    p, total = cache.params, q.shape[0]
+    cu, cur, table = _batch_on(cache, cu_new, cur_lens, block_table)
+    qp, qs = _rows_on(cache, "q", q, total, p.n_q_heads)
+    shape = (p.batch, p.n_kv_heads, weights_out.shape[-1])
+    _check(load_library().ctkvr_cache_weights(
+        cache.handle, qp, qs, _on(cache, "lse", lse, torch.float32, (total, p.n_q_heads)), _pages_on(cache, "k_pages", k_pages), cu, cur,
+        table, total, *_masks_on(cache, total, slopes, prefix_lens, first_key), float(decay),
+        _on(cache, "weights_in", weights_in, torch.float32, shape), _on(cache, "weights_out", weights_out, torch.float32, shape), shape[2],
+        cache.stream()))
+
+
+def ctkvr_cache_evict(cache: Cache, weights_in, k_pages, v_pages, cur_lens, block_table, budget, out_ids, n_init=0, n_local=0,
+                      weights_out=None, out_lens=None) -> None:
+    """out_ids: int32 [batch][g][budget]; out_lens: int32 [batch] or None."""
+    import torch
+    p = cache.params
+    shape = (p.batch, p.n_kv_heads, weights_in.shape[-1])
+    _check(load_library().ctkvr_cache_evict(
+        cache.handle, _on(cache, "weights_in", weights_in, torch.float32, shape), shape[2],
+        _on(cache, "cur_lens", cur_lens, torch.int32, (p.batch,)), _on(cache, "block_table", block_table, torch.int32, (p.batch, p.max_pages)),
+        int(budget), int(n_init), int(n_local), _pages_on(cache, "k_pages", k_pages), _pages_on(cache, "v_pages", v_pages),
+        _on(cache, "weights_out", weights_out, torch.float32, shape),
+        _on(cache, "out_ids", out_ids, torch.int32, (p.batch, p.n_kv_heads, int(budget))),
+        _on(cache, "out_lens", out_lens, torch.int32, (p.batch,)), cache.stream()))

@@ -1,11 +1,11 @@
-"""Compile the HIP library for gfx950 with hipcc, in-tree: two translation units (the host side with
-the staged and build kernels; the single-launch decode kernel), compiled side by side, then linked."""
+"""Compile the HIP library for gfx950 with hipcc, in-tree: three translation units (the host side with
+the staged and build kernels; the single-launch decode kernel; the operators on the paged KV cache), compiled side by side, then linked."""
 import os
 import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = ["ctkvr.hip", "fused.hip"]
+SOURCES = ["ctkvr.hip", "fused.hip", "cache.hip"]
 LIB = os.path.join(HERE, "libctkvr.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 

@@ -1,0 +1,879 @@
+// Kernels of the operators on the paged KV cache: append with rotary positions, attention of new tokens, accumulated attention weights,
+// eviction.  gfx950, wave64, matrix cores.
+//
+// Rows.  The G query heads that share a KV head are rows of one problem: row r of a (sequence, KV head) unit is head r % G of the
+// sequence's new token r / G, so a tile of rows reads each key once for the whole group.
+//
+// Scores come transposed, S^T = K Q^T: in the 32 x 32 result a lane holds one row (column lane % 32) and 16 keys, so that a row's maximum and
+// sum are a chain within the lane and one exchange with the other half of the wave, and the probabilities are, where they stand, the B operand of the
+// next product O^T = V^T P^T for keys in the order 8 a + 4 (lane / 32) + c, which V's operand follows.
+#pragma once
+#include "cache_args.hpp"
+#include "common.hpp"
+
+namespace ctkvr {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
+
+#define CTKVR_LDS __attribute__((address_space(3)))
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// Tile `tile` of the tiles of 2^LOG rows that the batch's units of one KV head fall into, sequence by sequence: its sequence and its
+// number there (by one wave; every lane gets them)
+template <int LOG> __device__ __forceinline__ bool locate_tile(const CacheView &v, int tile, int *b, int *at)
+{
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int b0 = 0; b0 < v.batch; b0 += 64) {
+        int mine = 0;
+        if (b0 + lane < v.batch) mine = (((seq_span(v, b0 + lane).n << v.lg) + (1 << LOG) - 1) >> LOG);
+        int upto = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+        }
+        const int all = __builtin_amdgcn_readlane(upto, 63);
+        if (tile < base + all) {
+            const int l = __builtin_ctzll(__ballot(base + upto > tile));
+            *b = b0 + l;
+            *at = tile - base - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l));
+            return true;
+        }
+        base += all;
+    }
+    return false;
+}
+
+// ---- tiles of 128-element rows in shared memory ------------------------------------------------------
+// 16 KB: 64 rows of bf16 or 32 of fp32.  The 16-byte chunk c of row r stands at chunk c ^ swz(r): the 32 rows that an operand of the
+// matrix instructions reads at one chunk, and the four rows at two chunks that the transposing load takes, then fall on all banks alike.
+template <typename T> struct RowTile {
+    static constexpr int kRows = sizeof(T) == 2 ? 64 : 32, kRowBytes = 128 * sizeof(T), kChunks = kRowBytes / 16;
+    static constexpr int kRowsPerLoad = 64 / kChunks;   // rows of one load of a wave
+    static constexpr int kBytes = kRows * kRowBytes;
+};
+template <typename T> __device__ __forceinline__ int swz(int row)
+{
+    if constexpr (sizeof(T) == 2) return ((row & 3) << 2) | ((row >> 2) & 3);
+    else return row & 15;
+}
+// 16 bytes a lane from `from` straight into shared memory at byte `to` + 16 * lane (uniform `to`); waited for like a load
+__device__ __forceinline__ void row_to_lds(uint32_t to, const void *from)
+{
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "{m0}"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_at(const void *p) { return (uint32_t)(uintptr_t)(const CTKVR_LDS void *)p; }
+
+// Loads in flight have landed, in registers and shared memory (of a wave: a barrier for the block behind it).  The compiler, which does not know of
+// those in assembly, would not wait for them at the barrier.
+__device__ __forceinline__ void loads_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// One exchange between the halves of a wave
+__device__ __forceinline__ float half_max(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A row's part of a product's operand: lane (row, half) holds the chunks 2 i + half
+template <typename T> struct Operand;
+template <> struct Operand<bf16_t> { bf16x8_t c[8]; };
+template <> struct Operand<float> { f32x4_t c[16]; };
+template <typename T> __device__ __forceinline__ void load_operand(Operand<T> &o, const T *row, int half)
+{
+    using C = std::remove_reference_t<decltype(o.c[0])>;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(o.c) / 16); ++i) o.c[i] = *reinterpret_cast<const C *>(reinterpret_cast<const char *>(row) + 32 * i + 16 * half);
+}
+// acc += A B^T over 128 dimensions: A's row lane % 32 of a tile in shared memory from row r0 on, B an operand in registers
+template <typename T> __device__ __forceinline__ f32x16_t rows_dot(const char *tile, int r0, const Operand<T> &b, f32x16_t acc)
+{
+    const int lane = threadIdx.x & 63, r = r0 + (lane & 31), half = lane >> 5, s = swz<T>(r);
+    const char *row = tile + r * RowTile<T>::kRowBytes;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bf16x8_t a = *reinterpret_cast<const bf16x8_t *>(row + (((2 * i + half) ^ s) << 4));
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b.c[i], acc, 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const f32x4_t a = *reinterpret_cast<const f32x4_t *>(row + (((2 * i + half) ^ s) << 4));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b.c[i][e], acc, 0, 0, 0);
+        }
+    }
+    return acc;
+}
+
+// tanh(x): a continued fraction's fifth convergent below 0.6 (off by 1e-9 of it), (1 - e) / (1 + e) with e = exp(-2 x) above, where that loses nothing
+__device__ __forceinline__ float tanh_f(float x)
+{
+    const float a = fabsf(x), y = x * x;
+    const float e = exp2_fast(a * (-2.0f * kLog2e));
+    const float ns = a * fmaf(y, 105.0f + y, 945.0f), ds = fmaf(y, fmaf(y, 15.0f, 420.0f), 945.0f);
+    const bool small = a < 0.6f;
+    const float n = small ? ns : 1.0f - e, d = small ? ds : 1.0f + e;
+    return copysignf(n * __builtin_amdgcn_rcpf(d), x);
+}
+
+// ---- scores ------------------------------------------------------------------------------------------
+constexpr int kCap = 1, kBias = 2;
+// scores times log2 e, from the dot products (without cap and bias the factor is left to the exponent)
+template <int OPT> __device__ __forceinline__ void score_regs(f32x16_t &s, const ScoreOpts &o, float slope2, int pos_minus_key0, int half)
+{
+    if constexpr (OPT != 0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float z = (OPT & kCap) ? o.cap_out * tanh_f(s[i] * o.cap_in) : s[i] * o.c2;
+            if constexpr ((OPT & kBias) != 0) z = fmaf(-slope2, fabsf((float)(pos_minus_key0 - (8 * (i >> 2) + 4 * half + (i & 3)))), z);
+            s[i] = z;
+        }
+    }
+}
+
+// ---- attention of new tokens --------------------------------------------------------------------------
+struct AttnArgs {
+    CacheView v;
+    ScoreOpts o;
+    const void *q;
+    int64_t q_stride;          // elements from a token to the next
+    const void *k_pages, *v_pages;
+    void *out;                 // [total][h][128]
+    float *lse;                // [total][h] or null
+    float *part_o, *part_lse;  // [nsplit][total][h][128] and [nsplit][total][h], where keys are split
+    int tiles, nsplit;
+};
+
+// One block a tile of 32 NW rows of a unit and, where the keys are split, one of nsplit runs of their tiles; a wave has 32 rows.  Each
+// tile of keys goes straight to shared memory while the one before it is worked on; the maximum runs with them.
+template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW) void attn_kernel(AttnArgs a)
+{
+    constexpr int kRowsLog = NW == 4 ? 7 : 8, kKeys = RowTile<T>::kRows, kBlocks = kKeys / 32, kTile = RowTile<T>::kBytes;
+    constexpr int kPer = RowTile<T>::kRowsPerLoad, kLoads = kKeys / (NW * kPer);   // loads a wave makes of a tile of K, and of V
+    static_assert(NW == 4 || NW == 8, "");
+    __shared__ __align__(16) char smem[2][2][kTile];   // [buffer][K, V]
+    const CacheView &v = a.v;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    // (a KV head's tiles stay on an XCD where the heads are a multiple of 8; the tiles with most keys go first)
+    const int kv = blockIdx.x % v.g, rest = blockIdx.x / v.g, split = rest % a.nsplit;
+    int b, at;
+    if (!locate_tile<kRowsLog>(v, a.tiles - 1 - rest / a.nsplit, &b, &at)) return;
+    const SeqSpan s = seq_span(v, b);
+    const int rows = s.n << v.lg, r0 = at << kRowsLog, row = r0 + 32 * wave + (lane & 31);
+    const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
+    const int token = min(row, rows - 1) >> v.lg, head = (kv << v.lg) + (min(row, rows - 1) & ((1 << v.lg) - 1));
+    const RowSight sight = row_sight(v, a.o, s, prefix, token);
+
+    Operand<T> q;
+    load_operand(q, (const T *)a.q + (int64_t)(s.c0 + token) * a.q_stride + head * 128, half);
+
+    // keys that some row of the block sees, and those that all of them see
+    const int tok0 = r0 >> v.lg, tok1 = (min(r0 + 32 * NW, rows) - 1) >> v.lg;
+    const int pos0 = s.old + tok0, pos1 = s.old + tok1;
+    const int k_hi = pos1 < 0 ? 0 : min(max(pos1 + 1, prefix), s.len), all_hi = pos0 < 0 ? 0 : min(max(pos0 + 1, prefix), s.len);
+    int k_lo = 0, all_lo = 0;
+    if (a.o.first) {
+        int lo = sight.lo, hi = sight.lo;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            lo = min(lo, __shfl_xor(lo, d));
+            hi = max(hi, __shfl_xor(hi, d));
+        }
+        int *ex = reinterpret_cast<int *>(smem);
+        if (lane == 0) {
+            ex[2 * wave] = lo;
+            ex[2 * wave + 1] = hi;
+        }
+        __syncthreads();
+        k_lo = ex[0];
+        all_lo = ex[1];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) {
+            k_lo = min(k_lo, ex[2 * w]);
+            all_lo = max(all_lo, ex[2 * w + 1]);
+        }
+        __syncthreads();
+    }
+    int t0 = k_lo / kKeys, t1 = k_hi > k_lo ? (k_hi + kKeys - 1) / kKeys : t0;
+    if (a.nsplit > 1) {   // this block's run of them
+        const int n = t1 - t0, from = (int)((int64_t)n * split / a.nsplit), to = (int)((int64_t)n * (split + 1) / a.nsplit);
+        t1 = t0 + to;
+        t0 += from;
+    }
+
+    t0 = __builtin_amdgcn_readfirstlane(t0);
+    t1 = __builtin_amdgcn_readfirstlane(t1);
+
+    // KV row of key (tile, lane), and which keys of a tile have none.  Those, and what lies behind the last key, take a row
+    // that is there: whatever the memory behind them holds reaches no product.
+    const int max_key = max(k_hi - 1, 0);
+    uint64_t bad = 0;
+    auto rows_of = [&](int t) -> int64_t {
+        const int64_t r = cache_row(v, b, kv, min(t * kKeys + (kKeys == 64 ? lane : (lane & 31)), max_key));
+        const uint64_t ok = __ballot(r >= 0);
+        bad = ~ok;
+        if (ok == ~0ull) return r;
+        if (!ok) return 0;
+        const int l = __builtin_ctzll(ok);
+        const int64_t other = ((int64_t)__builtin_amdgcn_readlane((int)(r >> 32), l) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)r, l);
+        return r >= 0 ? r : other;
+    };
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_at(smem));
+    auto fetch = [&](int buf, int64_t r) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int at0 = (wave * kLoads + j) * kPer, key = at0 + lane / RowTile<T>::kChunks, c = (lane % RowTile<T>::kChunks) ^ swz<T>(key);
+            const int64_t from = (((int64_t)__shfl((int)(r >> 32), key) << 32) | (uint32_t)__shfl((int)r, key)) * RowTile<T>::kRowBytes + 16 * c;
+            const uint32_t to = lds0 + buf * 2 * kTile + at0 * RowTile<T>::kRowBytes;
+            row_to_lds(to, (const char *)a.k_pages + from);
+            row_to_lds(to + kTile, (const char *)a.v_pages + from);
+        }
+    };
+
+    f32x16_t o[4] = {};
+    float m = -INFINITY, l = 0.0f;
+    const float slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
+    uint64_t bad_now = 0;
+    int64_t next = 0;
+    if (t0 < t1) {
+        fetch(0, rows_of(t0));
+        bad_now = bad;
+        if (t0 + 1 < t1) next = rows_of(t0 + 1);
+        loads_landed();
+        __syncthreads();
+    }
+    for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1;
+        const uint64_t bad_next = bad;
+        if (t + 1 < t1) {
+            fetch(buf ^ 1, next);
+            if (t + 2 < t1) next = rows_of(t + 2);
+        }
+        char *kt = smem[buf][0], *vt = smem[buf][1];
+        const int key0 = t * kKeys;
+        const bool masked = key0 + kKeys > all_hi || key0 < all_lo || bad_now != 0;
+        if (masked) {
+            // A key that a row does not see has probability 0 there, but 0 times an infinity or NaN is no 0.  Values that are
+            // not finite are added to the rows that see them and then taken out of the tile.
+            const int words = kTile / 4 / (64 * NW);
+            uint32_t *w = reinterpret_cast<uint32_t *>(vt) + threadIdx.x * words;
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < words; ++i) {
+                const uint32_t x = w[i];
+                odd |= sizeof(T) == 2 ? (((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0 : (x & 0x7f800000u) == 0x7f800000u;
+            }
+            if (__syncthreads_or(odd)) {
+                for (int k = 0; k < kKeys; ++k) {
+                    const bool sees = key0 + k >= sight.lo && key0 + k < sight.hi && !((bad_now >> k) & 1);
+#pragma unroll
+                    for (int db = 0; db < 4; ++db)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int d = 32 * db + 8 * (i >> 2) + 4 * half + (i & 3), c = d * (int)sizeof(T) / 16;
+                            const char *p = vt + k * RowTile<T>::kRowBytes + ((c ^ swz<T>(k)) << 4) + (d * (int)sizeof(T) & 15);
+                            float x;
+                            if constexpr (sizeof(T) == 2) x = __uint_as_float((uint32_t)*reinterpret_cast<const bf16_t *>(p) << 16);
+                            else x = *reinterpret_cast<const float *>(p);
+                            if (sees && !(fabsf(x) < INFINITY)) o[db][i] += x;
+                        }
+                }
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < words; ++i) {
+                    uint32_t x = w[i];
+                    if constexpr (sizeof(T) == 2) {
+                        if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+                        if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
+                    } else if ((x & 0x7f800000u) == 0x7f800000u)
+                        x = 0;
+                    w[i] = x;
+                }
+                __syncthreads();
+            }
+        }
+        // scores
+        f32x16_t sc[kBlocks];
+        float top = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < kBlocks; ++kb) {
+            sc[kb] = rows_dot<T>(kt, 32 * kb, q, f32x16_t{});
+            score_regs<OPT>(sc[kb], a.o, slope2, sight.pos - (key0 + 32 * kb), half);
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int k = 32 * kb + 8 * (i >> 2) + 4 * half + (i & 3);
+                    const bool sees = key0 + k >= sight.lo && key0 + k < sight.hi && !((bad_now >> k) & 1);
+                    sc[kb][i] = sees ? sc[kb][i] : -INFINITY;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
+        }
+        top = half_max(top);
+        if constexpr (OPT == 0) top *= a.o.c2;
+        if (__any(top > m)) {
+            const float m_new = fmaxf(m, top), scale = m == -INFINITY ? 1.0f : exp2_fast(m - m_new);   // (nothing to scale, or infinities)
+            m = m_new;
+            l *= scale;
+#pragma unroll
+            for (int db = 0; db < 4; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[db][i] *= scale;
+        }
+        const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int kb = 0; kb < kBlocks; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float p = exp2_fast(OPT == 0 ? fmaf(sc[kb][i], a.o.c2, -ref) : sc[kb][i] - ref);
+                l += p;
+                sc[kb][i] = p;
+            }
+        // O^T += V^T P^T.  In bf16 the probabilities are rounded to the values' type, as the matrix cores take them: off by 2^-9 each at most, which is
+        // what rounding the output costs; the sum under them is of the unrounded ones.
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int kb = 0; kb < kBlocks; ++kb)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    bf16x8_t p;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) p[j] = (__bf16)sc[kb][8 * ks + j];
+#pragma unroll
+                    for (int db = 0; db < 4; ++db) {
+                        union { s16x4_t h[2]; bf16x8_t w; } x;
+#pragma unroll
+                        for (int aa = 0; aa < 2; ++aa) {
+                            const int k = 32 * kb + 16 * ks + 8 * aa + 4 * half + ((lane & 15) >> 2);
+                            const int c = (4 * db + 2 * ((lane & 31) >> 4) + ((lane & 3) >> 1)) ^ swz<T>(k);
+                            x.h[aa] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CTKVR_LDS s16x4_t *)(vt + k * 256 + (c << 4) + 8 * (lane & 1)));
+                        }
+                        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.w, p, o[db], 0, 0, 0);
+                    }
+                }
+        } else {
+#pragma unroll
+            for (int kb = 0; kb < kBlocks; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int k = 32 * kb + 8 * (i >> 2) + 4 * half + (i & 3), s = swz<T>(k);
+#pragma unroll
+                    for (int db = 0; db < 4; ++db) {
+                        const int d = 32 * db + (lane & 31);
+                        const float x = *reinterpret_cast<const float *>(vt + k * 512 + (((d >> 2) ^ s) << 4) + 4 * (d & 3));
+                        o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, sc[kb][i], o[db], 0, 0, 0);
+                    }
+                }
+        }
+        bad_now = bad_next;
+        loads_landed();
+        __syncthreads();
+    }
+
+    l = half_sum(l);
+    if (row >= rows) return;
+    const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);   // (NaN stays)
+    const float lse = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : (l == 0.0f ? -INFINITY : l);
+    const size_t at_row = (size_t)(s.c0 + token) * v.h + head;
+    if (a.nsplit > 1) {
+        const size_t n = (size_t)split * v.total * v.h + at_row;
+        if (half == 0) a.part_lse[n] = lse;
+        if (t0 < t1) {
+#pragma unroll
+            for (int db = 0; db < 4; ++db)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f32x4_t x;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) x[c] = o[db][4 * i + c] * inv;
+                    *reinterpret_cast<f32x4_t *>(a.part_o + n * 128 + 32 * db + 8 * i + 4 * half) = x;
+                }
+        }
+        return;
+    }
+    if (a.lse && half == 0) a.lse[at_row] = lse;
+    T *out = (T *)a.out + at_row * 128;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int d = 32 * db + 8 * i + 4 * half;
+            if constexpr (sizeof(T) == 2) {
+                bf16x4_t x;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) x[c] = (__bf16)(o[db][4 * i + c] * inv);
+                *reinterpret_cast<bf16x4_t *>(out + d) = x;
+            } else {
+                f32x4_t x;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) x[c] = o[db][4 * i + c] * inv;
+                *reinterpret_cast<f32x4_t *>(out + d) = x;
+            }
+        }
+}
+
+// The runs of a row joined by their log-sum-exps: 32 lanes a row
+template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
+{
+    const int rows = min(max(a.v.cu[a.v.batch], 0), a.v.total) * a.v.h;   // (tokens behind the last sequence have no runs)
+    const int row = blockIdx.x * 8 + (threadIdx.x >> 5), l32 = threadIdx.x & 31;
+    if (row >= rows || row < a.v.cu[0] * a.v.h) return;
+    const size_t step = (size_t)a.v.total * a.v.h;
+    float top = -INFINITY, nan = 0.0f;
+    for (int i = l32; i < a.nsplit; i += 32) {
+        const float x = a.part_lse[i * step + row];
+        top = fmaxf(top, x);
+        if (x != x) nan = x;
+    }
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        top = fmaxf(top, __shfl_xor(top, d));
+        nan += __shfl_xor(nan, d);
+    }
+    f32x4_t o = {};
+    float sum = 0.0f;
+    const float ref = top == -INFINITY ? 0.0f : top;
+    for (int i = 0; i < a.nsplit; ++i) {
+        const float x = a.part_lse[i * step + row];
+        if (x == -INFINITY) continue;
+        const float w = exp2_fast((x - ref) * kLog2e);
+        sum += w;
+        const f32x4_t p = *reinterpret_cast<const f32x4_t *>(a.part_o + (i * step + row) * 128 + 4 * l32);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] = fmaf(w, p[c], o[c]);
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    if (a.lse && l32 == 0) a.lse[row] = nan != nan ? nan : sum == 0.0f ? -INFINITY : ref + __builtin_amdgcn_logf(sum) * kLn2;
+    T *out = (T *)a.out + (size_t)row * 128 + 4 * l32;
+    if constexpr (sizeof(T) == 2) {
+        bf16x4_t x;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[c] = (__bf16)(o[c] * inv);
+        *reinterpret_cast<bf16x4_t *>(out) = x;
+    } else {
+        *reinterpret_cast<f32x4_t *>(out) = o * inv;
+    }
+}
+
+// ---- accumulated attention weight ----------------------------------------------------------------------
+struct WeightArgs {
+    CacheView v;
+    ScoreOpts o;
+    const void *q;
+    int64_t q_stride;
+    const float *lse;       // [total][h]
+    const void *k_pages;
+    const float *w_in;      // [batch][g][w_stride] or null
+    float *w_out;
+    int w_stride;
+    float decay;
+    int key_tiles;          // of a sequence, at most
+};
+
+// One block 4 x 32 kBlocks keys of a unit; a wave keeps its keys as operands and adds up their probabilities over the rows, which come
+// through shared memory.  A key's sum has one owner: the same in every call.
+template <typename T, int OPT> __global__ __launch_bounds__(256) void weights_kernel(WeightArgs a)
+{
+    constexpr int kBlocks = sizeof(T) == 2 ? 2 : 1, kKeys = 128 * kBlocks;
+    constexpr int kRows = RowTile<T>::kRows, kTile = RowTile<T>::kBytes, kPer = RowTile<T>::kRowsPerLoad, kLoads = kRows / (4 * kPer);
+    __shared__ __align__(16) char smem[2][kTile];
+    const CacheView &v = a.v;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int kv = blockIdx.x % v.g, b = blockIdx.x / v.g % v.batch, key0 = blockIdx.x / v.g / v.batch * kKeys, mine0 = key0 + 32 * kBlocks * wave;
+    const SeqSpan s = seq_span(v, b);
+    if (key0 >= s.len) return;
+    const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
+    const int rows = s.n << v.lg;
+
+    Operand<T> k[kBlocks];
+    uint64_t bad = 0;   // keys of the wave that are not there
+#pragma unroll
+    for (int kb = 0; kb < kBlocks; ++kb) {
+        const int key = mine0 + 32 * kb + (lane & 31);
+        const int64_t r = key < s.len ? cache_row(v, b, kv, key) : -1;
+        bad |= (__ballot(r < 0) & 0xffffffffull) << (32 * kb);
+        load_operand(k[kb], (const T *)a.k_pages + max(r, (int64_t)0) * 128, half);
+    }
+
+    // rows that may see one of the block's keys
+    const int tok0 = prefix > key0 ? 0 : min(max(key0 - s.old, 0), s.n), tok_pos = max(0, -s.old);
+    const int t0 = (max(tok0, min(tok_pos, s.n)) << v.lg) / kRows, t1 = (rows + kRows - 1) / kRows;
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_at(smem));
+    auto row_at = [&](int row, int *token) -> int64_t {
+        row = min(row, rows - 1);
+        *token = row >> v.lg;
+        return (int64_t)(s.c0 + *token) * a.q_stride + ((kv << v.lg) + (row & ((1 << v.lg) - 1))) * 128;
+    };
+    auto fetch = [&](int buf, int t) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int at0 = (wave * kLoads + j) * kPer, r = at0 + lane / RowTile<T>::kChunks, c = (lane % RowTile<T>::kChunks) ^ swz<T>(r);
+            int token;
+            row_to_lds(lds0 + buf * kTile + at0 * RowTile<T>::kRowBytes, (const char *)((const T *)a.q + row_at(t * kRows + r, &token)) + 16 * c);
+        }
+    };
+    f32x16_t sum[kBlocks] = {};
+    if (t0 < t1) fetch(0, t0);
+    for (int t = t0; t < t1; ++t) {
+        loads_landed();
+        __syncthreads();
+        if (t + 1 < t1) fetch((t - t0 + 1) & 1, t + 1);
+#pragma unroll
+        for (int rb = 0; rb < kRows / 32; ++rb) {
+            const int row = t * kRows + 32 * rb + (lane & 31);
+            int token;
+            (void)row_at(row, &token);
+            const int head = (kv << v.lg) + (min(row, rows - 1) & ((1 << v.lg) - 1));
+            RowSight sight = row_sight(v, a.o, s, prefix, token);
+            float lse = a.lse[(size_t)(s.c0 + token) * v.h + head];
+            if (row >= rows) sight.hi = 0;
+            const float nlse = lse == -INFINITY ? -INFINITY : -lse * kLog2e;   // (a row that sees nothing adds nothing)
+            const float slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
+            const char *qt = smem[(t - t0) & 1] + 32 * rb * RowTile<T>::kRowBytes;
+            // the rows are this product's second operand
+            Operand<T> q;
+#pragma unroll
+            for (int i = 0; i < (int)(sizeof(q.c) / 16); ++i) {
+                using C = std::remove_reference_t<decltype(q.c[0])>;
+                q.c[i] = *reinterpret_cast<const C *>(qt + (lane & 31) * RowTile<T>::kRowBytes + (((2 * i + half) ^ swz<T>(32 * rb + (lane & 31))) << 4));
+            }
+#pragma unroll
+            for (int kb = 0; kb < kBlocks; ++kb) {
+                const int k0 = mine0 + 32 * kb;
+                const bool masked = !__all(sight.lo <= k0 && sight.hi >= k0 + 32) || ((bad >> (32 * kb)) & 0xffffffffull) != 0;
+                if (masked && !__any(sight.lo < k0 + 32 && sight.hi > k0)) continue;
+                f32x16_t sc = {};
+                if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kb].c[i], q.c[i], sc, 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_32x32x2f32(k[kb].c[i][e], q.c[i][e], sc, 0, 0, 0);
+                }
+                score_regs<OPT>(sc, a.o, slope2, sight.pos - k0, half);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    float p = exp2_fast(OPT == 0 ? fmaf(sc[i], a.o.c2, nlse) : sc[i] + nlse);
+                    if (masked) {
+                        const int kk = 8 * (i >> 2) + 4 * half + (i & 3);
+                        p = k0 + kk >= sight.lo && k0 + kk < sight.hi && !((bad >> (32 * kb + kk)) & 1) ? p : 0.0f;
+                    }
+                    sum[kb][i] += p;
+                }
+            }
+        }
+    }
+    const size_t unit = ((size_t)b * v.g + kv) * a.w_stride;
+#pragma unroll
+    for (int kb = 0; kb < kBlocks; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float x = sum[kb][i];
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) x += __shfl_xor(x, d);
+            const int key = mine0 + 32 * kb + 8 * (i >> 2) + 4 * half + (i & 3);
+            if ((lane & 31) == i && key < s.len) {
+                if (a.w_in && key < s.old) x = fmaf(a.decay, a.w_in[unit + key], x);
+                a.w_out[unit + key] = x;
+            }
+        }
+}
+
+// ---- append with rotary positions -----------------------------------------------------------------------
+// Angles.  A pair's frequency is held as a 64-bit fraction of a turn, so that position times frequency modulo 2^64 is the angle modulo a
+// turn, exactly: a position of 2^31 is off by 2^-34 of a turn at most, where a product in 32 bits would have lost it.
+struct RopeTable {
+    uint64_t turn[64];
+    uint8_t axis[64];
+};
+struct AppendArgs {
+    CacheView v;
+    RopeTable rope;
+    const void *q, *k, *val;
+    int64_t q_stride, k_stride, v_stride;
+    const int32_t *positions;   // [axes][total] or null: the token's place in the cache on every axis
+    void *q_out, *k_pages, *v_pages;
+    int parts;                  // blocks a token's rows are shared out over
+};
+
+// sine and cosine of u / 2^32 turns: an eighth of a turn either side of a quarter, by their series (off by 2e-9)
+__device__ __forceinline__ void sincos_turn(uint32_t u, float *sn, float *cs)
+{
+    const uint32_t quarter = (u + 0x20000000u) >> 30;
+    const float x = (float)(int32_t)(u - (quarter << 30)) * 1.46291807926715968105e-9f, y = x * x;   // 2 pi / 2^32
+    float s = fmaf(y, 2.7557319223985893e-6f, -1.9841269841269841e-4f);
+    s = fmaf(y, s, 8.3333333333333333e-3f);
+    s = fmaf(y, s, -1.6666666666666667e-1f);
+    s = fmaf(x * y, s, x);
+    float c = fmaf(y, -2.7557319223985888e-7f, 2.4801587301587302e-5f);
+    c = fmaf(y, c, -1.3888888888888889e-3f);
+    c = fmaf(y, c, 4.1666666666666667e-2f);
+    c = fmaf(y, c, -0.5f);
+    c = fmaf(y, c, 1.0f);
+    const float a = (quarter & 1) ? c : s, b = (quarter & 1) ? s : c;
+    *sn = (quarter & 2) ? -a : a;
+    *cs = (quarter == 1 || quarter == 2) ? -b : b;
+}
+
+__device__ __forceinline__ void store_chunk(float *p, const float (&x)[8])
+{
+    reinterpret_cast<float4 *>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void store_chunk(bf16_t *p, const float (&x)[8])
+{
+    bf16x8_t v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (__bf16)x[i];
+    *reinterpret_cast<bf16x8_t *>(p) = v;
+}
+
+// A wave has a token (or one of `parts` shares of its rows): lane i turns pair i's angle into sine and cosine, once for all heads, then 8 lanes
+// take a row, the chunks i and i + 8 of 8 elements each.
+template <typename T> __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
+{
+    __shared__ float2 turn[4][64];
+    const CacheView &v = a.v;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, unit = blockIdx.x * 4 + wave;
+    const int token = unit / a.parts, part = unit % a.parts;
+    if (token >= v.total) return;
+    // the token's sequence: the last one that begins at or before it
+    int b = -1;
+    for (int b0 = 0; b0 < v.batch; b0 += 64) {
+        const bool before = b0 + lane < v.batch && v.cu[b0 + lane] <= token && v.cu[b0 + lane + 1] > token;
+        const uint64_t hit = __ballot(before);
+        if (hit) {
+            b = b0 + __builtin_ctzll(hit);
+            break;
+        }
+    }
+    if (b < 0) return;   // behind the last sequence
+    const SeqSpan s = seq_span(v, b);
+    const int slot = s.old + token - s.c0;
+    const int pos = a.positions ? a.positions[(size_t)a.rope.axis[lane] * v.total + token] : slot;
+    float2 t;
+    sincos_turn((uint32_t)(((uint64_t)(int64_t)pos * a.rope.turn[lane]) >> 32), &t.y, &t.x);
+    turn[wave][lane] = t;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const int i8 = lane & 7;
+    float cs[8], sn[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float2 x = turn[wave][8 * i8 + i];
+        cs[i] = x.x;
+        sn[i] = x.y;
+    }
+    const bool held = slot >= 0 && slot < s.len;
+    uint32_t page = held ? (uint32_t)v.table[(size_t)b * v.max_pages + (slot >> v.page_shift)] : 0xffffffffu;
+    const int nq = a.q ? v.h : 0, nk = a.k ? v.g : 0, rows = nq + 2 * nk;
+    for (int r = part * 8 + (lane >> 3); r < rows; r += 8 * a.parts) {
+        const int kv = r - nq;
+        const T *from = r < nq ? (const T *)a.q + (int64_t)token * a.q_stride + r * 128
+                        : kv < nk ? (const T *)a.k + (int64_t)token * a.k_stride + kv * 128
+                                  : (const T *)a.val + (int64_t)token * a.v_stride + (kv - nk) * 128;
+        const Chunk<T> lo = load_chunk(from, i8), hi = load_chunk(from, i8 + 8);
+        T *to;
+        if (r < nq) {
+            to = (T *)a.q_out + ((size_t)token * v.h + r) * 128;
+        } else {
+            if (page >= v.num_pages) continue;
+            const int64_t row = (((int64_t)page * v.g + (kv < nk ? kv : kv - nk)) << v.page_shift) + (slot & ((1 << v.page_shift) - 1));
+            to = (T *)(kv < nk ? a.k_pages : a.v_pages) + row * 128;
+        }
+        if (kv >= nk) {   // values as they are
+            *reinterpret_cast<Chunk<T> *>(to + 8 * i8) = lo;
+            *reinterpret_cast<Chunk<T> *>(to + 64 + 8 * i8) = hi;
+            continue;
+        }
+        float x[8], y[8], p[8], q[8];
+        unpack(lo, x);
+        unpack(hi, y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            p[i] = fmaf(x[i], cs[i], -(y[i] * sn[i]));
+            q[i] = fmaf(y[i], cs[i], x[i] * sn[i]);
+        }
+        store_chunk(to + 8 * i8, p);
+        store_chunk(to + 64 + 8 * i8, q);
+    }
+}
+
+// ---- eviction ----------------------------------------------------------------------------------------------
+struct EvictArgs {
+    CacheView v;
+    const float *w_in;     // [batch][g][w_stride]
+    float *w_out;          // the same, or null
+    int w_stride;
+    int budget, n_init, n_local;
+    int32_t *ids;          // [batch][g][budget]
+    int32_t *lens;         // [batch] or null
+    void *k_pages, *v_pages;
+    int slices;
+};
+
+// a weight's rank: larger weights have larger words, -0 is +0, NaN comes last
+__device__ __forceinline__ uint32_t weight_rank(float w)
+{
+    if (w != w) return 0;
+    const uint32_t u = __float_as_uint(w + 0.0f);
+    return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+
+// One block a unit: the rank of the last weight that stays, by four rounds of 8 bits over the keys that are free to go, then the kept ids in order, each
+// wave from a run of the keys of its own.
+__global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a)
+{
+    __shared__ uint32_t hist[256], found[2], count[2][16];
+    const CacheView &v = a.v;
+    const int unit = blockIdx.x, b = unit / v.g, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int len = min(max(v.cur[b], 0), v.max_pages << v.page_shift), keep = min(len, a.budget);
+    int32_t *ids = a.ids + (size_t)unit * a.budget;
+    const float *w = a.w_in + (size_t)unit * a.w_stride;
+    if (a.lens && unit % v.g == 0 && threadIdx.x == 0) a.lens[b] = keep;
+    for (int j = keep + threadIdx.x; j < a.budget; j += 1024) ids[j] = -1;
+    if (keep == len) {
+        for (int j = threadIdx.x; j < len; j += 1024) ids[j] = j;
+        return;
+    }
+    const int from = a.n_init, to = len - a.n_local;
+    uint32_t want = keep - a.n_init - a.n_local, prefix = 0, mask = 0;   // want: how many of those with the prefix stay
+    for (int shift = 24; shift >= 0 && want; shift -= 8) {
+        if (threadIdx.x < 256) hist[threadIdx.x] = 0;
+        __syncthreads();
+        for (int t = from + threadIdx.x; t < to; t += 1024) {
+            const uint32_t r = weight_rank(w[t]);
+            if ((r & mask) == prefix) atomicAdd(&hist[(r >> shift) & 255], 1u);
+        }
+        __syncthreads();
+        if (wave == 0) {   // from the largest bin down: the one in which the want-th lies
+            uint32_t mine[4], all = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) all += mine[i] = hist[255 - (4 * lane + i)];
+            uint32_t upto = all;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const uint32_t o = __shfl_up(upto, d);
+                if (lane >= d) upto += o;
+            }
+            uint32_t above = upto - all;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (above < want && above + mine[i] >= want) {
+                    found[0] = 255 - (4 * lane + i);
+                    found[1] = want - above;
+                }
+                above += mine[i];
+            }
+        }
+        __syncthreads();
+        prefix |= found[0] << shift;
+        mask |= 255u << shift;
+        want = found[1];
+        __syncthreads();
+    }
+    // above the prefix (the rank itself) a weight stays, at it the first `want` do
+    const bool none = keep == a.n_init + a.n_local;
+    const int run = ((to - from + 15) / 16 + 63) & ~63, my0 = from + wave * run, my1 = min(my0 + run, to);
+    uint32_t over = 0, tie = 0;
+    if (!none) {
+        for (int t = my0 + lane; t < my1; t += 64) {
+            const uint32_t r = weight_rank(w[t]);
+            over += r > prefix;
+            tie += r == prefix;
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            over += __shfl_xor(over, d);
+            tie += __shfl_xor(tie, d);
+        }
+    }
+    if (lane == 0) {
+        count[0][wave] = over;
+        count[1][wave] = tie;
+    }
+    __syncthreads();
+    uint32_t ties = 0, at = a.n_init;
+    for (int i = 0; i < wave; ++i) {
+        at += count[0][i] + min(count[1][i], want - min(want, ties));
+        ties += count[1][i];
+    }
+    if (!none)
+        for (int t0 = my0; t0 < my1; t0 += 64) {
+            const uint32_t r = t0 + lane < my1 ? weight_rank(w[t0 + lane]) : 0;
+            const uint64_t here = __ballot(t0 + lane < my1 && r == prefix), below = (1ull << lane) - 1;
+            const bool stays = t0 + lane < my1 && (r > prefix || (r == prefix && ties + __popcll(here & below) < want));
+            const uint64_t kept = __ballot(stays);
+            if (stays) ids[at + __popcll(kept & below)] = t0 + lane;
+            at += __popcll(kept);
+            ties += __popcll(here);
+        }
+    for (int j = threadIdx.x; j < a.n_init; j += 1024) ids[j] = j;
+    for (int j = threadIdx.x; j < a.n_local; j += 1024) ids[keep - a.n_local + j] = to + j;
+}
+
+// The kept rows to the front, in order and in place.  Row j comes from ids[j] >= j, so rounds of rows, read as a whole before the first of them is
+// written, overwrite nothing that a later round reads; a block has 1 / slices of every row of its unit, which no other block touches.
+template <typename T> __global__ __launch_bounds__(512) void evict_move_kernel(EvictArgs a)
+{
+    constexpr int kPieces = 2 * 128 * sizeof(T) / 16, kEach = 8;   // 16-byte pieces of a key's K and V rows
+    const CacheView &v = a.v;
+    const int unit = blockIdx.x / a.slices, slice = blockIdx.x % a.slices, b = unit / v.g, kv = unit % v.g;
+    const int len = min(max(v.cur[b], 0), v.max_pages << v.page_shift), keep = min(len, a.budget);
+    const int32_t *ids = a.ids + (size_t)unit * a.budget;
+    const size_t w0 = (size_t)unit * a.w_stride;
+    const bool weights = a.w_out && slice == 0;
+    if (keep == len) {
+        if (weights && a.w_out != a.w_in)
+            for (int j = threadIdx.x; j < keep; j += 512) a.w_out[w0 + j] = a.w_in[w0 + j];
+        return;
+    }
+    const int wide = kPieces / a.slices, lane_rows = 512 / wide, my = threadIdx.x / wide, piece = slice * wide + threadIdx.x % wide;
+    char *pages = (char *)(piece < kPieces / 2 ? a.k_pages : a.v_pages) + 16 * (piece % (kPieces / 2));
+    for (int j0 = 0; j0 < keep; j0 += lane_rows * kEach) {
+        u32x4_t x[kEach];
+        char *to[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int j = j0 + i * lane_rows + my;
+            to[i] = nullptr;
+            if (j >= keep || ids[j] == j) continue;
+            const int64_t src = cache_row(v, b, kv, ids[j]), dst = cache_row(v, b, kv, j);
+            if (src < 0 || dst < 0) continue;
+            to[i] = pages + dst * 128 * (int64_t)sizeof(T);
+            x[i] = *reinterpret_cast<const u32x4_t *>(pages + src * 128 * (int64_t)sizeof(T));
+        }
+        loads_landed();
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (to[i]) *reinterpret_cast<u32x4_t *>(to[i]) = x[i];
+    }
+    if (weights)
+        for (int j0 = 0; j0 < keep; j0 += 512) {
+            const int j = j0 + threadIdx.x;
+            const float x = j < keep ? a.w_in[w0 + ids[j]] : 0.0f;
+            loads_landed();
+            __syncthreads();
+            if (j < keep) a.w_out[w0 + j] = x;
+        }
+}
+
+}  // namespace ctkvr

@@ -20,14 +20,15 @@
 #include "kernels.hpp"
 #include "kmeans.hpp"
 #include "fused_args.hpp"
+#include "host.hpp"
 
 using namespace ctkvr;
 
 namespace {
-
 thread_local std::string g_err;
+}  // namespace
 
-int fail(int code, const char *fmt, ...)
+int ctkvr::fail(int code, const char *fmt, ...)
 {
     char buf[512];
     va_list ap;
@@ -38,30 +39,7 @@ int fail(int code, const char *fmt, ...)
     return code;
 }
 
-#define HIP_TRY(expr)                                                                           \
-    do {                                                                                        \
-        hipError_t e_ = (expr);                                                                 \
-        if (e_ != hipSuccess)                                                                   \
-            return fail(e_ == hipErrorOutOfMemory ? CTKVR_ENOMEM : CTKVR_EHIP, "%s: %s", #expr, \
-                        hipGetErrorString(e_));                                                 \
-    } while (0)
-
-// Makes a device the calling thread's current one for a scope.  Events, the null stream, function attributes and
-// device-wide waits are those of the current device, which need not be the one an index lives on.
-struct DeviceScope {
-    int before = -1;
-    hipError_t err;
-    explicit DeviceScope(int dev)
-    {
-        err = hipGetDevice(&before);
-        if (err == hipSuccess && before == dev) before = -1;   // nothing to restore
-        else err = hipSetDevice(dev);
-    }
-    ~DeviceScope()
-    {
-        if (before >= 0) (void)hipSetDevice(before);
-    }
-};
+namespace {
 
 size_t elem_size(int dtype) { return dtype == CTKVR_BF16 ? 2 : 4; }
 
@@ -110,10 +88,6 @@ int static_scratch(unsigned char **out)
 // be waited for while one of its streams is being captured in global mode -- the block is set aside: nothing has it, and it is not
 // freed, before a later wait for the device has succeeded (pool_settle).
 constexpr size_t kPoolMax = (size_t)2 << 30;
-struct PoolBlock {
-    void *base;
-    size_t bytes;
-};
 std::mutex g_pool_mu;
 std::vector<PoolBlock> g_pool[kMaxDevices];   // oldest first
 std::vector<PoolBlock> g_aside[kMaxDevices];  // blocks that work may still be using
@@ -132,13 +106,16 @@ void pool_drop(int dev)
     g_pool[dev].clear();
 }
 
-// the work on the current device has ended
-bool device_idle()
+}  // namespace
+
+bool ctkvr::device_idle()
 {
     if (hipDeviceSynchronize() == hipSuccess) return true;
     (void)hipGetLastError();   // (a launch's own check would report it)
     return false;
 }
+
+namespace {
 
 // an idle block into the pool, or to the runtime where it is not kept (the caller holds g_pool_mu)
 void pool_keep(int dev, PoolBlock b)
@@ -166,9 +143,9 @@ void pool_settle(int dev)
     g_aside[dev].clear();
 }
 
-// a block of at least `bytes` on the current device `dev`, and of at most bytes / spare more if it was kept; out->bytes is its
-// real size
-int pool_get(int dev, size_t bytes, size_t spare, PoolBlock *out)
+}  // namespace
+
+int ctkvr::pool_get(int dev, size_t bytes, size_t spare, PoolBlock *out)
 {
     const size_t grain = bytes < ((size_t)4 << 20) ? (size_t)64 << 10 : (size_t)2 << 20;
     bytes = (std::max<size_t>(bytes, 1) + grain - 1) / grain * grain;
@@ -205,8 +182,7 @@ int pool_get(int dev, size_t bytes, size_t spare, PoolBlock *out)
     return CTKVR_OK;
 }
 
-// gives a block of device `dev` back; idle: its users have been waited for
-void pool_put(int dev, PoolBlock b, bool idle)
+void ctkvr::pool_put(int dev, PoolBlock b, bool idle)
 {
     if (!b.base) return;
     if (dev < 0 || dev >= kMaxDevices) {
@@ -219,6 +195,8 @@ void pool_put(int dev, PoolBlock b, bool idle)
     else
         g_aside[dev].push_back(b);
 }
+
+namespace {
 
 // Scratch of one build, given back at the end of the scope: as idle if waited() has heard of a synchronisation that succeeded.
 struct BuildScratch {
@@ -461,12 +439,6 @@ struct ctkvr_index {
 };
 
 namespace {
-
-#define TRY(expr)                    \
-    do {                             \
-        int rc_ = (expr);            \
-        if (rc_ != CTKVR_OK) return rc_; \
-    } while (0)
 
 int check_params(const ctkvr_params *p, const int32_t *ctx_lens)
 {
