@@ -50,6 +50,8 @@ int check_cache_params(const ctkvr_cache_params *p)
         return fail(CTKVR_EUNSUPPORTED, "max_pages %d of %d tokens: sequences of 2^20 tokens at most", p->max_pages, p->page_size);
     if (p->max_new > (1 << 20) || p->batch > (1 << 16) || p->n_q_heads > (1 << 10))
         return fail(CTKVR_EUNSUPPORTED, "max_new %d, batch %d, n_q_heads %d: at most 2^20, 2^16, 2^10", p->max_new, p->batch, p->n_q_heads);
+    if ((int64_t)p->num_pages * p->page_size * p->n_kv_heads >= 0xffffffffll)
+        return fail(CTKVR_EUNSUPPORTED, "%d pages: a cache of 2^32 - 2 rows at most", p->num_pages);
     if ((((int64_t)p->max_pages * p->page_size + 127) / 128) * p->batch * p->n_kv_heads >= (1ll << 31))
         return fail(CTKVR_EUNSUPPORTED, "%d sequences of %d pages: too large a batch", p->batch, p->max_pages);
     if (!(p->sm_scale >= 0.0f) || std::isinf(p->sm_scale)) return fail(CTKVR_EINVAL, "sm_scale must be finite and >= 0");
@@ -115,14 +117,23 @@ int check_rows(const ctkvr_cache *c, const char *name, const void *p, int64_t st
     return CTKVR_OK;
 }
 
-// rows of a tile
-constexpr int kTileLog = 7;
-int attn_tiles(const ctkvr_cache *c, int total) { return (int)((((int64_t)total << c->lg) >> kTileLog) + std::min(total, c->p.batch)); }
-// Runs that a tile's keys are split into: as many as there are CUs for, of 256 keys at least
-int attn_splits(const ctkvr_cache *c, int total)
+// How a call's rows and keys fall into blocks.  Tiles of 128 rows read a key once for all of them; where they are too few for the chip, or most of their
+// rows would be empty, tiles of 32 rows whose keys a block's waves share out.  Either way the keys are split into runs where that gives every CU work.
+struct AttnPlan {
+    bool few;
+    int tiles, nsplit;
+};
+AttnPlan attn_plan(const ctkvr_cache *c, int total)
 {
-    const int64_t blocks = (int64_t)attn_tiles(c, total) * c->p.n_kv_heads, keys = (int64_t)c->p.max_pages * c->p.page_size;
-    return (int)std::max<int64_t>(1, std::min({2 * c->num_cu / std::max<int64_t>(blocks, 1), (keys + 255) / 256, (int64_t)kMaxSplit}));
+    const int64_t rows = (int64_t)total << c->lg, keys = (int64_t)c->p.max_pages * c->p.page_size, g = c->p.n_kv_heads, cus = c->num_cu;
+    const int used = std::min(total, c->p.batch);   // sequences with new tokens, at most
+    AttnPlan p{};
+    const int64_t wide = (rows >> 7) + used;
+    p.few = rows <= 64ll * used || wide * g < cus;
+    p.tiles = (int)(p.few ? (rows >> 5) + used : wide);
+    const int64_t blocks = p.tiles * g, want = p.few ? (used > 1 ? 8 * cus : cus) : cus, least = p.few ? 256 : 512;
+    p.nsplit = (int)std::max<int64_t>(1, std::min({want / blocks, (keys + least - 1) / least, (int64_t)kMaxSplit}));
+    return p;
 }
 
 template <typename F> int with_opts(int opt, F f)
@@ -140,14 +151,20 @@ int launched(const char *what)
     return e == hipSuccess ? CTKVR_OK : fail(CTKVR_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-template <typename T> int attn_launch(const ctkvr_cache *c, AttnArgs &a, int opt, hipStream_t st)
+template <typename T> int attn_launch(const ctkvr_cache *c, AttnArgs &a, bool few, int opt, hipStream_t st)
 {
     const unsigned grid = (unsigned)((int64_t)a.tiles * c->p.n_kv_heads * a.nsplit);
     with_opts(opt, [&](auto o) {
-        attn_kernel<T, decltype(o)::value, 4><<<dim3(grid), 256, 0, st>>>(a);
+        constexpr int kOpt = decltype(o)::value, kFew = sizeof(T) == 2 ? 4 : 2;
+        if (few) attn_few_kernel<T, kOpt, kFew><<<dim3(grid), 64 * kFew, 0, st>>>(a);
+        else attn_kernel<T, kOpt, 4><<<dim3(grid), 256, 0, st>>>(a);
         return 0;
     });
-    if (a.nsplit > 1) attn_join_kernel<T><<<dim3((unsigned)(((int64_t)a.v.total * c->p.n_q_heads + 7) / 8)), 256, 0, st>>>(a);
+    if (a.nsplit > 1) {
+        const unsigned rows = (unsigned)((int64_t)a.v.total * c->p.n_q_heads);
+        if (a.nsplit >= 8) attn_join_kernel<T, 8><<<dim3(rows), 256, 0, st>>>(a);
+        else attn_join_kernel<T, 1><<<dim3((rows + 7) / 8), 256, 0, st>>>(a);
+    }
     return launched("ctkvr_cache_attn");
 }
 template <typename T> int weights_launch(const ctkvr_cache *c, const WeightArgs &a, int opt, hipStream_t st)
@@ -193,9 +210,8 @@ int ctkvr_cache_create(const ctkvr_cache_params *p, ctkvr_cache **out_cache)
     }
     // partial outputs, for the largest product of rows and runs that a call may take
     for (int total = 1; total <= p->max_new; ++total) {
-        const int n = attn_splits(c, total);
-        if (n == 1) break;   // (more tokens, fewer runs)
-        c->part_rows = std::max(c->part_rows, (size_t)n * total * p->n_q_heads);
+        const int n = attn_plan(c, total).nsplit;
+        if (n > 1) c->part_rows = std::max(c->part_rows, (size_t)n * total * p->n_q_heads);
     }
     if (c->part_rows) {
         const int rc = pool_get(c->dev, c->part_rows * 129 * 4, 4, &c->mem);
@@ -277,10 +293,12 @@ int ctkvr_cache_attn(ctkvr_cache *c, const void *q, int64_t q_stride, const void
     a.lse = out_lse;
     a.part_o = c->part_o;
     a.part_lse = c->part_lse;
-    a.tiles = attn_tiles(c, total);
-    a.nsplit = attn_splits(c, total);
+    const AttnPlan plan = attn_plan(c, total);
+    a.tiles = plan.tiles;
+    a.nsplit = plan.nsplit;
     const int opt = (c->p.softcap > 0.0f ? kCap : 0) | (slopes ? kBias : 0);
-    return c->p.dtype == CTKVR_BF16 ? attn_launch<bf16_t>(c, a, opt, (hipStream_t)hip_stream) : attn_launch<float>(c, a, opt, (hipStream_t)hip_stream);
+    return c->p.dtype == CTKVR_BF16 ? attn_launch<bf16_t>(c, a, plan.few, opt, (hipStream_t)hip_stream)
+                                    : attn_launch<float>(c, a, plan.few, opt, (hipStream_t)hip_stream);
 }
 
 int ctkvr_cache_weights(ctkvr_cache *c, const void *q, int64_t q_stride, const float *lse, const void *k_pages, const int32_t *cu_new,

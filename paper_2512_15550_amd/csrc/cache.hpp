@@ -21,6 +21,7 @@ typedef short s16x8_t __attribute__((ext_vector_type(8)));
 
 #define CTKVR_LDS __attribute__((address_space(3)))
 
+constexpr uint32_t kNoRow = 0xffffffffu;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // Tile `tile` of the tiles of 2^LOG rows that the batch's units of one KV head fall into, sequence by sequence: its sequence and its
@@ -70,9 +71,22 @@ __device__ __forceinline__ void row_to_lds(uint32_t to, const void *from)
 }
 __device__ __forceinline__ uint32_t lds_at(const void *p) { return (uint32_t)(uintptr_t)(const CTKVR_LDS void *)p; }
 
-// Loads in flight have landed, in registers and shared memory (of a wave: a barrier for the block behind it).  The compiler, which does not know of
-// those in assembly, would not wait for them at the barrier.
-__device__ __forceinline__ void loads_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Waits until at most N of the wave's loads are in flight.  (The builtin, which the compiler reckons with; of loads in assembly it does not know, so
+// that neither its own waits nor a barrier would be enough.)
+template <int N> __device__ __forceinline__ void loads_landed()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0f70);
+    asm volatile("" ::: "memory");
+}
+
+// ... and until shared memory has answered
+__device__ __forceinline__ void settled()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    asm volatile("" ::: "memory");
+}
 
 // One exchange between the halves of a wave
 __device__ __forceinline__ float half_max(float x)
@@ -158,12 +172,175 @@ struct AttnArgs {
     int tiles, nsplit;
 };
 
+// A key that a row does not see has probability 0 there, but 0 times an infinity or NaN is no 0.  So where a tile has such keys for some row, values
+// that are not finite are added to the rows that see them and then taken out of the tile.
+template <typename T, int KEYS, int THREADS> struct OddValues {
+    static constexpr int kWords = KEYS * 128 * (int)sizeof(T) / 4 / THREADS;
+    static __device__ __forceinline__ bool any(const char *vt, int tid)
+    {
+        const u32x4_t *w = reinterpret_cast<const u32x4_t *>(vt) + tid;
+        uint32_t odd = 0;
+#pragma unroll
+        for (int i = 0; i < kWords / 4; ++i) {
+            const u32x4_t x = w[i * THREADS];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (sizeof(T) == 2) odd |= ((x[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+                else odd |= ((x[e] & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+            }
+        }
+        return odd != 0;
+    }
+    static __device__ __forceinline__ void clean(char *vt, int tid)
+    {
+        uint32_t *w = reinterpret_cast<uint32_t *>(vt) + tid;
+        for (int i = 0; i < kWords; ++i) {
+            uint32_t x = w[i * THREADS];
+            if constexpr (sizeof(T) == 2) {
+                if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+                if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
+            } else if ((x & 0x7f800000u) == 0x7f800000u)
+                x = 0;
+            w[i * THREADS] = x;
+        }
+    }
+    static __device__ __forceinline__ void add(f32x16_t (&o)[4], const char *vt, const RowSight &sight, int key0, uint64_t bad, int half)
+    {
+        for (int n = 0; n < KEYS; ++n) {
+            int k = n;
+            asm volatile("" : "+s"(k));   // (its addresses are not worth registers in the loop over the tiles)
+            const bool sees = key0 + k >= sight.lo && key0 + k < sight.hi && !((bad >> k) & 1);
+#pragma unroll
+            for (int db = 0; db < 4; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int d = 32 * db + 8 * (i >> 2) + 4 * half + (i & 3), c = d * (int)sizeof(T) / 16;
+                    const char *p = vt + k * RowTile<T>::kRowBytes + ((c ^ swz<T>(k)) << 4) + (d * (int)sizeof(T) & 15);
+                    float x;
+                    if constexpr (sizeof(T) == 2) x = __uint_as_float((uint32_t)*reinterpret_cast<const bf16_t *>(p) << 16);
+                    else x = *reinterpret_cast<const float *>(p);
+                    if (sees && !(fabsf(x) < INFINITY)) o[db][i] += x;
+                }
+        }
+    }
+};
+
+// scores of what a row does not see become -infinity
+__device__ __forceinline__ void mask_regs(f32x16_t &s, const RowSight &sight, int key0, uint64_t bad, int half)
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int k = 8 * (i >> 2) + 4 * half + (i & 3);
+        const bool sees = key0 + k >= sight.lo && key0 + k < sight.hi && !((bad >> k) & 1);
+        s[i] = sees ? s[i] : -INFINITY;
+    }
+}
+
+// A tile's scores to probabilities under the running maximum m (in units of log2 e, as all exponents here), their sum to l, the outputs so far to the
+// new maximum.  While m is -infinity the outputs are 0, or infinities that stay.
+template <int OPT, int NB> __device__ __forceinline__ void softmax_regs(f32x16_t (&sc)[NB], f32x16_t (&o)[4], float &m, float &l, float c2)
+{
+    float top = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
+    top = half_max(top);
+    if constexpr (OPT == 0) top *= c2;
+    if (__any(top > m)) {
+        const float m_new = fmaxf(m, top), scale = m == -INFINITY ? 1.0f : exp2_fast(m - m_new);
+        m = m_new;
+        l *= scale;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[db][i] *= scale;
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float p = exp2_fast(OPT == 0 ? fmaf(sc[kb][i], c2, -ref) : sc[kb][i] - ref);
+            l += p;
+            sc[kb][i] = p;
+        }
+}
+
+// O^T += V^T P^T.  In bf16 the probabilities are rounded to the values' type, as the matrix cores take them: off by 2^-8 of themselves at most, which
+// is what rounding the output costs; the sum under them is of the unrounded ones.
+template <typename T, int NB> __device__ __forceinline__ void values_dot(f32x16_t (&o)[4], const char *vt, const f32x16_t (&sc)[NB], int lane)
+{
+    const int half = lane >> 5;
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) {
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                bf16x8_t p;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) p[j] = (__bf16)sc[kb][8 * ks + j];
+#pragma unroll
+                for (int db = 0; db < 4; ++db) {
+                    union { s16x4_t h[2]; bf16x8_t w; } x;
+#pragma unroll
+                    for (int aa = 0; aa < 2; ++aa) {
+                        const int k = 32 * kb + 16 * ks + 8 * aa + 4 * half + ((lane & 15) >> 2);
+                        const int c = (4 * db + 2 * ((lane & 31) >> 4) + ((lane & 3) >> 1)) ^ swz<T>(k);
+                        x.h[aa] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CTKVR_LDS s16x4_t *)(vt + k * 256 + (c << 4) + 8 * (lane & 1)));
+                    }
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.w, p, o[db], 0, 0, 0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int k = 32 * kb + 8 * (i >> 2) + 4 * half + (i & 3), s = swz<T>(k);
+#pragma unroll
+                for (int db = 0; db < 4; ++db) {
+                    const int d = 32 * db + (lane & 31);
+                    const float x = *reinterpret_cast<const float *>(vt + k * 512 + (((d >> 2) ^ s) << 4) + 4 * (d & 3));
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, sc[kb][i], o[db], 0, 0, 0);
+                }
+            }
+        }
+    }
+}
+
+// keys that some token of tok0 .. tok1 sees, and those that all of them see, as far as positions say
+struct KeyRange {
+    int hi, all_hi;
+};
+__device__ __forceinline__ KeyRange key_range(const SeqSpan &s, int prefix, int tok0, int tok1)
+{
+    const int pos0 = s.old + tok0, pos1 = s.old + tok1;
+    KeyRange r;
+    r.hi = pos1 < 0 ? 0 : min(max(pos1 + 1, prefix), s.len);
+    r.all_hi = pos0 < 0 ? 0 : min(max(pos0 + 1, prefix), s.len);
+    return r;
+}
+
+template <typename T> __device__ __forceinline__ void store4(T *p, const f32x4_t &x)
+{
+    if constexpr (sizeof(T) == 2) {
+        bf16x4_t y;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) y[c] = (__bf16)x[c];
+        *reinterpret_cast<bf16x4_t *>(p) = y;
+    } else {
+        *reinterpret_cast<f32x4_t *>(p) = x;
+    }
+}
+__device__ __forceinline__ float inv_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }   // (NaN stays)
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2; }
+
 // One block a tile of 32 NW rows of a unit and, where the keys are split, one of nsplit runs of their tiles; a wave has 32 rows.  Each
 // tile of keys goes straight to shared memory while the one before it is worked on; the maximum runs with them.
-template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW) void attn_kernel(AttnArgs a)
+template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void attn_kernel(AttnArgs a)
 {
     constexpr int kRowsLog = NW == 4 ? 7 : 8, kKeys = RowTile<T>::kRows, kBlocks = kKeys / 32, kTile = RowTile<T>::kBytes;
     constexpr int kPer = RowTile<T>::kRowsPerLoad, kLoads = kKeys / (NW * kPer);   // loads a wave makes of a tile of K, and of V
+    using Odd = OddValues<T, kKeys, 64 * NW>;
     static_assert(NW == 4 || NW == 8, "");
     __shared__ __align__(16) char smem[2][2][kTile];   // [buffer][K, V]
     const CacheView &v = a.v;
@@ -181,10 +358,7 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW) voi
     Operand<T> q;
     load_operand(q, (const T *)a.q + (int64_t)(s.c0 + token) * a.q_stride + head * 128, half);
 
-    // keys that some row of the block sees, and those that all of them see
-    const int tok0 = r0 >> v.lg, tok1 = (min(r0 + 32 * NW, rows) - 1) >> v.lg;
-    const int pos0 = s.old + tok0, pos1 = s.old + tok1;
-    const int k_hi = pos1 < 0 ? 0 : min(max(pos1 + 1, prefix), s.len), all_hi = pos0 < 0 ? 0 : min(max(pos0 + 1, prefix), s.len);
+    const KeyRange range = key_range(s, prefix, r0 >> v.lg, (min(r0 + 32 * NW, rows) - 1) >> v.lg);
     int k_lo = 0, all_lo = 0;
     if (a.o.first) {
         int lo = sight.lo, hi = sight.lo;
@@ -208,36 +382,34 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW) voi
         }
         __syncthreads();
     }
-    int t0 = k_lo / kKeys, t1 = k_hi > k_lo ? (k_hi + kKeys - 1) / kKeys : t0;
+    int t0 = k_lo / kKeys, t1 = range.hi > k_lo ? (range.hi + kKeys - 1) / kKeys : t0;
     if (a.nsplit > 1) {   // this block's run of them
         const int n = t1 - t0, from = (int)((int64_t)n * split / a.nsplit), to = (int)((int64_t)n * (split + 1) / a.nsplit);
         t1 = t0 + to;
         t0 += from;
     }
-
     t0 = __builtin_amdgcn_readfirstlane(t0);
     t1 = __builtin_amdgcn_readfirstlane(t1);
 
     // KV row of key (tile, lane), and which keys of a tile have none.  Those, and what lies behind the last key, take a row
     // that is there: whatever the memory behind them holds reaches no product.
-    const int max_key = max(k_hi - 1, 0);
+    const int max_key = max(range.hi - 1, 0);
     uint64_t bad = 0;
-    auto rows_of = [&](int t) -> int64_t {
-        const int64_t r = cache_row(v, b, kv, min(t * kKeys + (kKeys == 64 ? lane : (lane & 31)), max_key));
-        const uint64_t ok = __ballot(r >= 0);
+    auto rows_of = [&](int t) -> uint32_t {
+        const uint32_t r = (uint32_t)cache_row(v, b, kv, min(t * kKeys + (lane & (kKeys - 1)), max_key));
+        const uint64_t ok = __ballot(r != kNoRow);
         bad = ~ok;
         if (ok == ~0ull) return r;
         if (!ok) return 0;
-        const int l = __builtin_ctzll(ok);
-        const int64_t other = ((int64_t)__builtin_amdgcn_readlane((int)(r >> 32), l) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)r, l);
-        return r >= 0 ? r : other;
+        const uint32_t other = __builtin_amdgcn_readlane(r, __builtin_ctzll(ok));
+        return r != kNoRow ? r : other;
     };
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_at(smem));
-    auto fetch = [&](int buf, int64_t r) {
+    auto fetch = [&](int buf, uint32_t r) {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const int at0 = (wave * kLoads + j) * kPer, key = at0 + lane / RowTile<T>::kChunks, c = (lane % RowTile<T>::kChunks) ^ swz<T>(key);
-            const int64_t from = (((int64_t)__shfl((int)(r >> 32), key) << 32) | (uint32_t)__shfl((int)r, key)) * RowTile<T>::kRowBytes + 16 * c;
+            const int64_t from = (int64_t)(uint32_t)__shfl((int)r, key) * RowTile<T>::kRowBytes + 16 * c;
             const uint32_t to = lds0 + buf * 2 * kTile + at0 * RowTile<T>::kRowBytes;
             row_to_lds(to, (const char *)a.k_pages + from);
             row_to_lds(to + kTile, (const char *)a.v_pages + from);
@@ -248,12 +420,12 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW) voi
     float m = -INFINITY, l = 0.0f;
     const float slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
     uint64_t bad_now = 0;
-    int64_t next = 0;
+    uint32_t next = 0;
     if (t0 < t1) {
         fetch(0, rows_of(t0));
         bad_now = bad;
         if (t0 + 1 < t1) next = rows_of(t0 + 1);
-        loads_landed();
+        loads_landed<0>();
         __syncthreads();
     }
     for (int t = t0; t < t1; ++t) {
@@ -265,209 +437,268 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW) voi
         }
         char *kt = smem[buf][0], *vt = smem[buf][1];
         const int key0 = t * kKeys;
-        const bool masked = key0 + kKeys > all_hi || key0 < all_lo || bad_now != 0;
-        if (masked) {
-            // A key that a row does not see has probability 0 there, but 0 times an infinity or NaN is no 0.  Values that are
-            // not finite are added to the rows that see them and then taken out of the tile.
-            const int words = kTile / 4 / (64 * NW);
-            uint32_t *w = reinterpret_cast<uint32_t *>(vt) + threadIdx.x * words;
-            bool odd = false;
-#pragma unroll
-            for (int i = 0; i < words; ++i) {
-                const uint32_t x = w[i];
-                odd |= sizeof(T) == 2 ? (((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0 : (x & 0x7f800000u) == 0x7f800000u;
-            }
-            if (__syncthreads_or(odd)) {
-                for (int k = 0; k < kKeys; ++k) {
-                    const bool sees = key0 + k >= sight.lo && key0 + k < sight.hi && !((bad_now >> k) & 1);
-#pragma unroll
-                    for (int db = 0; db < 4; ++db)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int d = 32 * db + 8 * (i >> 2) + 4 * half + (i & 3), c = d * (int)sizeof(T) / 16;
-                            const char *p = vt + k * RowTile<T>::kRowBytes + ((c ^ swz<T>(k)) << 4) + (d * (int)sizeof(T) & 15);
-                            float x;
-                            if constexpr (sizeof(T) == 2) x = __uint_as_float((uint32_t)*reinterpret_cast<const bf16_t *>(p) << 16);
-                            else x = *reinterpret_cast<const float *>(p);
-                            if (sees && !(fabsf(x) < INFINITY)) o[db][i] += x;
-                        }
-                }
-                __syncthreads();
-#pragma unroll
-                for (int i = 0; i < words; ++i) {
-                    uint32_t x = w[i];
-                    if constexpr (sizeof(T) == 2) {
-                        if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
-                        if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
-                    } else if ((x & 0x7f800000u) == 0x7f800000u)
-                        x = 0;
-                    w[i] = x;
-                }
-                __syncthreads();
-            }
+        const bool masked = key0 + kKeys > range.all_hi || key0 < all_lo || bad_now != 0;
+        if (masked && __syncthreads_or(Odd::any(vt, threadIdx.x))) {
+            Odd::add(o, vt, sight, key0, bad_now, half);
+            __syncthreads();
+            Odd::clean(vt, threadIdx.x);
+            __syncthreads();
         }
-        // scores
         f32x16_t sc[kBlocks];
-        float top = -INFINITY;
 #pragma unroll
         for (int kb = 0; kb < kBlocks; ++kb) {
             sc[kb] = rows_dot<T>(kt, 32 * kb, q, f32x16_t{});
             score_regs<OPT>(sc[kb], a.o, slope2, sight.pos - (key0 + 32 * kb), half);
-            if (masked) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int k = 32 * kb + 8 * (i >> 2) + 4 * half + (i & 3);
-                    const bool sees = key0 + k >= sight.lo && key0 + k < sight.hi && !((bad_now >> k) & 1);
-                    sc[kb][i] = sees ? sc[kb][i] : -INFINITY;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
+            if (masked) mask_regs(sc[kb], sight, key0 + 32 * kb, bad_now >> (32 * kb), half);
         }
-        top = half_max(top);
-        if constexpr (OPT == 0) top *= a.o.c2;
-        if (__any(top > m)) {
-            const float m_new = fmaxf(m, top), scale = m == -INFINITY ? 1.0f : exp2_fast(m - m_new);   // (nothing to scale, or infinities)
-            m = m_new;
-            l *= scale;
-#pragma unroll
-            for (int db = 0; db < 4; ++db)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[db][i] *= scale;
-        }
-        const float ref = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-        for (int kb = 0; kb < kBlocks; ++kb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float p = exp2_fast(OPT == 0 ? fmaf(sc[kb][i], a.o.c2, -ref) : sc[kb][i] - ref);
-                l += p;
-                sc[kb][i] = p;
-            }
-        // O^T += V^T P^T.  In bf16 the probabilities are rounded to the values' type, as the matrix cores take them: off by 2^-9 each at most, which is
-        // what rounding the output costs; the sum under them is of the unrounded ones.
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int kb = 0; kb < kBlocks; ++kb)
-#pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-                    bf16x8_t p;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) p[j] = (__bf16)sc[kb][8 * ks + j];
-#pragma unroll
-                    for (int db = 0; db < 4; ++db) {
-                        union { s16x4_t h[2]; bf16x8_t w; } x;
-#pragma unroll
-                        for (int aa = 0; aa < 2; ++aa) {
-                            const int k = 32 * kb + 16 * ks + 8 * aa + 4 * half + ((lane & 15) >> 2);
-                            const int c = (4 * db + 2 * ((lane & 31) >> 4) + ((lane & 3) >> 1)) ^ swz<T>(k);
-                            x.h[aa] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CTKVR_LDS s16x4_t *)(vt + k * 256 + (c << 4) + 8 * (lane & 1)));
-                        }
-                        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.w, p, o[db], 0, 0, 0);
-                    }
-                }
-        } else {
-#pragma unroll
-            for (int kb = 0; kb < kBlocks; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int k = 32 * kb + 8 * (i >> 2) + 4 * half + (i & 3), s = swz<T>(k);
-#pragma unroll
-                    for (int db = 0; db < 4; ++db) {
-                        const int d = 32 * db + (lane & 31);
-                        const float x = *reinterpret_cast<const float *>(vt + k * 512 + (((d >> 2) ^ s) << 4) + 4 * (d & 3));
-                        o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, sc[kb][i], o[db], 0, 0, 0);
-                    }
-                }
-        }
+        softmax_regs<OPT, kBlocks>(sc, o, m, l, a.o.c2);
+        values_dot<T, kBlocks>(o, vt, sc, lane);
         bad_now = bad_next;
-        loads_landed();
+        loads_landed<0>();
         __syncthreads();
     }
 
     l = half_sum(l);
     if (row >= rows) return;
-    const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);   // (NaN stays)
-    const float lse = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : (l == 0.0f ? -INFINITY : l);
+    const float inv = inv_sum(l), lse = lse_of(m, l);
     const size_t at_row = (size_t)(s.c0 + token) * v.h + head;
-    if (a.nsplit > 1) {
-        const size_t n = (size_t)split * v.total * v.h + at_row;
-        if (half == 0) a.part_lse[n] = lse;
-        if (t0 < t1) {
-#pragma unroll
-            for (int db = 0; db < 4; ++db)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    f32x4_t x;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) x[c] = o[db][4 * i + c] * inv;
-                    *reinterpret_cast<f32x4_t *>(a.part_o + n * 128 + 32 * db + 8 * i + 4 * half) = x;
-                }
-        }
-        return;
+    const size_t n = (size_t)split * v.total * v.h + at_row;
+    if (half == 0) {
+        if (a.nsplit > 1) a.part_lse[n] = lse;
+        else if (a.lse) a.lse[at_row] = lse;
     }
-    if (a.lse && half == 0) a.lse[at_row] = lse;
-    T *out = (T *)a.out + at_row * 128;
+    if (a.nsplit > 1 && t0 == t1) return;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int d = 32 * db + 8 * i + 4 * half;
-            if constexpr (sizeof(T) == 2) {
-                bf16x4_t x;
+            f32x4_t x;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) x[c] = (__bf16)(o[db][4 * i + c] * inv);
-                *reinterpret_cast<bf16x4_t *>(out + d) = x;
-            } else {
-                f32x4_t x;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) x[c] = o[db][4 * i + c] * inv;
-                *reinterpret_cast<f32x4_t *>(out + d) = x;
-            }
+            for (int c = 0; c < 4; ++c) x[c] = o[db][4 * i + c] * inv;
+            if (a.nsplit > 1) store4(a.part_o + n * 128 + d, x);
+            else store4((T *)a.out + at_row * 128 + d, x);
         }
 }
 
-// The runs of a row joined by their log-sum-exps: 32 lanes a row
-template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
+// Few rows, many keys: one block a tile of 32 rows and a run of their keys, which its waves share out, each with a maximum and outputs of its own until
+// they are joined at the end; no wave waits for another before that.  Keys go to registers as operands, values to shared memory, a tile of 32 ahead.
+template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void attn_few_kernel(AttnArgs a)
 {
+    constexpr int kTile = 32 * RowTile<T>::kRowBytes, kPer = RowTile<T>::kRowsPerLoad, kLoads = 32 / kPer;
+    using Odd = OddValues<T, 32, 64>;
+    __shared__ __align__(16) char smem[NW][2][kTile];
+    __shared__ float join[NW][2][32];
+    const CacheView &v = a.v;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int kv = blockIdx.x % v.g, rest = blockIdx.x / v.g, split = rest % a.nsplit;
+    int b, at;
+    if (!locate_tile<5>(v, a.tiles - 1 - rest / a.nsplit, &b, &at)) return;
+    const SeqSpan s = seq_span(v, b);
+    const int rows = s.n << v.lg, r0 = at << 5, row = r0 + (lane & 31);
+    const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
+    const int token = min(row, rows - 1) >> v.lg, head = (kv << v.lg) + (min(row, rows - 1) & ((1 << v.lg) - 1));
+    const RowSight sight = row_sight(v, a.o, s, prefix, token);
+
+    Operand<T> q;
+    load_operand(q, (const T *)a.q + (int64_t)(s.c0 + token) * a.q_stride + head * 128, half);
+
+    const KeyRange range = key_range(s, prefix, r0 >> v.lg, (min(r0 + 32, rows) - 1) >> v.lg);
+    int k_lo = 0, all_lo = 0;
+    if (a.o.first) {
+        k_lo = all_lo = sight.lo;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            k_lo = min(k_lo, __shfl_xor(k_lo, d));
+            all_lo = max(all_lo, __shfl_xor(all_lo, d));
+        }
+    }
+    const int first_tile = k_lo / 32, tiles = range.hi > k_lo ? (range.hi + 31) / 32 - first_tile : 0;
+    const int64_t runs = (int64_t)a.nsplit * NW, run = split * NW + wave;
+    const int t0 = __builtin_amdgcn_readfirstlane(first_tile + (int)(tiles * run / runs));
+    const int t1 = __builtin_amdgcn_readfirstlane(first_tile + (int)(tiles * (run + 1) / runs));
+
+    // 64 of the table's entries at a time, a lane each
+    const int max_key = max(range.hi - 1, 0);
+    const int32_t *table = v.table + (size_t)b * v.max_pages;
+    int e0 = -64;
+    uint32_t page = 0;
+    uint64_t bad = 0;
+    auto rows_of = [&](int t) -> uint32_t {
+        const int key = min(t * 32 + (lane & 31), max_key), e = key >> v.page_shift;
+        const int last = min(t * 32 + 31, max_key) >> v.page_shift;
+        if (last >= e0 + 64) {
+            e0 = (t * 32) >> v.page_shift;
+            page = (uint32_t)table[min(e0 + lane, v.max_pages - 1)];
+            loads_landed<0>();
+        }
+        const uint32_t p = (uint32_t)__shfl((int)page, e - e0);
+        const uint32_t r = p < v.num_pages ? (uint32_t)((p * (uint64_t)v.g + kv) << v.page_shift) + (key & ((1 << v.page_shift) - 1)) : kNoRow;
+        const uint64_t ok = __ballot(r != kNoRow);
+        bad = ~ok;
+        if (ok == ~0ull) return r;
+        if (!ok) return 0;
+        const uint32_t other = __builtin_amdgcn_readlane(r, __builtin_ctzll(ok));
+        return r != kNoRow ? r : other;
+    };
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_at(smem[wave]));
+    auto fetch_values = [&](int buf, uint32_t r) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int key = j * kPer + lane / RowTile<T>::kChunks, c = (lane % RowTile<T>::kChunks) ^ swz<T>(key);
+            row_to_lds(lds0 + buf * kTile + j * kPer * RowTile<T>::kRowBytes,
+                       (const char *)a.v_pages + (int64_t)(uint32_t)__shfl((int)r, key) * RowTile<T>::kRowBytes + 16 * c);
+        }
+    };
+
+    f32x16_t o[4] = {};
+    float m = -INFINITY, l = 0.0f;
+    const float slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
+    Operand<T> k;
+    uint64_t bad_now = 0;
+    if (t0 < t1) {
+        const uint32_t r = rows_of(t0);
+        bad_now = bad;
+        fetch_values(0, r);
+        load_operand(k, (const T *)a.k_pages + (int64_t)r * 128, half);
+    }
+    for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1, key0 = t * 32;
+        const bool more = t + 1 < t1;
+        const uint32_t r = more ? rows_of(t + 1) : 0;
+        const uint64_t bad_next = bad;
+        settled();   // this tile's keys and values are there, those of the last have been read
+        f32x16_t sc[1] = {};
+        Operand<T> k_next;
+        if (sizeof(T) == 2 && more) {   // (fp32 operands are too wide for two)
+            fetch_values(buf ^ 1, r);
+            load_operand(k_next, (const T *)a.k_pages + (int64_t)r * 128, half);
+        }
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.c[i], q.c[i], sc[0], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k.c[i][e], q.c[i][e], sc[0], 0, 0, 0);
+        }
+        if (sizeof(T) == 4 && more) {
+            fetch_values(buf ^ 1, r);
+            load_operand(k, (const T *)a.k_pages + (int64_t)r * 128, half);
+        }
+        if constexpr (sizeof(T) == 2) k = k_next;
+        char *vt = smem[wave][buf];
+        score_regs<OPT>(sc[0], a.o, slope2, sight.pos - key0, half);
+        if (key0 + 32 > range.all_hi || key0 < all_lo || bad_now != 0) {
+            mask_regs(sc[0], sight, key0, bad_now, half);
+            if (__any(Odd::any(vt, lane))) {
+                Odd::add(o, vt, sight, key0, bad_now, half);
+                __builtin_amdgcn_wave_barrier();
+                Odd::clean(vt, lane);
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+        softmax_regs<OPT, 1>(sc, o, m, l, a.o.c2);
+        values_dot<T, 1>(o, vt, sc, lane);
+        bad_now = bad_next;
+        __builtin_amdgcn_wave_barrier();
+    }
+
+    // the waves' outputs to one maximum, through shared memory (16-byte chunks at chunk ^ row)
+    l = half_sum(l);
+    if (half == 0) {
+        join[wave][0][lane] = m;
+        join[wave][1][lane] = l;
+    }
+    loads_landed<0>();
+    __syncthreads();   // (and nobody needs its values any more)
+    const int r32 = lane & 31;
+    float top = join[0][0][r32];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) top = fmaxf(top, join[w][0][r32]);
+    const float scale = m == -INFINITY ? 1.0f : exp2_fast(m - top);
+    char *mine = smem[0][0] + wave * 32 * 512;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f32x4_t x;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) x[c] = o[db][4 * i + c] * scale;
+            *reinterpret_cast<f32x4_t *>(mine + r32 * 512 + (((8 * db + 2 * i + half) ^ r32) << 4)) = x;
+        }
+    __syncthreads();
+    const int have = min(32, rows - r0);
+    for (int j = threadIdx.x; j < have * 32; j += 64 * NW) {   // (row, four elements)
+        const int r = j >> 5, c = j & 31;
+        float t = join[0][0][r], sum = 0.0f;
+#pragma unroll
+        for (int w = 1; w < NW; ++w) t = fmaxf(t, join[w][0][r]);
+        f32x4_t x = {};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float mw = join[w][0][r];
+            sum += join[w][1][r] * (mw == -INFINITY ? 1.0f : exp2_fast(mw - t));
+            x += *reinterpret_cast<const f32x4_t *>(smem[0][0] + w * 32 * 512 + r * 512 + ((c ^ r) << 4));
+        }
+        x *= inv_sum(sum);
+        const float lse = lse_of(t, sum);
+        const size_t at_row = (size_t)(s.c0 + ((r0 + r) >> v.lg)) * v.h + (kv << v.lg) + ((r0 + r) & ((1 << v.lg) - 1));
+        if (a.nsplit > 1) {
+            const size_t n = (size_t)split * v.total * v.h + at_row;
+            if (c == 0) a.part_lse[n] = lse;
+            store4(a.part_o + n * 128 + 4 * c, x);
+        } else {
+            if (c == 0 && a.lse) a.lse[at_row] = lse;
+            store4((T *)a.out + at_row * 128 + 4 * c, x);
+        }
+    }
+}
+
+// The runs of a row joined by their log-sum-exps: a row has WAYS groups of 32 lanes, four elements a lane, that take the runs in turn
+template <typename T, int WAYS> __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a)
+{
+    __shared__ f32x4_t part[WAYS > 1 ? 8 : 1][32];
+    __shared__ float sums[WAYS > 1 ? 8 : 1];
     const int rows = min(max(a.v.cu[a.v.batch], 0), a.v.total) * a.v.h;   // (tokens behind the last sequence have no runs)
-    const int row = blockIdx.x * 8 + (threadIdx.x >> 5), l32 = threadIdx.x & 31;
-    if (row >= rows || row < a.v.cu[0] * a.v.h) return;
+    const int group = threadIdx.x >> 5, l32 = threadIdx.x & 31, way = group % WAYS;
+    const int row = blockIdx.x * (8 / WAYS) + group / WAYS;
+    const bool live = row < rows && row >= a.v.cu[0] * a.v.h;
     const size_t step = (size_t)a.v.total * a.v.h;
-    float top = -INFINITY, nan = 0.0f;
-    for (int i = l32; i < a.nsplit; i += 32) {
-        const float x = a.part_lse[i * step + row];
-        top = fmaxf(top, x);
-        if (x != x) nan = x;
-    }
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        top = fmaxf(top, __shfl_xor(top, d));
-        nan += __shfl_xor(nan, d);
-    }
+    float top = -INFINITY;
     f32x4_t o = {};
-    float sum = 0.0f;
-    const float ref = top == -INFINITY ? 0.0f : top;
-    for (int i = 0; i < a.nsplit; ++i) {
-        const float x = a.part_lse[i * step + row];
-        if (x == -INFINITY) continue;
-        const float w = exp2_fast((x - ref) * kLog2e);
-        sum += w;
-        const f32x4_t p = *reinterpret_cast<const f32x4_t *>(a.part_o + (i * step + row) * 128 + 4 * l32);
+    float sum = 0.0f, ref = 0.0f;
+    if (live) {
+        for (int i = l32; i < a.nsplit; i += 32) top = fmaxf(top, a.part_lse[i * step + row]);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) o[c] = fmaf(w, p[c], o[c]);
-    }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    if (a.lse && l32 == 0) a.lse[row] = nan != nan ? nan : sum == 0.0f ? -INFINITY : ref + __builtin_amdgcn_logf(sum) * kLn2;
-    T *out = (T *)a.out + (size_t)row * 128 + 4 * l32;
-    if constexpr (sizeof(T) == 2) {
-        bf16x4_t x;
+        for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+        ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll 4
+        for (int i = way; i < a.nsplit; i += WAYS) {
+            const float x = a.part_lse[i * step + row];
+            if (x == -INFINITY) continue;   // (an empty run has no outputs)
+            const float w = exp2_fast((x - ref) * kLog2e);
+            sum += w;
+            const f32x4_t p = *reinterpret_cast<const f32x4_t *>(a.part_o + (i * step + row) * 128 + 4 * l32);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) x[c] = (__bf16)(o[c] * inv);
-        *reinterpret_cast<bf16x4_t *>(out) = x;
-    } else {
-        *reinterpret_cast<f32x4_t *>(out) = o * inv;
+            for (int c = 0; c < 4; ++c) o[c] = fmaf(w, p[c], o[c]);
+        }
     }
+    if constexpr (WAYS > 1) {
+        part[group][l32] = o;
+        if (l32 == 0) sums[group] = sum;
+        __syncthreads();
+        if (way) return;
+#pragma unroll
+        for (int w = 1; w < WAYS; ++w) {
+            o += part[group + w][l32];
+            sum += sums[group + w];
+        }
+    }
+    if (!live) return;
+    if (a.lse && l32 == 0) a.lse[row] = sum == 0.0f ? -INFINITY : ref + __builtin_amdgcn_logf(sum) * kLn2;
+    store4((T *)a.out + (size_t)row * 128 + 4 * l32, o * inv_sum(sum));
 }
 
 // ---- accumulated attention weight ----------------------------------------------------------------------
@@ -530,7 +761,7 @@ template <typename T, int OPT> __global__ __launch_bounds__(256) void weights_ke
     f32x16_t sum[kBlocks] = {};
     if (t0 < t1) fetch(0, t0);
     for (int t = t0; t < t1; ++t) {
-        loads_landed();
+        loads_landed<0>();
         __syncthreads();
         if (t + 1 < t1) fetch((t - t0 + 1) & 1, t + 1);
 #pragma unroll
@@ -860,7 +1091,7 @@ template <typename T> __global__ __launch_bounds__(512) void evict_move_kernel(E
             to[i] = pages + dst * 128 * (int64_t)sizeof(T);
             x[i] = *reinterpret_cast<const u32x4_t *>(pages + src * 128 * (int64_t)sizeof(T));
         }
-        loads_landed();
+        loads_landed<0>();
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
@@ -870,7 +1101,7 @@ template <typename T> __global__ __launch_bounds__(512) void evict_move_kernel(E
         for (int j0 = 0; j0 < keep; j0 += 512) {
             const int j = j0 + threadIdx.x;
             const float x = j < keep ? a.w_in[w0 + ids[j]] : 0.0f;
-            loads_landed();
+            loads_landed<0>();
             __syncthreads();
             if (j < keep) a.w_out[w0 + j] = x;
         }
