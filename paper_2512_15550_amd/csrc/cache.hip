@@ -167,14 +167,24 @@ template <typename T> int attn_launch(const ctkvr_cache *c, AttnArgs &a, bool fe
     }
     return launched("ctkvr_cache_attn");
 }
-template <typename T> int weights_launch(const ctkvr_cache *c, const WeightArgs &a, int opt, hipStream_t st)
+template <typename T> int weights_launch(const ctkvr_cache *c, WeightArgs &a, int opt, hipStream_t st)
 {
-    const int keys = c->p.max_pages * c->p.page_size, tile = sizeof(T) == 2 ? 256 : 128;
-    const unsigned grid = (unsigned)((int64_t)((keys + tile - 1) / tile) * c->p.batch * c->p.n_kv_heads);
-    with_opts(opt, [&](auto o) {
-        weights_kernel<T, decltype(o)::value><<<dim3(grid), 256, 0, st>>>(a);
-        return 0;
-    });
+    const int64_t keys = (int64_t)c->p.max_pages * c->p.page_size, units = (int64_t)c->p.batch * c->p.n_kv_heads;
+    // Rows that fit a block's shared memory once or twice: keys go past them.  More rows: they go past the keys.
+    const int held = 65536 / (128 * (int)sizeof(T)), used = std::max(1, std::min(a.v.total, c->p.batch));
+    if (((int64_t)a.v.total << c->lg) <= 2ll * held * used) {
+        a.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>((c->p.batch > 1 ? 8 : 2) * c->num_cu / units, (keys + 127) / 128));
+        with_opts(opt, [&](auto o) {
+            weights_few_kernel<T, decltype(o)::value><<<dim3((unsigned)(units * a.nsplit)), 256, 0, st>>>(a);
+            return 0;
+        });
+    } else {
+        const int tile = sizeof(T) == 2 ? 256 : 128;
+        with_opts(opt, [&](auto o) {
+            weights_kernel<T, decltype(o)::value><<<dim3((unsigned)((keys + tile - 1) / tile * units)), 512, 0, st>>>(a);
+            return 0;
+        });
+    }
     return launched("ctkvr_cache_weights");
 }
 
@@ -358,10 +368,17 @@ int ctkvr_cache_evict(ctkvr_cache *c, const float *weights_in, int32_t weights_s
     a.lens = out_lens;
     a.k_pages = k_pages;
     a.v_pages = v_pages;
-    a.slices = 8;
-    const int units = c->p.batch * c->p.n_kv_heads;
+    const int units = c->p.batch * c->p.n_kv_heads, keys = c->p.max_pages * c->p.page_size;
     hipStream_t st = (hipStream_t)hip_stream;
-    evict_select_kernel<<<dim3((unsigned)units), 1024, 0, st>>>(a);
+    // (a thread holds the ranks of so many keys of the longest sequence that the table has room for)
+    if (keys <= 8192) evict_select_kernel<8><<<dim3((unsigned)units), 1024, 0, st>>>(a);
+    else if (keys <= 32768) evict_select_kernel<32><<<dim3((unsigned)units), 1024, 0, st>>>(a);
+    else if (keys <= 65536) evict_select_kernel<64><<<dim3((unsigned)units), 1024, 0, st>>>(a);
+    else evict_select_kernel<0><<<dim3((unsigned)units), 1024, 0, st>>>(a);
+    // two blocks a CU, and as few slices of a row as that takes: lines of 128 bytes first
+    const int pieces = c->p.dtype == CTKVR_BF16 ? 32 : 64;
+    a.slices = pieces / 8;
+    while (a.slices < pieces && units * a.slices < 2 * c->num_cu) a.slices *= 2;
     if (c->p.dtype == CTKVR_BF16) evict_move_kernel<bf16_t><<<dim3((unsigned)(units * a.slices)), 512, 0, st>>>(a);
     else evict_move_kernel<float><<<dim3((unsigned)(units * a.slices)), 512, 0, st>>>(a);
     return launched("ctkvr_cache_evict");

@@ -713,19 +713,90 @@ struct WeightArgs {
     float *w_out;
     int w_stride;
     float decay;
-    int key_tiles;          // of a sequence, at most
+    int nsplit;             // weights_few_kernel: blocks of a unit
 };
 
-// One block 4 x 32 kBlocks keys of a unit; a wave keeps its keys as operands and adds up their probabilities over the rows, which come
-// through shared memory.  A key's sum has one owner: the same in every call.
-template <typename T, int OPT> __global__ __launch_bounds__(256) void weights_kernel(WeightArgs a)
+// x added over the 32 lanes of a half; its first 16 lanes get the sum (`live` lanes hold something, from the first on)
+__device__ __forceinline__ float lanes32_sum(float x, int live)
+{
+    x = group16_sum(x);
+    if (live > 16) x += __shfl_xor(x, 16);
+    return x;
+}
+// A row's part in the sums: what it sees and minus its log-sum-exp (in units of log2 e; a row that sees nothing adds nothing)
+struct WeightRow {
+    RowSight sight;
+    float nlse, slope2;
+};
+template <int OPT> __device__ __forceinline__ WeightRow weight_row(const WeightArgs &a, const SeqSpan &s, int prefix, int kv, int row, int rows)
+{
+    const int r = min(row, rows - 1), token = r >> a.v.lg, head = (kv << a.v.lg) + (r & ((1 << a.v.lg) - 1));
+    WeightRow w;
+    w.sight = row_sight(a.v, a.o, s, prefix, token);
+    const float lse = a.lse[(size_t)(s.c0 + token) * a.v.h + head];
+    w.nlse = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
+    w.slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
+    if (row >= rows) w.sight.hi = 0;
+    return w;
+}
+// sum += the probabilities of 32 NB keys from k0 on (their operands: k) under the lane's row (q)
+template <typename T, int OPT, int NB> __device__ __forceinline__ void add_weights(f32x16_t (&sum)[NB], const Operand<T> (&k)[NB], const Operand<T> &q, const WeightRow &w,
+                                                                                   const ScoreOpts &o, int k0, uint64_t bad, int half)
+{
+    const bool masked = !__all(w.sight.lo <= k0 && w.sight.hi >= k0 + 32 * NB) || bad != 0;
+    if (masked && !__any(w.sight.lo < k0 + 32 * NB && w.sight.hi > k0)) return;
+    f32x16_t sc[NB] = {};
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb) sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kb].c[i], q.c[i], sc[kb], 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int kb = 0; kb < NB; ++kb) sc[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[kb].c[i][e], q.c[i][e], sc[kb], 0, 0, 0);
+    }
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) score_regs<OPT>(sc[kb], o, w.slope2, w.sight.pos - k0 - 32 * kb, half);
+    if (masked) {
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            mask_regs(sc[kb], w.sight, k0 + 32 * kb, bad >> (32 * kb), half);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float p = exp2_fast(OPT == 0 ? fmaf(sc[kb][i], o.c2, w.nlse) : sc[kb][i] + w.nlse);
+                sum[kb][i] += sc[kb][i] == -INFINITY ? 0.0f : p;
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[kb][i] += exp2_fast(OPT == 0 ? fmaf(sc[kb][i], o.c2, w.nlse) : sc[kb][i] + w.nlse);
+}
+// a row of a tile in shared memory as the second operand
+template <typename T> __device__ __forceinline__ void tile_operand(Operand<T> &q, const char *tile, int r, int half)
+{
+    using C = std::remove_reference_t<decltype(q.c[0])>;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(q.c) / 16); ++i)
+        q.c[i] = *reinterpret_cast<const C *>(tile + r * RowTile<T>::kRowBytes + (((2 * i + half) ^ swz<T>(r)) << 4));
+}
+
+// Many rows.  One block of eight waves 4 x 32 kBlocks keys of a unit; a wave keeps its keys as operands and adds up their probabilities over half of the
+// rows, which come through shared memory, 128 at a time.  A key's sum has two owners that are added at the end: the same in every call.
+template <typename T, int OPT> __global__ __launch_bounds__(512, 2) void weights_kernel(WeightArgs a)
 {
     constexpr int kBlocks = sizeof(T) == 2 ? 2 : 1, kKeys = 128 * kBlocks;
-    constexpr int kRows = RowTile<T>::kRows, kTile = RowTile<T>::kBytes, kPer = RowTile<T>::kRowsPerLoad, kLoads = kRows / (4 * kPer);
+    constexpr int kRows = 128, kTile = kRows * RowTile<T>::kRowBytes, kPer = RowTile<T>::kRowsPerLoad, kLoads = kRows / (8 * kPer);
     __shared__ __align__(16) char smem[2][kTile];
     const CacheView &v = a.v;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int kv = blockIdx.x % v.g, b = blockIdx.x / v.g % v.batch, key0 = blockIdx.x / v.g / v.batch * kKeys, mine0 = key0 + 32 * kBlocks * wave;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, side = wave >> 2;
+    const int kv = blockIdx.x % v.g, b = blockIdx.x / v.g % v.batch, key0 = blockIdx.x / v.g / v.batch * kKeys, mine0 = key0 + 32 * kBlocks * (wave & 3);
     const SeqSpan s = seq_span(v, b);
     if (key0 >= s.len) return;
     const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
@@ -736,95 +807,158 @@ template <typename T, int OPT> __global__ __launch_bounds__(256) void weights_ke
 #pragma unroll
     for (int kb = 0; kb < kBlocks; ++kb) {
         const int key = mine0 + 32 * kb + (lane & 31);
-        const int64_t r = key < s.len ? cache_row(v, b, kv, key) : -1;
-        bad |= (__ballot(r < 0) & 0xffffffffull) << (32 * kb);
-        load_operand(k[kb], (const T *)a.k_pages + max(r, (int64_t)0) * 128, half);
+        const uint32_t r = key < s.len ? (uint32_t)cache_row(v, b, kv, key) : kNoRow;
+        bad |= (__ballot(r == kNoRow) & 0xffffffffull) << (32 * kb);
+        load_operand(k[kb], (const T *)a.k_pages + (int64_t)(r == kNoRow ? 0 : r) * 128, half);
     }
 
     // rows that may see one of the block's keys
-    const int tok0 = prefix > key0 ? 0 : min(max(key0 - s.old, 0), s.n), tok_pos = max(0, -s.old);
-    const int t0 = (max(tok0, min(tok_pos, s.n)) << v.lg) / kRows, t1 = (rows + kRows - 1) / kRows;
+    const int tok0 = prefix > key0 ? 0 : min(max(key0 - s.old, 0), s.n), tok_pos = min(max(0, -s.old), s.n);
+    const int t0 = __builtin_amdgcn_readfirstlane((max(tok0, tok_pos) << v.lg) / kRows), t1 = __builtin_amdgcn_readfirstlane((rows + kRows - 1) / kRows);
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_at(smem));
-    auto row_at = [&](int row, int *token) -> int64_t {
-        row = min(row, rows - 1);
-        *token = row >> v.lg;
-        return (int64_t)(s.c0 + *token) * a.q_stride + ((kv << v.lg) + (row & ((1 << v.lg) - 1))) * 128;
-    };
     auto fetch = [&](int buf, int t) {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const int at0 = (wave * kLoads + j) * kPer, r = at0 + lane / RowTile<T>::kChunks, c = (lane % RowTile<T>::kChunks) ^ swz<T>(r);
-            int token;
-            row_to_lds(lds0 + buf * kTile + at0 * RowTile<T>::kRowBytes, (const char *)((const T *)a.q + row_at(t * kRows + r, &token)) + 16 * c);
+            const int row = min(t * kRows + r, rows - 1);
+            row_to_lds(lds0 + buf * kTile + at0 * RowTile<T>::kRowBytes,
+                       (const char *)((const T *)a.q + (int64_t)(s.c0 + (row >> v.lg)) * a.q_stride + ((kv << v.lg) + (row & ((1 << v.lg) - 1))) * 128) + 16 * c);
         }
     };
     f32x16_t sum[kBlocks] = {};
-    if (t0 < t1) fetch(0, t0);
+    WeightRow w[2];
+    if (t0 < t1) {
+        fetch(0, t0);
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb) w[rb] = weight_row<OPT>(a, s, prefix, kv, t0 * kRows + 64 * side + 32 * rb + (lane & 31), rows);
+    }
     for (int t = t0; t < t1; ++t) {
         loads_landed<0>();
         __syncthreads();
-        if (t + 1 < t1) fetch((t - t0 + 1) & 1, t + 1);
+        WeightRow next[2];
+        if (t + 1 < t1) {   // the next rows' log-sum-exps come in the shadow of this tile too
+            fetch((t - t0 + 1) & 1, t + 1);
 #pragma unroll
-        for (int rb = 0; rb < kRows / 32; ++rb) {
-            const int row = t * kRows + 32 * rb + (lane & 31);
-            int token;
-            (void)row_at(row, &token);
-            const int head = (kv << v.lg) + (min(row, rows - 1) & ((1 << v.lg) - 1));
-            RowSight sight = row_sight(v, a.o, s, prefix, token);
-            float lse = a.lse[(size_t)(s.c0 + token) * v.h + head];
-            if (row >= rows) sight.hi = 0;
-            const float nlse = lse == -INFINITY ? -INFINITY : -lse * kLog2e;   // (a row that sees nothing adds nothing)
-            const float slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
-            const char *qt = smem[(t - t0) & 1] + 32 * rb * RowTile<T>::kRowBytes;
-            // the rows are this product's second operand
-            Operand<T> q;
-#pragma unroll
-            for (int i = 0; i < (int)(sizeof(q.c) / 16); ++i) {
-                using C = std::remove_reference_t<decltype(q.c[0])>;
-                q.c[i] = *reinterpret_cast<const C *>(qt + (lane & 31) * RowTile<T>::kRowBytes + (((2 * i + half) ^ swz<T>(32 * rb + (lane & 31))) << 4));
-            }
-#pragma unroll
-            for (int kb = 0; kb < kBlocks; ++kb) {
-                const int k0 = mine0 + 32 * kb;
-                const bool masked = !__all(sight.lo <= k0 && sight.hi >= k0 + 32) || ((bad >> (32 * kb)) & 0xffffffffull) != 0;
-                if (masked && !__any(sight.lo < k0 + 32 && sight.hi > k0)) continue;
-                f32x16_t sc = {};
-                if constexpr (sizeof(T) == 2) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kb].c[i], q.c[i], sc, 0, 0, 0);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_32x32x2f32(k[kb].c[i][e], q.c[i][e], sc, 0, 0, 0);
-                }
-                score_regs<OPT>(sc, a.o, slope2, sight.pos - k0, half);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float p = exp2_fast(OPT == 0 ? fmaf(sc[i], a.o.c2, nlse) : sc[i] + nlse);
-                    if (masked) {
-                        const int kk = 8 * (i >> 2) + 4 * half + (i & 3);
-                        p = k0 + kk >= sight.lo && k0 + kk < sight.hi && !((bad >> (32 * kb + kk)) & 1) ? p : 0.0f;
-                    }
-                    sum[kb][i] += p;
-                }
-            }
+            for (int rb = 0; rb < 2; ++rb) next[rb] = weight_row<OPT>(a, s, prefix, kv, (t + 1) * kRows + 64 * side + 32 * rb + (lane & 31), rows);
         }
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb) {
+            Operand<T> q;
+            tile_operand(q, smem[(t - t0) & 1], 64 * side + 32 * rb + (lane & 31), half);
+            add_weights<T, OPT, kBlocks>(sum, k, q, w[rb], a.o, mine0, bad, half);
+        }
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb) w[rb] = next[rb];
     }
     const size_t unit = ((size_t)b * v.g + kv) * a.w_stride;
+    float *other = reinterpret_cast<float *>(smem) + (wave & 3) * 32 * kBlocks;
+    __syncthreads();
 #pragma unroll
-    for (int kb = 0; kb < kBlocks; ++kb)
+    for (int turn = 1; turn >= 0; --turn) {   // the second half's sums, then the first half's with them
+        if (side == turn) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float x = sum[kb][i];
+            for (int kb = 0; kb < kBlocks; ++kb)
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) x += __shfl_xor(x, d);
-            const int key = mine0 + 32 * kb + 8 * (i >> 2) + 4 * half + (i & 3);
-            if ((lane & 31) == i && key < s.len) {
-                if (a.w_in && key < s.old) x = fmaf(a.decay, a.w_in[unit + key], x);
-                a.w_out[unit + key] = x;
+                for (int i = 0; i < 16; ++i) {
+                    float x = lanes32_sum(sum[kb][i], 32);
+                    const int at = 32 * kb + 8 * (i >> 2) + 4 * half + (i & 3), key = mine0 + at;
+                    if ((lane & 31) == i) {   // (i < 16)
+                        if (turn) {
+                            other[at] = x;
+                        } else if (key < s.len) {
+                            x += other[at];
+                            if (a.w_in && key < s.old) x = fmaf(a.decay, a.w_in[unit + key], x);
+                            a.w_out[unit + key] = x;
+                        }
+                    }
+                }
+        }
+        if (turn) __syncthreads();
+    }
+}
+
+// Few rows, many keys: a block keeps up to 64 KB of a unit's rows in shared memory, and each of its waves walks a run of the unit's keys past them, the
+// next 32 keys' rows on their way to registers meanwhile.  More rows than that take another turn over the run, which adds to what the last one wrote.
+template <typename T, int OPT> __global__ __launch_bounds__(256, 2) void weights_few_kernel(WeightArgs a)
+{
+    constexpr int kPer = RowTile<T>::kRowsPerLoad, kRows = 65536 / RowTile<T>::kRowBytes;
+    __shared__ __align__(16) char smem[65536];
+    __shared__ WeightRow part[kRows];
+    const CacheView &v = a.v;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int units = v.batch * v.g, unit = blockIdx.x % units, split = blockIdx.x / units, b = unit / v.g, kv = unit % v.g;
+    const SeqSpan s = seq_span(v, b);
+    const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0, rows = s.n << v.lg;
+    const int64_t tiles = (s.len + 31) / 32, runs = (int64_t)a.nsplit * 4, run = split * 4 + wave;
+    const int t0 = __builtin_amdgcn_readfirstlane((int)(tiles * run / runs)), t1 = __builtin_amdgcn_readfirstlane((int)(tiles * (run + 1) / runs));
+    if (tiles * (split + 1) / a.nsplit == tiles * split / a.nsplit) return;   // nothing for any of the waves
+
+    const int32_t *table = v.table + (size_t)b * v.max_pages;
+    int e0 = -64;
+    uint32_t page = 0, bad = 0;
+    auto rows_of = [&](int t) -> uint32_t {
+        const int key = min(t * 32 + (lane & 31), s.len - 1), e = key >> v.page_shift, last = min(t * 32 + 31, s.len - 1) >> v.page_shift;
+        if (last >= e0 + 64 || (t * 32) >> v.page_shift < e0) {
+            e0 = (t * 32) >> v.page_shift;
+            page = (uint32_t)table[min(e0 + lane, v.max_pages - 1)];
+            loads_landed<0>();
+        }
+        const uint32_t p = (uint32_t)__shfl((int)page, e - e0);
+        bad = (uint32_t)__ballot(p >= v.num_pages || t * 32 + (lane & 31) >= s.len);
+        return p < v.num_pages ? (uint32_t)((p * (uint64_t)v.g + kv) << v.page_shift) + (key & ((1 << v.page_shift) - 1)) : 0u;
+    };
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_at(smem));
+    const size_t w0 = (size_t)unit * a.w_stride;
+    const int mine = 8 * ((lane & 15) >> 2) + 4 * half + (lane & 3);   // the key whose sum the lane writes (lanes 0 .. 15 of a half)
+    int r0 = 0;
+    do {
+        const int have = min(rows - r0, kRows), blocks = (have + 31) / 32;
+        __syncthreads();
+        for (int j = wave; j * kPer < have; j += 4) {
+            const int r = j * kPer + lane / RowTile<T>::kChunks, c = (lane % RowTile<T>::kChunks) ^ swz<T>(r), row = r0 + min(r, have - 1);
+            row_to_lds(lds0 + j * kPer * RowTile<T>::kRowBytes,
+                       (const char *)((const T *)a.q + (int64_t)(s.c0 + (row >> v.lg)) * a.q_stride + ((kv << v.lg) + (row & ((1 << v.lg) - 1))) * 128) + 16 * c);
+        }
+        Operand<T> k[1];
+        uint32_t bad_now = 0;
+        if (t0 < t1) {
+            load_operand(k[0], (const T *)a.k_pages + (int64_t)rows_of(t0) * 128, half);
+            bad_now = bad;
+        }
+        for (int r = threadIdx.x; r < 32 * blocks; r += 256) part[r] = weight_row<OPT>(a, s, prefix, kv, r0 + r, rows);
+        loads_landed<0>();
+        __syncthreads();
+        for (int t = t0; t < t1; ++t) {
+            const int key = t * 32 + mine;
+            float before = 0.0f;
+            if (r0 > 0) before = key < s.len ? a.w_out[w0 + key] : 0.0f;
+            else if (a.w_in && key < min(s.old, s.len)) before = a.decay * a.w_in[w0 + key];
+            Operand<T> next;
+            if (sizeof(T) == 2 && t + 1 < t1) load_operand(next, (const T *)a.k_pages + (int64_t)rows_of(t + 1) * 128, half);
+            const uint32_t bad_next = bad;
+            f32x16_t sum[1] = {};
+            for (int rb = 0; rb < blocks; ++rb) {
+                Operand<T> q;
+                tile_operand(q, smem, 32 * rb + (lane & 31), half);
+                add_weights<T, OPT, 1>(sum, k, q, part[32 * rb + (lane & 31)], a.o, t * 32, bad_now, half);
+            }
+            if (sizeof(T) == 4 && t + 1 < t1) load_operand(k[0], (const T *)a.k_pages + (int64_t)rows_of(t + 1) * 128, half);
+            float x = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float y = lanes32_sum(sum[0][i], have);
+                x = (lane & 15) == i ? y : x;
+            }
+            if ((lane & 16) == 0 && key < s.len) a.w_out[w0 + key] = x + before;
+            if constexpr (sizeof(T) == 2) {
+                k[0] = next;
+                bad_now = bad_next;
+            } else {
+                bad_now = bad;
             }
         }
+        r0 += kRows;
+    } while (r0 < rows);
 }
 
 // ---- append with rotary positions -----------------------------------------------------------------------
@@ -968,63 +1102,123 @@ __device__ __forceinline__ uint32_t weight_rank(float w)
     return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-// One block a unit: the rank of the last weight that stays, by four rounds of 8 bits over the keys that are free to go, then the kept ids in order, each
-// wave from a run of the keys of its own.
-__global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a)
+constexpr int kBins = 2048;   // of a round: 11, 11 and 10 bits of a rank
+
+// One block a unit: the rank of the last weight that stays, in rounds over the ranks of the keys that are free to go, then the kept ids in order.
+// With EACH > 0 a thread holds EACH ranks (keys from + 1024 i + its number), which are read once; with 0 they are read in every round.
+template <int EACH> __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a)
 {
-    __shared__ uint32_t hist[256], found[2], count[2][16];
+    constexpr int kRounds = EACH ? EACH : 1;
+    __shared__ uint32_t hist[kBins], found[2];
+    __shared__ uint64_t wave_sum[16];
+    __shared__ uint64_t count[EACH ? EACH * 16 : 16];   // over and tied keys (32 bits each) of a wave's 64 keys, then of all before them
     const CacheView &v = a.v;
-    const int unit = blockIdx.x, b = unit / v.g, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int unit = blockIdx.x, b = unit / v.g, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
     const int len = min(max(v.cur[b], 0), v.max_pages << v.page_shift), keep = min(len, a.budget);
     int32_t *ids = a.ids + (size_t)unit * a.budget;
     const float *w = a.w_in + (size_t)unit * a.w_stride;
-    if (a.lens && unit % v.g == 0 && threadIdx.x == 0) a.lens[b] = keep;
-    for (int j = keep + threadIdx.x; j < a.budget; j += 1024) ids[j] = -1;
+    if (a.lens && unit % v.g == 0 && tid == 0) a.lens[b] = keep;
+    for (int j = keep + tid; j < a.budget; j += 1024) ids[j] = -1;
     if (keep == len) {
-        for (int j = threadIdx.x; j < len; j += 1024) ids[j] = j;
+        for (int j = tid; j < len; j += 1024) ids[j] = j;
         return;
     }
-    const int from = a.n_init, to = len - a.n_local;
+    const int from = a.n_init, to = len - a.n_local, n = to - from;
+    for (int j = tid; j < a.n_init; j += 1024) ids[j] = j;
+    for (int j = tid; j < a.n_local; j += 1024) ids[keep - a.n_local + j] = to + j;
     uint32_t want = keep - a.n_init - a.n_local, prefix = 0, mask = 0;   // want: how many of those with the prefix stay
-    for (int shift = 24; shift >= 0 && want; shift -= 8) {
-        if (threadIdx.x < 256) hist[threadIdx.x] = 0;
-        __syncthreads();
-        for (int t = from + threadIdx.x; t < to; t += 1024) {
-            const uint32_t r = weight_rank(w[t]);
-            if ((r & mask) == prefix) atomicAdd(&hist[(r >> shift) & 255], 1u);
+    if (!want) return;
+    uint32_t rank[kRounds];
+    if constexpr (EACH > 0) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) rank[i] = i * 1024 + tid < n ? weight_rank(w[from + i * 1024 + tid]) : 0;
+    }
+    // f(rank, whether the key is there, its number), for all of the thread's keys; whole waves call it together
+    auto each = [&](auto f) {
+        if constexpr (EACH > 0) {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i)
+                if (i * 1024 < n) f(rank[i], i * 1024 + tid < n, i);
+        } else {
+            for (int i = 0; i * 1024 < n; ++i) f(i * 1024 + tid < n ? weight_rank(w[from + i * 1024 + tid]) : 0u, i * 1024 + tid < n, i);
         }
+    };
+    for (int shift = 21; ; shift = shift > 10 ? shift - 11 : 0) {
+        const int bits = shift ? 11 : 10;
+        hist[tid] = hist[tid + 1024] = 0;
         __syncthreads();
-        if (wave == 0) {   // from the largest bin down: the one in which the want-th lies
-            uint32_t mine[4], all = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) all += mine[i] = hist[255 - (4 * lane + i)];
-            uint32_t upto = all;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t o = __shfl_up(upto, d);
-                if (lane >= d) upto += o;
+        each([&](uint32_t r, bool there, int) {
+            const bool in = there && (r & mask) == prefix;
+            const uint32_t bin = (r >> shift) & ((1u << bits) - 1);
+            const uint64_t lanes = __ballot(in);
+            if (!lanes) return;
+            // (weights that agree in these bits, as equal ones do: one addition for all of them)
+            const uint32_t one = __builtin_amdgcn_readlane(bin, __builtin_ctzll(lanes));
+            if (__ballot(in && bin == one) == lanes) {
+                if (lane == __builtin_ctzll(lanes)) atomicAdd(&hist[one], (uint32_t)__popcll(lanes));
+            } else if (in) {
+                atomicAdd(&hist[bin], 1u);
             }
-            uint32_t above = upto - all;
+        });
+        __syncthreads();
+        // from the largest bin down (two a thread): the one in which the want-th lies
+        const uint32_t h0 = hist[kBins - 1 - 2 * tid], h1 = hist[kBins - 2 - 2 * tid];
+        uint32_t upto = h0 + h1;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (above < want && above + mine[i] >= want) {
-                    found[0] = 255 - (4 * lane + i);
-                    found[1] = want - above;
-                }
-                above += mine[i];
-            }
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+        }
+        if (lane == 63) wave_sum[wave] = upto;
+        __syncthreads();
+        uint32_t above = upto - h0 - h1;
+        for (int i = 0; i < wave; ++i) above += (uint32_t)wave_sum[i];
+        if (above < want && above + h0 >= want) {
+            found[0] = kBins - 1 - 2 * tid;
+            found[1] = want - above;
+        } else if (above + h0 < want && above + h0 + h1 >= want) {
+            found[0] = kBins - 2 - 2 * tid;
+            found[1] = want - above - h0;
         }
         __syncthreads();
         prefix |= found[0] << shift;
-        mask |= 255u << shift;
+        mask |= ((1u << bits) - 1) << shift;
         want = found[1];
-        __syncthreads();
+        if (!shift) break;
     }
     // above the prefix (the rank itself) a weight stays, at it the first `want` do
-    const bool none = keep == a.n_init + a.n_local;
-    const int run = ((to - from + 15) / 16 + 63) & ~63, my0 = from + wave * run, my1 = min(my0 + run, to);
-    uint32_t over = 0, tie = 0;
-    if (!none) {
+    const uint64_t below = (1ull << lane) - 1;
+    if constexpr (EACH > 0) {
+        each([&](uint32_t r, bool there, int i) {
+            const uint64_t over = __ballot(there && r > prefix), tie = __ballot(there && r == prefix);
+            if (lane == 0) count[i * 16 + wave] = ((uint64_t)__popcll(over) << 32) | (uint32_t)__popcll(tie);
+        });
+        __syncthreads();
+        const int slots = (n + 1023) / 1024 * 16;
+        uint64_t mine = tid < slots ? count[tid] : 0, upto = mine;   // (EACH is 64 at most)
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint64_t o = __shfl_up((unsigned long long)upto, d);
+            if (lane >= d) upto += o;
+        }
+        if (lane == 63) wave_sum[wave] = upto;
+        __syncthreads();
+        uint64_t before = upto - mine;
+        for (int i = 0; i < wave; ++i) before += wave_sum[i];
+        if (tid < slots) count[tid] = before;
+        __syncthreads();
+        each([&](uint32_t r, bool there, int i) {
+            const uint64_t c = count[i * 16 + wave];
+            const uint32_t over = (uint32_t)(c >> 32), ties = (uint32_t)c;
+            const uint64_t tie = __ballot(there && r == prefix);
+            const bool stays = there && (r > prefix || (r == prefix && ties + __popcll(tie & below) < want));
+            const uint64_t kept = __ballot(stays);
+            if (stays) ids[a.n_init + over + min(ties, want) + __popcll(kept & below)] = from + i * 1024 + tid;
+        });
+    } else {
+        // each wave from a run of the keys of its own
+        const int run = ((n + 15) / 16 + 63) & ~63, my0 = from + wave * run, my1 = min(my0 + run, to);
+        uint32_t over = 0, tie = 0;
         for (int t = my0 + lane; t < my1; t += 64) {
             const uint32_t r = weight_rank(w[t]);
             over += r > prefix;
@@ -1035,38 +1229,34 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a)
             over += __shfl_xor(over, d);
             tie += __shfl_xor(tie, d);
         }
-    }
-    if (lane == 0) {
-        count[0][wave] = over;
-        count[1][wave] = tie;
-    }
-    __syncthreads();
-    uint32_t ties = 0, at = a.n_init;
-    for (int i = 0; i < wave; ++i) {
-        at += count[0][i] + min(count[1][i], want - min(want, ties));
-        ties += count[1][i];
-    }
-    if (!none)
-        for (int t0 = my0; t0 < my1; t0 += 64) {
-            const uint32_t r = t0 + lane < my1 ? weight_rank(w[t0 + lane]) : 0;
-            const uint64_t here = __ballot(t0 + lane < my1 && r == prefix), below = (1ull << lane) - 1;
-            const bool stays = t0 + lane < my1 && (r > prefix || (r == prefix && ties + __popcll(here & below) < want));
+        if (lane == 0) count[wave] = ((uint64_t)over << 32) | tie;
+        __syncthreads();
+        uint32_t ties = 0, at = a.n_init;
+        for (int i = 0; i < wave; ++i) {
+            at += (uint32_t)(count[i] >> 32);
+            ties += (uint32_t)count[i];
+        }
+        at += min(ties, want);
+        for (int t = my0; t < my1; t += 64) {
+            const uint32_t r = t + lane < my1 ? weight_rank(w[t + lane]) : 0;
+            const uint64_t here = __ballot(t + lane < my1 && r == prefix);
+            const bool stays = t + lane < my1 && (r > prefix || (r == prefix && ties + __popcll(here & below) < want));
             const uint64_t kept = __ballot(stays);
-            if (stays) ids[at + __popcll(kept & below)] = t0 + lane;
+            if (stays) ids[at + __popcll(kept & below)] = t + lane;
             at += __popcll(kept);
             ties += __popcll(here);
         }
-    for (int j = threadIdx.x; j < a.n_init; j += 1024) ids[j] = j;
-    for (int j = threadIdx.x; j < a.n_local; j += 1024) ids[keep - a.n_local + j] = to + j;
+    }
 }
 
 // The kept rows to the front, in order and in place.  Row j comes from ids[j] >= j, so rounds of rows, read as a whole before the first of them is
-// written, overwrite nothing that a later round reads; a block has 1 / slices of every row of its unit, which no other block touches.
+// written, overwrite nothing that a later round reads; a block has 1 / slices of every row of its unit, which no other block touches.  A unit's
+// slices share lines of its rows, so they are on one XCD where the units are a multiple of 8.
 template <typename T> __global__ __launch_bounds__(512) void evict_move_kernel(EvictArgs a)
 {
     constexpr int kPieces = 2 * 128 * sizeof(T) / 16, kEach = 8;   // 16-byte pieces of a key's K and V rows
     const CacheView &v = a.v;
-    const int unit = blockIdx.x / a.slices, slice = blockIdx.x % a.slices, b = unit / v.g, kv = unit % v.g;
+    const int units = v.batch * v.g, unit = blockIdx.x % units, slice = blockIdx.x / units, b = unit / v.g, kv = unit % v.g;
     const int len = min(max(v.cur[b], 0), v.max_pages << v.page_shift), keep = min(len, a.budget);
     const int32_t *ids = a.ids + (size_t)unit * a.budget;
     const size_t w0 = (size_t)unit * a.w_stride;
@@ -1078,24 +1268,40 @@ template <typename T> __global__ __launch_bounds__(512) void evict_move_kernel(E
     }
     const int wide = kPieces / a.slices, lane_rows = 512 / wide, my = threadIdx.x / wide, piece = slice * wide + threadIdx.x % wide;
     char *pages = (char *)(piece < kPieces / 2 ? a.k_pages : a.v_pages) + 16 * (piece % (kPieces / 2));
+    const int32_t *table = v.table + (size_t)b * v.max_pages;
+    const int in_page = (1 << v.page_shift) - 1;
     for (int j0 = 0; j0 < keep; j0 += lane_rows * kEach) {
+        int id[kEach];
+        uint32_t src[kEach], dst[kEach];
         u32x4_t x[kEach];
-        char *to[kEach];
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int j = j0 + i * lane_rows + my;
-            to[i] = nullptr;
-            if (j >= keep || ids[j] == j) continue;
-            const int64_t src = cache_row(v, b, kv, ids[j]), dst = cache_row(v, b, kv, j);
-            if (src < 0 || dst < 0) continue;
-            to[i] = pages + dst * 128 * (int64_t)sizeof(T);
-            x[i] = *reinterpret_cast<const u32x4_t *>(pages + src * 128 * (int64_t)sizeof(T));
+            id[i] = j < keep ? ids[j] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int j = min(j0 + i * lane_rows + my, keep - 1);
+            src[i] = (uint32_t)table[id[i] >> v.page_shift];
+            dst[i] = (uint32_t)table[j >> v.page_shift];
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int j = j0 + i * lane_rows + my;
+            const bool move = j < keep && id[i] != j && src[i] < v.num_pages && dst[i] < v.num_pages;
+            if (move) {
+                const uint32_t from = (uint32_t)((src[i] * (uint64_t)v.g + kv) << v.page_shift) + (id[i] & in_page);
+                dst[i] = (uint32_t)((dst[i] * (uint64_t)v.g + kv) << v.page_shift) + (j & in_page);
+                x[i] = *reinterpret_cast<const u32x4_t *>(pages + (int64_t)from * (128 * (int)sizeof(T)));
+            } else {
+                dst[i] = kNoRow;
+            }
         }
         loads_landed<0>();
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
-            if (to[i]) *reinterpret_cast<u32x4_t *>(to[i]) = x[i];
+            if (dst[i] != kNoRow) *reinterpret_cast<u32x4_t *>(pages + (int64_t)dst[i] * (128 * (int)sizeof(T))) = x[i];
     }
     if (weights)
         for (int j0 = 0; j0 < keep; j0 += 512) {
