@@ -150,10 +150,11 @@ constexpr int kCap = 1, kBias = 2;
 template <int OPT> __device__ __forceinline__ void score_regs(f32x16_t &s, const ScoreOpts &o, float slope2, int pos_minus_key0, int half)
 {
     if constexpr (OPT != 0) {
+        const float far = (float)(pos_minus_key0 - 4 * half);   // (distances below 2^24 are exact)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             float z = (OPT & kCap) ? o.cap_out * tanh_f(s[i] * o.cap_in) : s[i] * o.c2;
-            if constexpr ((OPT & kBias) != 0) z = fmaf(-slope2, fabsf((float)(pos_minus_key0 - (8 * (i >> 2) + 4 * half + (i & 3)))), z);
+            if constexpr ((OPT & kBias) != 0) z = fmaf(-slope2, fabsf(far - (float)(8 * (i >> 2) + (i & 3))), z);
             s[i] = z;
         }
     }
@@ -225,14 +226,19 @@ template <typename T, int KEYS, int THREADS> struct OddValues {
     }
 };
 
-// scores of what a row does not see become -infinity
-__device__ __forceinline__ void mask_regs(f32x16_t &s, const RowSight &sight, int key0, uint64_t bad, int half)
+// Of 32 keys from key0 on (bad: those that are not there), what a row does not see becomes `none`
+__device__ __forceinline__ void mask_regs(f32x16_t &s, const RowSight &sight, int key0, uint32_t bad, int half, float none)
 {
+    const int lo = sight.lo - key0 - 4 * half, hi = sight.hi - key0 - 4 * half;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        const int k = 8 * (i >> 2) + 4 * half + (i & 3);
-        const bool sees = key0 + k >= sight.lo && key0 + k < sight.hi && !((bad >> k) & 1);
-        s[i] = sees ? s[i] : -INFINITY;
+        const int k = 8 * (i >> 2) + (i & 3);
+        s[i] = k >= lo && k < hi ? s[i] : none;
+    }
+    if (bad) {
+        const uint32_t mine = bad >> (4 * half);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = (mine >> (8 * (i >> 2) + (i & 3))) & 1 ? none : s[i];
     }
 }
 
@@ -449,7 +455,7 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
         for (int kb = 0; kb < kBlocks; ++kb) {
             sc[kb] = rows_dot<T>(kt, 32 * kb, q, f32x16_t{});
             score_regs<OPT>(sc[kb], a.o, slope2, sight.pos - (key0 + 32 * kb), half);
-            if (masked) mask_regs(sc[kb], sight, key0 + 32 * kb, bad_now >> (32 * kb), half);
+            if (masked) mask_regs(sc[kb], sight, key0 + 32 * kb, (uint32_t)(bad_now >> (32 * kb)), half, -INFINITY);
         }
         softmax_regs<OPT, kBlocks>(sc, o, m, l, a.o.c2);
         values_dot<T, kBlocks>(o, vt, sc, lane);
@@ -591,7 +597,7 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
         char *vt = smem[wave][buf];
         score_regs<OPT>(sc[0], a.o, slope2, sight.pos - key0, half);
         if (key0 + 32 > range.all_hi || key0 < all_lo || bad_now != 0) {
-            mask_regs(sc[0], sight, key0, bad_now, half);
+            mask_regs(sc[0], sight, key0, (uint32_t)bad_now, half, -INFINITY);
             if (__any(Odd::any(vt, lane))) {
                 Odd::add(o, vt, sight, key0, bad_now, half);
                 __builtin_amdgcn_wave_barrier();
@@ -716,12 +722,28 @@ struct WeightArgs {
     int nsplit;             // weights_few_kernel: blocks of a unit
 };
 
-// x added over the 32 lanes of a half; its first 16 lanes get the sum (`live` lanes hold something, from the first on)
-__device__ __forceinline__ float lanes32_sum(float x, int live)
+// 16 values a lane, each added over the 32 lanes of its half: the lane gets the sum of value (lane % 32) / 2.  At every step half of what is left goes to the
+// lanes of one half of the group and half to the other, so that it takes 38 instructions where 16 sums apart would take 80 and 16 exchanges.
+__device__ __forceinline__ float scattered_sum(const f32x16_t &s, int lane)
 {
-    x = group16_sum(x);
-    if (live > 16) x += __shfl_xor(x, 16);
-    return x;
+    float r[8], t[4], u[2];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(s[i]), __float_as_uint(s[i + 8]), false, false);
+        r[i] = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+    }
+    const bool b3 = lane & 8, b2 = lane & 4, b1 = lane & 2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = (b3 ? r[i + 4] : r[i]) + dpp_f<0x128>(b3 ? r[i] : r[i + 4]);   // row_ror:8
+#pragma unroll
+    for (int i = 0; i < 2; ++i) u[i] = (b2 ? t[i + 2] : t[i]) + dpp_f<0x141>(b2 ? t[i] : t[i + 2]);
+    const float v = (b1 ? u[1] : u[0]) + dpp_f<0x4E>(b1 ? u[0] : u[1]);
+    return v + dpp_f<0xB1>(v);
+}
+__device__ __forceinline__ int scattered_key(int lane)   // the key (of 32) whose sum that is
+{
+    const int i = (lane & 31) >> 1;
+    return 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
 }
 // A row's part in the sums: what it sees and minus its log-sum-exp (in units of log2 e; a row that sees nothing adds nothing)
 struct WeightRow {
@@ -761,22 +783,18 @@ template <typename T, int OPT, int NB> __device__ __forceinline__ void add_weigh
     }
 #pragma unroll
     for (int kb = 0; kb < NB; ++kb) score_regs<OPT>(sc[kb], o, w.slope2, w.sight.pos - k0 - 32 * kb, half);
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[kb][i] = exp2_fast(OPT == 0 ? fmaf(sc[kb][i], o.c2, w.nlse) : sc[kb][i] + w.nlse);
     if (masked) {
 #pragma unroll
-        for (int kb = 0; kb < NB; ++kb) {
-            mask_regs(sc[kb], w.sight, k0 + 32 * kb, bad >> (32 * kb), half);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float p = exp2_fast(OPT == 0 ? fmaf(sc[kb][i], o.c2, w.nlse) : sc[kb][i] + w.nlse);
-                sum[kb][i] += sc[kb][i] == -INFINITY ? 0.0f : p;
-            }
-        }
-        return;
+        for (int kb = 0; kb < NB; ++kb) mask_regs(sc[kb], w.sight, k0 + 32 * kb, (uint32_t)(bad >> (32 * kb)), half, 0.0f);
     }
 #pragma unroll
     for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum[kb][i] += exp2_fast(OPT == 0 ? fmaf(sc[kb][i], o.c2, w.nlse) : sc[kb][i] + w.nlse);
+        for (int i = 0; i < 16; ++i) sum[kb][i] += sc[kb][i];
 }
 // a row of a tile in shared memory as the second operand
 template <typename T> __device__ __forceinline__ void tile_operand(Operand<T> &q, const char *tile, int r, int half)
@@ -857,21 +875,18 @@ template <typename T, int OPT> __global__ __launch_bounds__(512, 2) void weights
     for (int turn = 1; turn >= 0; --turn) {   // the second half's sums, then the first half's with them
         if (side == turn) {
 #pragma unroll
-            for (int kb = 0; kb < kBlocks; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float x = lanes32_sum(sum[kb][i], 32);
-                    const int at = 32 * kb + 8 * (i >> 2) + 4 * half + (i & 3), key = mine0 + at;
-                    if ((lane & 31) == i) {   // (i < 16)
-                        if (turn) {
-                            other[at] = x;
-                        } else if (key < s.len) {
-                            x += other[at];
-                            if (a.w_in && key < s.old) x = fmaf(a.decay, a.w_in[unit + key], x);
-                            a.w_out[unit + key] = x;
-                        }
-                    }
+            for (int kb = 0; kb < kBlocks; ++kb) {
+                float x = scattered_sum(sum[kb], lane);
+                const int at = 32 * kb + scattered_key(lane), key = mine0 + at;
+                if (lane & 1) continue;
+                if (turn) {
+                    other[at] = x;
+                } else if (key < s.len) {
+                    x += other[at];
+                    if (a.w_in && key < s.old) x = fmaf(a.decay, a.w_in[unit + key], x);
+                    a.w_out[unit + key] = x;
                 }
+            }
         }
         if (turn) __syncthreads();
     }
@@ -909,7 +924,7 @@ template <typename T, int OPT> __global__ __launch_bounds__(256, 2) void weights
     };
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_at(smem));
     const size_t w0 = (size_t)unit * a.w_stride;
-    const int mine = 8 * ((lane & 15) >> 2) + 4 * half + (lane & 3);   // the key whose sum the lane writes (lanes 0 .. 15 of a half)
+    const int mine = scattered_key(lane);
     int r0 = 0;
     do {
         const int have = min(rows - r0, kRows), blocks = (have + 31) / 32;
@@ -943,13 +958,8 @@ template <typename T, int OPT> __global__ __launch_bounds__(256, 2) void weights
                 add_weights<T, OPT, 1>(sum, k, q, part[32 * rb + (lane & 31)], a.o, t * 32, bad_now, half);
             }
             if (sizeof(T) == 4 && t + 1 < t1) load_operand(k[0], (const T *)a.k_pages + (int64_t)rows_of(t + 1) * 128, half);
-            float x = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float y = lanes32_sum(sum[0][i], have);
-                x = (lane & 15) == i ? y : x;
-            }
-            if ((lane & 16) == 0 && key < s.len) a.w_out[w0 + key] = x + before;
+            const float x = scattered_sum(sum[0], lane);
+            if ((lane & 1) == 0 && key < s.len) a.w_out[w0 + key] = x + before;
             if constexpr (sizeof(T) == 2) {
                 k[0] = next;
                 bad_now = bad_next;
