@@ -414,15 +414,23 @@ class Cache:
 
     def __init__(self, handle: int, params: CacheParams, device: int):
         import torch
+        p = params
         self.handle = handle
-        self.params = params
+        self.params = p
         self.device = device
-        self.torch_dtype = _torch_dtype(params.dtype)
-        self.n_axes = 1 if params.rope_axis is None else int(np.max(params.rope_axis)) + 1
-        self._current_stream = torch.cuda.current_stream
+        self.torch_dtype = _torch_dtype(p.dtype)
+        self.n_axes = 1 if p.rope_axis is None else int(np.max(p.rope_axis)) + 1
+        # what every call asks for; a step of one token is a few microseconds, of which looking these up again would be a fair part
+        self._lib = load_library()
+        self._int, self._float = torch.int32, torch.float32
+        self._shapes = {"pages": (p.num_pages, p.n_kv_heads, p.page_size, 128), "cu": (p.batch + 1,), "batch": (p.batch,),
+                        "table": (p.batch, p.max_pages), "heads": (p.n_q_heads,)}
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._stream = raw if raw is not None else (lambda d: torch.cuda.current_stream(d).cuda_stream)
 
     def stream(self) -> int:
-        return self._current_stream(self.device).cuda_stream
+        """The current stream of the cache's device."""
+        return self._stream(self.device)
 
     def __del__(self):
         try:
@@ -431,50 +439,36 @@ class Cache:
             pass
 
 
-def _shape_of(name, t, shape):
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
-
-
 def _on(cache: Cache, name, t, dtype, shape):
     """Device pointer of a contiguous tensor of this type and shape on the cache's device (None passes NULL)."""
     if t is None:
         return None
-    if t.dtype != dtype:
-        raise ValueError(f"{name}: expected dtype {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        _shape_of(name, t, shape)
-    if not t.is_cuda or t.get_device() != cache.device or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous tensor on device {cache.device}")
-    return t.data_ptr()
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == cache.device:
+        return t.data_ptr()
+    raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on device {cache.device}, got "
+                     f"{t.dtype}, {tuple(t.shape)}, strides {t.stride()}, {t.device}")
 
 
 def _rows_on(cache: Cache, name, t, total, heads):
     """Device pointer and token stride of [total][heads][128], the heads of a token contiguous."""
     if t is None:
         return None, 0
-    if t.dtype != cache.torch_dtype:
-        raise ValueError(f"{name}: expected dtype {cache.torch_dtype}, got {t.dtype}")
-    if t.shape != (total, heads, 128):
-        _shape_of(name, t, (total, heads, 128))
-    if not t.is_cuda or t.get_device() != cache.device:
-        raise ValueError(f"{name}: expected a tensor on device {cache.device}")
-    stride = t.stride()
-    if total and (stride[2] != 1 or (heads > 1 and stride[1] != 128)):
-        raise ValueError(f"{name}: a token's heads must be contiguous")
-    return t.data_ptr(), (stride[0] if total > 1 else heads * 128)
+    if t.dtype is cache.torch_dtype and t.shape == (total, heads, 128) and t.get_device() == cache.device:
+        token, head, element = t.stride()
+        if total == 0 or (element == 1 and (heads == 1 or head == 128)):
+            return t.data_ptr(), (token if total > 1 else heads * 128)
+    raise ValueError(f"{name}: expected a {cache.torch_dtype} tensor of shape {(total, heads, 128)} on device {cache.device}, a token's heads "
+                     f"contiguous, got {t.dtype}, {tuple(t.shape)}, strides {t.stride()}, {t.device}")
 
 
 def _pages_on(cache: Cache, name, t):
-    p = cache.params
-    return _on(cache, name, t, cache.torch_dtype, (p.num_pages, p.n_kv_heads, p.page_size, 128))
+    return _on(cache, name, t, cache.torch_dtype, cache._shapes["pages"])
 
 
 def _batch_on(cache: Cache, cu_new, cur_lens, block_table):
-    import torch
-    p, i32 = cache.params, torch.int32
-    return (_on(cache, "cu_new", cu_new, i32, (p.batch + 1,)), _on(cache, "cur_lens", cur_lens, i32, (p.batch,)),
-            _on(cache, "block_table", block_table, i32, (p.batch, p.max_pages)))
+    s, i32 = cache._shapes, cache._int
+    return (_on(cache, "cu_new", cu_new, i32, s["cu"]), _on(cache, "cur_lens", cur_lens, i32, s["batch"]),
+            _on(cache, "block_table", block_table, i32, s["table"]))
 
 
 def ctkvr_cache_create(params: CacheParams) -> Cache:
@@ -501,62 +495,57 @@ def ctkvr_cache_free(cache: Optional[Cache]) -> None:
 
 def ctkvr_cache_append(cache: Cache, q, k, v, cu_new, cur_lens, block_table, q_out, k_pages, v_pages, positions=None) -> None:
     """q, k and v may be views of a fused projection; q and q_out, or k and v, may be None."""
-    import torch
     p = cache.params
     total = (q if q is not None else k).shape[0]
     cu, cur, table = _batch_on(cache, cu_new, cur_lens, block_table)
     (qp, qs), (kp, ks) = _rows_on(cache, "q", q, total, p.n_q_heads), _rows_on(cache, "k", k, total, p.n_kv_heads)
     vp, vs = _rows_on(cache, "v", v, total, p.n_kv_heads)
-    _check(load_library().ctkvr_cache_append(
-        cache.handle, qp, qs, kp, ks, vp, vs, _on(cache, "positions", positions, torch.int32, (cache.n_axes, total)), cu, cur, table, total,
+    _check(cache._lib.ctkvr_cache_append(
+        cache.handle, qp, qs, kp, ks, vp, vs, _on(cache, "positions", positions, cache._int, (cache.n_axes, total)), cu, cur, table, total,
         _on(cache, "q_out", q_out, cache.torch_dtype, (total, p.n_q_heads, 128)), _pages_on(cache, "k_pages", k_pages),
         _pages_on(cache, "v_pages", v_pages), cache.stream()))
 
 
 def _masks_on(cache: Cache, total, slopes, prefix_lens, first_key):
-    import torch
-    return (_on(cache, "slopes", slopes, torch.float32, (cache.params.n_q_heads,)),
-            _on(cache, "prefix_lens", prefix_lens, torch.int32, (cache.params.batch,)),
-            _on(cache, "first_key", first_key, torch.int32, (total,)))
+    return (_on(cache, "slopes", slopes, cache._float, cache._shapes["heads"]),
+            _on(cache, "prefix_lens", prefix_lens, cache._int, cache._shapes["batch"]),
+            _on(cache, "first_key", first_key, cache._int, (total,)))
 
 
 def ctkvr_cache_attn(cache: Cache, q, k_pages, v_pages, cu_new, cur_lens, block_table, out, out_lse=None, slopes=None, prefix_lens=None,
                      first_key=None) -> None:
-    import torch
     h, total = cache.params.n_q_heads, q.shape[0]
     cu, cur, table = _batch_on(cache, cu_new, cur_lens, block_table)
     qp, qs = _rows_on(cache, "q", q, total, h)
-    _check(load_library().ctkvr_cache_attn(
+    _check(cache._lib.ctkvr_cache_attn(
         cache.handle, qp, qs, _pages_on(cache, "k_pages", k_pages), _pages_on(cache, "v_pages", v_pages), cu, cur, table, total,
         *_masks_on(cache, total, slopes, prefix_lens, first_key), _on(cache, "out", out, cache.torch_dtype, (total, h, 128)),
-        _on(cache, "out_lse", out_lse, torch.float32, (total, h)), cache.stream()))
+        _on(cache, "out_lse", out_lse, cache._float, (total, h)), cache.stream()))
 
 
 def ctkvr_cache_weights(cache: Cache, q, lse, k_pages, cu_new, cur_lens, block_table, weights_in, weights_out, decay=1.0, slopes=None,
                         prefix_lens=None, first_key=None) -> None:
     """weights_in (None: zeros) and weights_out: fp32 [batch][g][weights_stride]."""
-    import torch
     p, total = cache.params, q.shape[0]
     cu, cur, table = _batch_on(cache, cu_new, cur_lens, block_table)
     qp, qs = _rows_on(cache, "q", q, total, p.n_q_heads)
     shape = (p.batch, p.n_kv_heads, weights_out.shape[-1])
-    _check(load_library().ctkvr_cache_weights(
-        cache.handle, qp, qs, _on(cache, "lse", lse, torch.float32, (total, p.n_q_heads)), _pages_on(cache, "k_pages", k_pages), cu, cur,
+    _check(cache._lib.ctkvr_cache_weights(
+        cache.handle, qp, qs, _on(cache, "lse", lse, cache._float, (total, p.n_q_heads)), _pages_on(cache, "k_pages", k_pages), cu, cur,
         table, total, *_masks_on(cache, total, slopes, prefix_lens, first_key), float(decay),
-        _on(cache, "weights_in", weights_in, torch.float32, shape), _on(cache, "weights_out", weights_out, torch.float32, shape), shape[2],
+        _on(cache, "weights_in", weights_in, cache._float, shape), _on(cache, "weights_out", weights_out, cache._float, shape), shape[2],
         cache.stream()))
 
 
 def ctkvr_cache_evict(cache: Cache, weights_in, k_pages, v_pages, cur_lens, block_table, budget, out_ids, n_init=0, n_local=0,
                       weights_out=None, out_lens=None) -> None:
     """out_ids: int32 [batch][g][budget]; out_lens: int32 [batch] or None."""
-    import torch
     p = cache.params
     shape = (p.batch, p.n_kv_heads, weights_in.shape[-1])
-    _check(load_library().ctkvr_cache_evict(
-        cache.handle, _on(cache, "weights_in", weights_in, torch.float32, shape), shape[2],
-        _on(cache, "cur_lens", cur_lens, torch.int32, (p.batch,)), _on(cache, "block_table", block_table, torch.int32, (p.batch, p.max_pages)),
+    _check(cache._lib.ctkvr_cache_evict(
+        cache.handle, _on(cache, "weights_in", weights_in, cache._float, shape), shape[2],
+        _on(cache, "cur_lens", cur_lens, cache._int, cache._shapes["batch"]), _on(cache, "block_table", block_table, cache._int, cache._shapes["table"]),
         int(budget), int(n_init), int(n_local), _pages_on(cache, "k_pages", k_pages), _pages_on(cache, "v_pages", v_pages),
-        _on(cache, "weights_out", weights_out, torch.float32, shape),
-        _on(cache, "out_ids", out_ids, torch.int32, (p.batch, p.n_kv_heads, int(budget))),
-        _on(cache, "out_lens", out_lens, torch.int32, (p.batch,)), cache.stream()))
+        _on(cache, "weights_out", weights_out, cache._float, shape),
+        _on(cache, "out_ids", out_ids, cache._int, (p.batch, p.n_kv_heads, int(budget))),
+        _on(cache, "out_lens", out_lens, cache._int, cache._shapes["batch"]), cache.stream()))

@@ -1104,26 +1104,59 @@ struct EvictArgs {
     int slices;
 };
 
-// a weight's rank: larger weights have larger words, -0 is +0, NaN comes last
+// a weight's rank: larger weights have larger words, -0 is +0; NaN comes last, with 1, and 0 is no key's
 __device__ __forceinline__ uint32_t weight_rank(float w)
 {
-    if (w != w) return 0;
     const uint32_t u = __float_as_uint(w + 0.0f);
-    return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+    const uint32_t r = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+    return w == w ? r : 1;
 }
 
-constexpr int kBins = 2048;   // of a round: 11, 11 and 10 bits of a rank
+constexpr int kBins = 2048;    // of a round over the ranks: 11, 11 and 10 bits, four counters each (lanes that agree in these bits wait for fewer others)
+constexpr int kTied = 256;     // ranks of the deciding bin that a wave holds in shared memory
 
-// One block a unit: the rank of the last weight that stays, in rounds over the ranks of the keys that are free to go, then the kept ids in order.
-// With EACH > 0 a thread holds EACH ranks (keys from + 1024 i + its number), which are read once; with 0 they are read in every round.
+// The bin (from the largest down, two a thread) in which the want-th value lies, how many of that bin's are wanted, and how many it has
+struct Found {
+    uint32_t bin, want, has;
+};
+__device__ __forceinline__ Found find_bin(const uint4 *hist, uint32_t want, uint32_t *wave_sum, Found *found)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint4 c0 = hist[kBins - 1 - 2 * tid], c1 = hist[kBins - 2 - 2 * tid];
+    const uint32_t h0 = c0.x + c0.y + c0.z + c0.w, h1 = c1.x + c1.y + c1.z + c1.w;
+    uint32_t upto = h0 + h1;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_up(upto, d);
+        if (lane >= d) upto += o;
+    }
+    if (lane == 63) wave_sum[wave] = upto;
+    __syncthreads();
+    uint32_t above = upto - h0 - h1;
+    for (int i = 0; i < wave; ++i) above += wave_sum[i];
+    if (above < want && above + h0 >= want) *found = Found{(uint32_t)(kBins - 1 - 2 * tid), want - above, h0};
+    else if (above + h0 < want && above + h0 + h1 >= want) *found = Found{(uint32_t)(kBins - 2 - 2 * tid), want - above - h0, h1};
+    __syncthreads();
+    return *found;
+}
+__device__ __forceinline__ uint32_t lanes_below(uint64_t mask)   // lanes of the mask before this one
+{
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// One block a unit: the rank of the last weight that stays, found over the ranks of the keys that are free to go by their first 11 bits and then among those
+// that share these, then the kept ids in order.  Each wave has a run of the keys, 64 at a time; with EACH > 0 that is 64 EACH keys whose ranks it holds, with 0
+// they are read in every pass.  Lanes without a key hold rank 0, the lowest, which is never reached: more keys than are wanted have one above it.
+// What bounds it is the instructions of the unit's one CU.
 template <int EACH> __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a)
 {
-    constexpr int kRounds = EACH ? EACH : 1;
-    __shared__ uint32_t hist[kBins], found[2];
-    __shared__ uint64_t wave_sum[16];
-    __shared__ uint64_t count[EACH ? EACH * 16 : 16];   // over and tied keys (32 bits each) of a wave's 64 keys, then of all before them
+    __shared__ uint4 hist4[kBins];
+    __shared__ uint32_t tied[16][kTied], wave_sum[16], many;
+    __shared__ uint2 count[16];   // a wave's keys above the last rank, and at it
+    __shared__ Found found;
+    uint32_t *hist = reinterpret_cast<uint32_t *>(hist4);
     const CacheView &v = a.v;
-    const int unit = blockIdx.x, b = unit / v.g, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
+    const int unit = blockIdx.x, b = unit / v.g, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tid = threadIdx.x;
     const int len = min(max(v.cur[b], 0), v.max_pages << v.page_shift), keep = min(len, a.budget);
     int32_t *ids = a.ids + (size_t)unit * a.budget;
     const float *w = a.w_in + (size_t)unit * a.w_stride;
@@ -1134,135 +1167,135 @@ template <int EACH> __global__ __launch_bounds__(1024) void evict_select_kernel(
         return;
     }
     const int from = a.n_init, to = len - a.n_local, n = to - from;
-    for (int j = tid; j < a.n_init; j += 1024) ids[j] = j;
-    for (int j = tid; j < a.n_local; j += 1024) ids[keep - a.n_local + j] = to + j;
-    uint32_t want = keep - a.n_init - a.n_local, prefix = 0, mask = 0;   // want: how many of those with the prefix stay
-    if (!want) return;
-    uint32_t rank[kRounds];
+    const int run = EACH ? 64 * EACH : ((n + 15) / 16 + 63) & ~63, my0 = from + wave * run, mine = min(max(to - my0, 0), run);
+    const uint32_t all = keep - a.n_init - a.n_local;   // so many of them stay, fewer than n
+    uint32_t rank[EACH ? EACH : 1];
     if constexpr (EACH > 0) {
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) rank[i] = i * 1024 + tid < n ? weight_rank(w[from + i * 1024 + tid]) : 0;
+        for (int i = 0; i < EACH; ++i)
+            if (64 * i < mine) rank[i] = __float_as_uint(w[my0 + min(64 * i + lane, mine - 1)]);
     }
-    // f(rank, whether the key is there, its number), for all of the thread's keys; whole waves call it together
+    for (int j = tid; j < a.n_init; j += 1024) ids[j] = j;
+    for (int j = tid; j < a.n_local; j += 1024) ids[keep - a.n_local + j] = to + j;
+    if (!all) return;
+    hist4[tid] = hist4[tid + 1024] = uint4{};
+    if (tid == 0) many = 0;
+    __syncthreads();
+    if constexpr (EACH > 0) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (64 * i < mine) rank[i] = 64 * i + lane < mine ? weight_rank(__uint_as_float(rank[i])) : 0;
+    }
+    // f(rank, key), for all of the wave's keys
     auto each = [&](auto f) {
         if constexpr (EACH > 0) {
 #pragma unroll
             for (int i = 0; i < EACH; ++i)
-                if (i * 1024 < n) f(rank[i], i * 1024 + tid < n, i);
+                if (64 * i < mine) f(rank[i], my0 + 64 * i + lane);
         } else {
-            for (int i = 0; i * 1024 < n; ++i) f(i * 1024 + tid < n ? weight_rank(w[from + i * 1024 + tid]) : 0u, i * 1024 + tid < n, i);
+            for (int i = 0; i < mine; i += 64) f(i + lane < mine ? weight_rank(w[my0 + i + lane]) : 0u, my0 + i + lane);
         }
     };
-    for (int shift = 21; ; shift = shift > 10 ? shift - 11 : 0) {
-        const int bits = shift ? 11 : 10;
-        hist[tid] = hist[tid + 1024] = 0;
-        __syncthreads();
-        each([&](uint32_t r, bool there, int) {
-            const bool in = there && (r & mask) == prefix;
-            const uint32_t bin = (r >> shift) & ((1u << bits) - 1);
-            const uint64_t lanes = __ballot(in);
-            if (!lanes) return;
-            // (weights that agree in these bits, as equal ones do: one addition for all of them)
-            const uint32_t one = __builtin_amdgcn_readlane(bin, __builtin_ctzll(lanes));
-            if (__ballot(in && bin == one) == lanes) {
-                if (lane == __builtin_ctzll(lanes)) atomicAdd(&hist[one], (uint32_t)__popcll(lanes));
-            } else if (in) {
-                atomicAdd(&hist[bin], 1u);
-            }
-        });
-        __syncthreads();
-        // from the largest bin down (two a thread): the one in which the want-th lies
-        const uint32_t h0 = hist[kBins - 1 - 2 * tid], h1 = hist[kBins - 2 - 2 * tid];
-        uint32_t upto = h0 + h1;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t o = __shfl_up(upto, d);
-            if (lane >= d) upto += o;
+    const uint32_t way = lane & 3;
+    each([&](uint32_t r, int) { atomicAdd(&hist[(r >> 21) * 4 + way], 1u); });
+    __syncthreads();
+    const Found top = find_bin(hist4, all, wave_sum, &found);
+    // the bin's ranks of each wave to shared memory, as far as there is room, and how many of the wave's keys are above it
+    uint32_t over = 0, tie = 0, held = 0;
+    each([&](uint32_t r, int) {
+        over += __popcll(__ballot(r >> 21 > top.bin));
+        const uint64_t in = __ballot(r >> 21 == top.bin);
+        if (!in) return;
+        const uint32_t at = held + lanes_below(in);
+        if (r >> 21 == top.bin && at < kTied) tied[wave][at] = r;
+        held += __popcll(in);
+    });
+    if (held > kTied) many = 1;
+    uint32_t last = top.bin << 21, want = top.want;
+    hist4[tid] = hist4[tid + 1024] = uint4{};
+    __syncthreads();
+    // the ranks that share the bin, from shared memory or where they are
+    auto each_tied = [&](auto f) {
+        if (!many) {
+            for (uint32_t i = lane; i < held; i += 64) f(tied[wave][i]);
+        } else {
+            each([&](uint32_t r, int) {
+                if (r >> 21 == top.bin) f(r);
+            });
         }
-        if (lane == 63) wave_sum[wave] = upto;
+    };
+    if (want < top.has) {
+        each_tied([&](uint32_t r) { atomicAdd(&hist[((r >> 10) & 2047) * 4 + way], 1u); });
         __syncthreads();
-        uint32_t above = upto - h0 - h1;
-        for (int i = 0; i < wave; ++i) above += (uint32_t)wave_sum[i];
-        if (above < want && above + h0 >= want) {
-            found[0] = kBins - 1 - 2 * tid;
-            found[1] = want - above;
-        } else if (above + h0 < want && above + h0 + h1 >= want) {
-            found[0] = kBins - 2 - 2 * tid;
-            found[1] = want - above - h0;
+        const Found mid = find_bin(hist4, want, wave_sum, &found);
+        last |= mid.bin << 10;
+        want = mid.want;
+        if (want < mid.has) {
+            __syncthreads();
+            hist4[tid] = hist4[tid + 1024] = uint4{};
+            __syncthreads();
+            each_tied([&](uint32_t r) {
+                if ((r & ~1023u) == last) atomicAdd(&hist[(r & 1023) * 4 + way], 1u);
+            });
+            __syncthreads();
+            const Found low = find_bin(hist4, want, wave_sum, &found);
+            last |= low.bin;
+            want = low.want;
+            if (want == low.has) want = 0, last -= 1;
+        } else {
+            want = 0, last -= 1;
         }
-        __syncthreads();
-        prefix |= found[0] << shift;
-        mask |= ((1u << bits) - 1) << shift;
-        want = found[1];
-        if (!shift) break;
-    }
-    // above the prefix (the rank itself) a weight stays, at it the first `want` do
-    const uint64_t below = (1ull << lane) - 1;
-    if constexpr (EACH > 0) {
-        each([&](uint32_t r, bool there, int i) {
-            const uint64_t over = __ballot(there && r > prefix), tie = __ballot(there && r == prefix);
-            if (lane == 0) count[i * 16 + wave] = ((uint64_t)__popcll(over) << 32) | (uint32_t)__popcll(tie);
-        });
-        __syncthreads();
-        const int slots = (n + 1023) / 1024 * 16;
-        uint64_t mine = tid < slots ? count[tid] : 0, upto = mine;   // (EACH is 64 at most)
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint64_t o = __shfl_up((unsigned long long)upto, d);
-            if (lane >= d) upto += o;
-        }
-        if (lane == 63) wave_sum[wave] = upto;
-        __syncthreads();
-        uint64_t before = upto - mine;
-        for (int i = 0; i < wave; ++i) before += wave_sum[i];
-        if (tid < slots) count[tid] = before;
-        __syncthreads();
-        each([&](uint32_t r, bool there, int i) {
-            const uint64_t c = count[i * 16 + wave];
-            const uint32_t over = (uint32_t)(c >> 32), ties = (uint32_t)c;
-            const uint64_t tie = __ballot(there && r == prefix);
-            const bool stays = there && (r > prefix || (r == prefix && ties + __popcll(tie & below) < want));
-            const uint64_t kept = __ballot(stays);
-            if (stays) ids[a.n_init + over + min(ties, want) + __popcll(kept & below)] = from + i * 1024 + tid;
-        });
     } else {
-        // each wave from a run of the keys of its own
-        const int run = ((n + 15) / 16 + 63) & ~63, my0 = from + wave * run, my1 = min(my0 + run, to);
-        uint32_t over = 0, tie = 0;
-        for (int t = my0 + lane; t < my1; t += 64) {
-            const uint32_t r = weight_rank(w[t]);
-            over += r > prefix;
-            tie += r == prefix;
+        want = 0, last -= 1;   // (a whole bin stays: what is above the rank before it)
+    }
+    // above `last` a weight stays, at it the first `want` do
+    if (!many) {
+        uint32_t x = 0, y = 0;
+        for (uint32_t i = lane; i < held; i += 64) {
+            const uint32_t r = tied[wave][i];
+            x += r > last;
+            y += r == last;
         }
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            over += __shfl_xor(over, d);
-            tie += __shfl_xor(tie, d);
+            x += __shfl_xor(x, d);
+            y += __shfl_xor(y, d);
         }
-        if (lane == 0) count[wave] = ((uint64_t)over << 32) | tie;
-        __syncthreads();
-        uint32_t ties = 0, at = a.n_init;
-        for (int i = 0; i < wave; ++i) {
-            at += (uint32_t)(count[i] >> 32);
-            ties += (uint32_t)count[i];
-        }
-        at += min(ties, want);
-        for (int t = my0; t < my1; t += 64) {
-            const uint32_t r = t + lane < my1 ? weight_rank(w[t + lane]) : 0;
-            const uint64_t here = __ballot(t + lane < my1 && r == prefix);
-            const bool stays = t + lane < my1 && (r > prefix || (r == prefix && ties + __popcll(here & below) < want));
-            const uint64_t kept = __ballot(stays);
-            if (stays) ids[at + __popcll(kept & below)] = t + lane;
-            at += __popcll(kept);
-            ties += __popcll(here);
-        }
+        over += x;
+        tie = y;
+    } else {
+        over = 0;
+        each([&](uint32_t r, int) {
+            over += __popcll(__ballot(r > last));
+            tie += __popcll(__ballot(r == last));
+        });
     }
+    if (lane == 0) count[wave] = make_uint2(over, tie);
+    __syncthreads();
+    uint32_t ties = 0, at = a.n_init;
+    for (int i = 0; i < wave; ++i) {
+        at += count[i].x;
+        ties += count[i].y;
+    }
+    at += min(ties, want);
+    each([&](uint32_t r, int key) {
+        uint64_t kept = __ballot(r > last);
+        if (want) {
+            const uint64_t here = __ballot(r == last);
+            if (here) {
+                kept |= __ballot(r == last && ties + lanes_below(here) < want);
+                ties += __popcll(here);
+            }
+        }
+        if (kept >> lane & 1) ids[at + lanes_below(kept)] = key;
+        at += __popcll(kept);
+    });
 }
 
 // The kept rows to the front, in order and in place.  Row j comes from ids[j] >= j, so rounds of rows, read as a whole before the first of them is
 // written, overwrite nothing that a later round reads; a block has 1 / slices of every row of its unit, which no other block touches.  A unit's
 // slices share lines of its rows, so they are on one XCD where the units are a multiple of 8.
-template <typename T> __global__ __launch_bounds__(512) void evict_move_kernel(EvictArgs a)
+template <typename T> __global__ __launch_bounds__(1024) void evict_move_kernel(EvictArgs a)
 {
     constexpr int kPieces = 2 * 128 * sizeof(T) / 16, kEach = 8;   // 16-byte pieces of a key's K and V rows
     const CacheView &v = a.v;
@@ -1273,10 +1306,10 @@ template <typename T> __global__ __launch_bounds__(512) void evict_move_kernel(E
     const bool weights = a.w_out && slice == 0;
     if (keep == len) {
         if (weights && a.w_out != a.w_in)
-            for (int j = threadIdx.x; j < keep; j += 512) a.w_out[w0 + j] = a.w_in[w0 + j];
+            for (int j = threadIdx.x; j < keep; j += 1024) a.w_out[w0 + j] = a.w_in[w0 + j];
         return;
     }
-    const int wide = kPieces / a.slices, lane_rows = 512 / wide, my = threadIdx.x / wide, piece = slice * wide + threadIdx.x % wide;
+    const int wide = kPieces / a.slices, lane_rows = 1024 / wide, my = threadIdx.x / wide, piece = slice * wide + threadIdx.x % wide;
     char *pages = (char *)(piece < kPieces / 2 ? a.k_pages : a.v_pages) + 16 * (piece % (kPieces / 2));
     const int32_t *table = v.table + (size_t)b * v.max_pages;
     const int in_page = (1 << v.page_shift) - 1;
@@ -1314,7 +1347,7 @@ template <typename T> __global__ __launch_bounds__(512) void evict_move_kernel(E
             if (dst[i] != kNoRow) *reinterpret_cast<u32x4_t *>(pages + (int64_t)dst[i] * (128 * (int)sizeof(T))) = x[i];
     }
     if (weights)
-        for (int j0 = 0; j0 < keep; j0 += 512) {
+        for (int j0 = 0; j0 < keep; j0 += 1024) {
             const int j = j0 + threadIdx.x;
             const float x = j < keep ? a.w_in[w0 + ids[j]] : 0.0f;
             loads_landed<0>();
