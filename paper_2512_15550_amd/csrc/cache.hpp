@@ -243,7 +243,10 @@ __device__ __forceinline__ void mask_regs(f32x16_t &s, const RowSight &sight, in
 }
 
 // A tile's scores to probabilities under the running maximum m (in units of log2 e, as all exponents here), their sum to l, the outputs so far to the
-// new maximum.  While m is -infinity the outputs are 0, or infinities that stay.
+// new maximum.  m follows the scores only where they have left it by kSlack behind: up to there a probability is 2^kSlack at most, which costs no precision, and
+// the 64 products for the outputs are needed in few tiles rather than wherever one of 32 rows finds a new maximum.  While m is -infinity the outputs
+// are 0, or infinities that stay.
+constexpr float kSlack = 8.0f;
 template <int OPT, int NB> __device__ __forceinline__ void softmax_regs(f32x16_t (&sc)[NB], f32x16_t (&o)[4], float &m, float &l, float c2)
 {
     float top = -INFINITY;
@@ -253,7 +256,7 @@ template <int OPT, int NB> __device__ __forceinline__ void softmax_regs(f32x16_t
         for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
     top = half_max(top);
     if constexpr (OPT == 0) top *= c2;
-    if (__any(top > m)) {
+    if (__any(top > m + kSlack)) {
         const float m_new = fmaxf(m, top), scale = m == -INFINITY ? 1.0f : exp2_fast(m - m_new);
         m = m_new;
         l *= scale;
@@ -410,15 +413,35 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
         const uint32_t other = __builtin_amdgcn_readlane(r, __builtin_ctzll(ok));
         return r != kNoRow ? r : other;
     };
+    // A wave's share of a tile, 16 keys (8 in fp32) at a time.  Where they are in one page the distance to the first of them is the same in every tile and
+    // the address of that one is the wave's, not a lane's.
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_at(smem));
-    auto fetch = [&](int buf, uint32_t r) {
+    constexpr int kShare = kKeys / NW;
+    const bool one_page = (1 << v.page_shift) >= kShare;
+    uint32_t lane_off[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+        const int in = j * kPer + lane / RowTile<T>::kChunks;
+        lane_off[j] = in * RowTile<T>::kRowBytes + 16 * ((lane % RowTile<T>::kChunks) ^ swz<T>(wave * kShare + in));
+    }
+    auto fetch = [&](int buf, uint32_t r, bool whole) {
+        const uint32_t to = lds0 + buf * 2 * kTile + wave * kShare * RowTile<T>::kRowBytes;
+        if (one_page && whole) {
+            const int64_t from = (int64_t)(uint32_t)__builtin_amdgcn_readlane(r, wave * kShare) * RowTile<T>::kRowBytes;
+            const char *k = (const char *)a.k_pages + from, *x = (const char *)a.v_pages + from;
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                load_to_lds(to + j * 1024, k, lane_off[j]);
+                load_to_lds(to + j * 1024 + kTile, x, lane_off[j]);
+            }
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int at0 = (wave * kLoads + j) * kPer, key = at0 + lane / RowTile<T>::kChunks, c = (lane % RowTile<T>::kChunks) ^ swz<T>(key);
-            const int64_t from = (int64_t)(uint32_t)__shfl((int)r, key) * RowTile<T>::kRowBytes + 16 * c;
-            const uint32_t to = lds0 + buf * 2 * kTile + at0 * RowTile<T>::kRowBytes;
-            row_to_lds(to, (const char *)a.k_pages + from);
-            row_to_lds(to + kTile, (const char *)a.v_pages + from);
+            const int in = j * kPer + lane / RowTile<T>::kChunks;
+            const int64_t from = (int64_t)(uint32_t)__shfl((int)r, wave * kShare + in) * RowTile<T>::kRowBytes + (lane_off[j] - in * RowTile<T>::kRowBytes);
+            row_to_lds(to + j * 1024, (const char *)a.k_pages + from);
+            row_to_lds(to + j * 1024 + kTile, (const char *)a.v_pages + from);
         }
     };
 
@@ -427,41 +450,58 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
     const float slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
     uint64_t bad_now = 0;
     uint32_t next = 0;
-    if (t0 < t1) {
-        fetch(0, rows_of(t0));
-        bad_now = bad;
-        if (t0 + 1 < t1) next = rows_of(t0 + 1);
-        loads_landed<0>();
-        __syncthreads();
-    }
-    for (int t = t0; t < t1; ++t) {
-        const int buf = (t - t0) & 1;
+    // tile t in buffer `buf`, with the tile behind it on its way; MASKED: some row may not see some key
+    auto step = [&](auto buf, auto masked, int t) {
         const uint64_t bad_next = bad;
         if (t + 1 < t1) {
-            fetch(buf ^ 1, next);
+            fetch(buf ^ 1, next, bad == 0 && (t + 2) * kKeys <= range.hi);
             if (t + 2 < t1) next = rows_of(t + 2);
         }
         char *kt = smem[buf][0], *vt = smem[buf][1];
         const int key0 = t * kKeys;
-        const bool masked = key0 + kKeys > range.all_hi || key0 < all_lo || bad_now != 0;
-        if (masked && __syncthreads_or(Odd::any(vt, threadIdx.x))) {
-            Odd::add(o, vt, sight, key0, bad_now, half);
-            __syncthreads();
-            Odd::clean(vt, threadIdx.x);
-            __syncthreads();
+        if constexpr (decltype(masked)::value) {
+            if (__syncthreads_or(Odd::any(vt, threadIdx.x))) {
+                Odd::add(o, vt, sight, key0, bad_now, half);
+                __syncthreads();
+                Odd::clean(vt, threadIdx.x);
+                __syncthreads();
+            }
         }
         f32x16_t sc[kBlocks];
 #pragma unroll
+        for (int kb = 0; kb < kBlocks; ++kb) sc[kb] = rows_dot<T>(kt, 32 * kb, q, f32x16_t{});
+#pragma unroll
         for (int kb = 0; kb < kBlocks; ++kb) {
-            sc[kb] = rows_dot<T>(kt, 32 * kb, q, f32x16_t{});
             score_regs<OPT>(sc[kb], a.o, slope2, sight.pos - (key0 + 32 * kb), half);
-            if (masked) mask_regs(sc[kb], sight, key0 + 32 * kb, (uint32_t)(bad_now >> (32 * kb)), half, -INFINITY);
+            if constexpr (decltype(masked)::value) mask_regs(sc[kb], sight, key0 + 32 * kb, (uint32_t)(bad_now >> (32 * kb)), half, -INFINITY);
         }
         softmax_regs<OPT, kBlocks>(sc, o, m, l, a.o.c2);
         values_dot<T, kBlocks>(o, vt, sc, lane);
         bad_now = bad_next;
         loads_landed<0>();
         __syncthreads();
+    };
+    if (t0 < t1) {
+        const uint32_t r = rows_of(t0);
+        bad_now = bad;
+        fetch(0, r, bad == 0 && (t0 + 1) * kKeys <= range.hi);
+        if (t0 + 1 < t1) next = rows_of(t0 + 1);
+        loads_landed<0>();
+        __syncthreads();
+    }
+    auto seen_by_all = [&](int t, uint64_t none) { return (t + 1) * kKeys <= range.all_hi && t * kKeys >= all_lo && none == 0; };
+    int t = t0;
+    while (t < t1) {
+        // (two at a time: where a tile is in shared memory is then part of the instructions)
+        if (((t - t0) & 1) == 0)
+            while (t + 1 < t1 && seen_by_all(t, bad_now) && seen_by_all(t + 1, bad)) {
+                step(std::integral_constant<int, 0>(), std::false_type(), t);
+                step(std::integral_constant<int, 1>(), std::false_type(), t + 1);
+                t += 2;
+            }
+        if (t >= t1) break;
+        step((t - t0) & 1, std::true_type(), t);
+        ++t;
     }
 
     l = half_sum(l);
