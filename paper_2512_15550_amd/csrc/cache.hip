@@ -131,7 +131,8 @@ AttnPlan attn_plan(const ctkvr_cache *c, int total)
     const int64_t wide = (rows >> 7) + used;
     p.few = rows <= 64ll * used || wide * g < cus;
     p.tiles = (int)(p.few ? (rows >> 5) + used : wide);
-    const int64_t blocks = p.tiles * g, want = p.few ? (used > 1 ? 8 * cus : cus) : cus, least = p.few ? 256 : 512;
+    const int64_t blocks = p.tiles * g, want = p.few ? (used > 1 ? 8 : c->p.dtype == CTKVR_BF16 ? 1 : 2) * cus : cus;
+    const int64_t least = !p.few ? 512 : c->p.dtype == CTKVR_BF16 ? 256 : 64;   // keys of a run
     p.nsplit = (int)std::max<int64_t>(1, std::min({want / blocks, (keys + least - 1) / least, (int64_t)kMaxSplit}));
     return p;
 }
@@ -179,9 +180,12 @@ template <typename T> int weights_launch(const ctkvr_cache *c, WeightArgs &a, in
             return 0;
         });
     } else {
-        const int tile = sizeof(T) == 2 ? 256 : 128;
+        // (rows go past 256 keys of a block, 128 in fp32, unless that leaves CUs without one)
+        constexpr int kWide = sizeof(T) == 2 ? 256 : 128;
+        const int64_t wide = (keys + kWide - 1) / kWide * units, narrow = (keys + kWide / 4 - 1) / (kWide / 4) * units;
         with_opts(opt, [&](auto o) {
-            weights_kernel<T, decltype(o)::value><<<dim3((unsigned)((keys + tile - 1) / tile * units)), 512, 0, st>>>(a);
+            if (wide >= c->num_cu) weights_kernel<T, decltype(o)::value><<<dim3((unsigned)wide), 512, 0, st>>>(a);
+            else weights_rows_kernel<T, decltype(o)::value><<<dim3((unsigned)narrow), 512, 0, st>>>(a);
             return 0;
         });
     }
@@ -375,11 +379,11 @@ int ctkvr_cache_evict(ctkvr_cache *c, const float *weights_in, int32_t weights_s
     else if (keys <= 32768) evict_select_kernel<32><<<dim3((unsigned)units), 1024, 0, st>>>(a);
     else if (keys <= 65536) evict_select_kernel<64><<<dim3((unsigned)units), 1024, 0, st>>>(a);
     else evict_select_kernel<0><<<dim3((unsigned)units), 1024, 0, st>>>(a);
-    // Slices of 128 bytes, a line, unless that leaves CUs without a block; down to 32 bytes of a row then.  8 / 32 / 128 units of 4096 or 5000 kept rows, us, with
+    // Slices of 128 bytes, a line, and down to 32 while every block still has a CU.  8 / 32 / 128 units of 4096 or 5000 kept rows, us, with
     // slices of 128, 64, 32 and 16 bytes: 19.0, 12.5, 11.6, 14.1 / 29.1, 26.2, 33.6, 55.0 / 44.4, 45.3, 86.5, 191.
     const int pieces = c->p.dtype == CTKVR_BF16 ? 32 : 64;
     a.slices = pieces / 8;
-    while (a.slices < pieces / 2 && units * a.slices < c->num_cu) a.slices *= 2;
+    while (a.slices < pieces / 2 && 2 * units * a.slices <= c->num_cu) a.slices *= 2;
     if (c->p.dtype == CTKVR_BF16) evict_move_kernel<bf16_t><<<dim3((unsigned)(units * a.slices)), 1024, 0, st>>>(a);
     else evict_move_kernel<float><<<dim3((unsigned)(units * a.slices)), 1024, 0, st>>>(a);
     return launched("ctkvr_cache_evict");

@@ -559,8 +559,15 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
             all_lo = max(all_lo, __shfl_xor(all_lo, d));
         }
     }
-    const int first_tile = k_lo / 32, tiles = range.hi > k_lo ? (range.hi + 31) / 32 - first_tile : 0;
-    const int64_t runs = (int64_t)a.nsplit * NW, run = split * NW + wave;
+    const int first_tile = k_lo / 32, tiles = range.hi > k_lo ? (range.hi + 31) / 32 - first_tile : 0, have = min(32, rows - r0);
+    // as many of the runs as the keys are worth: two tiles a wave (in fp32 one) at least; the other blocks have nothing to do
+    const int per = sizeof(T) == 2 ? 2 * NW : NW, used = max(1, min(a.nsplit, (tiles + per - 1) / per));
+    auto row_out = [&](int r) { return (size_t)(s.c0 + ((r0 + r) >> v.lg)) * v.h + (kv << v.lg) + ((r0 + r) & ((1 << v.lg) - 1)); };
+    if (split >= used) {
+        if ((int)threadIdx.x < have) a.part_lse[(size_t)split * v.total * v.h + row_out(threadIdx.x)] = -INFINITY;
+        return;
+    }
+    const int64_t runs = (int64_t)used * NW, run = split * NW + wave;
     const int t0 = __builtin_amdgcn_readfirstlane(first_tile + (int)(tiles * run / runs));
     const int t1 = __builtin_amdgcn_readfirstlane(first_tile + (int)(tiles * (run + 1) / runs));
 
@@ -675,7 +682,6 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
             *reinterpret_cast<f32x4_t *>(mine + r32 * 512 + (((8 * db + 2 * i + half) ^ r32) << 4)) = x;
         }
     __syncthreads();
-    const int have = min(32, rows - r0);
     for (int j = threadIdx.x; j < have * 32; j += 64 * NW) {   // (row, four elements)
         const int r = j >> 5, c = j & 31;
         float t = join[0][0][r], sum = 0.0f;
@@ -690,7 +696,7 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
         }
         x *= inv_sum(sum);
         const float lse = lse_of(t, sum);
-        const size_t at_row = (size_t)(s.c0 + ((r0 + r) >> v.lg)) * v.h + (kv << v.lg) + ((r0 + r) & ((1 << v.lg) - 1));
+        const size_t at_row = row_out(r);
         if (a.nsplit > 1) {
             const size_t n = (size_t)split * v.total * v.h + at_row;
             if (c == 0) a.part_lse[n] = lse;
@@ -932,6 +938,70 @@ template <typename T, int OPT> __global__ __launch_bounds__(512, 2) void weights
     }
 }
 
+// Many rows, few keys: one block 32 kBlocks keys, a wave an eighth of the rows, which it reads as operands where they are (the keys being few, from a
+// cache); the eight sums of a key are added at the end, in order.
+template <typename T, int OPT> __global__ __launch_bounds__(512, 2) void weights_rows_kernel(WeightArgs a)
+{
+    constexpr int kBlocks = sizeof(T) == 2 ? 2 : 1, kKeys = 32 * kBlocks;
+    __shared__ float sums[8][kKeys];
+    const CacheView &v = a.v;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int kv = blockIdx.x % v.g, b = blockIdx.x / v.g % v.batch, key0 = blockIdx.x / v.g / v.batch * kKeys;
+    const SeqSpan s = seq_span(v, b);
+    if (key0 >= s.len) return;
+    const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0, rows = s.n << v.lg;
+    Operand<T> k[kBlocks];
+    uint64_t bad = 0;
+#pragma unroll
+    for (int kb = 0; kb < kBlocks; ++kb) {
+        const int key = key0 + 32 * kb + (lane & 31);
+        const uint32_t r = key < s.len ? (uint32_t)cache_row(v, b, kv, key) : kNoRow;
+        bad |= (__ballot(r == kNoRow) & 0xffffffffull) << (32 * kb);
+        load_operand(k[kb], (const T *)a.k_pages + (int64_t)(r == kNoRow ? 0 : r) * 128, half);
+    }
+    const int tok0 = prefix > key0 ? 0 : min(max(key0 - s.old, 0), s.n), tok_pos = min(max(0, -s.old), s.n);
+    const int t0 = (max(tok0, tok_pos) << v.lg) / 32, t1 = (rows + 31) / 32;
+    f32x16_t sum[kBlocks] = {};
+    auto operand = [&](Operand<T> &q, int t) {
+        const int r = min(32 * t + (lane & 31), rows - 1);
+        load_operand(q, (const T *)a.q + (int64_t)(s.c0 + (r >> v.lg)) * a.q_stride + ((kv << v.lg) + (r & ((1 << v.lg) - 1))) * 128, half);
+    };
+    int t = __builtin_amdgcn_readfirstlane(t0 + wave);
+    Operand<T> q;
+    WeightRow w{};
+    if (t < t1) {
+        operand(q, t);
+        w = weight_row<OPT>(a, s, prefix, kv, 32 * t + (lane & 31), rows);
+    }
+    for (; t < t1; t += 8) {
+        Operand<T> q_next;
+        WeightRow w_next{};
+        if (t + 8 < t1) {
+            if constexpr (sizeof(T) == 2) operand(q_next, t + 8);
+            w_next = weight_row<OPT>(a, s, prefix, kv, 32 * (t + 8) + (lane & 31), rows);
+        }
+        add_weights<T, OPT, kBlocks>(sum, k, q, w, a.o, key0, bad, half);
+        if constexpr (sizeof(T) == 2) q = q_next;
+        else if (t + 8 < t1) operand(q, t + 8);
+        w = w_next;
+    }
+#pragma unroll
+    for (int kb = 0; kb < kBlocks; ++kb) {
+        const float x = scattered_sum(sum[kb], lane);
+        if ((lane & 1) == 0) sums[wave][32 * kb + scattered_key(lane)] = x;
+    }
+    __syncthreads();
+    const int key = key0 + threadIdx.x;
+    if ((int)threadIdx.x < kKeys && key < s.len) {
+        float x = sums[0][threadIdx.x];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) x += sums[i][threadIdx.x];
+        const size_t at = ((size_t)b * v.g + kv) * a.w_stride + key;
+        if (a.w_in && key < s.old) x = fmaf(a.decay, a.w_in[at], x);
+        a.w_out[at] = x;
+    }
+}
+
 // Few rows, many keys: a block keeps up to 64 KB of a unit's rows in shared memory, and each of its waves walks a run of the unit's keys past them, the
 // next 32 keys' rows on their way to registers meanwhile.  More rows than that take another turn over the run, which adds to what the last one wrote.
 template <typename T, int OPT> __global__ __launch_bounds__(256, 2) void weights_few_kernel(WeightArgs a)
@@ -968,28 +1038,46 @@ template <typename T, int OPT> __global__ __launch_bounds__(256, 2) void weights
     int r0 = 0;
     do {
         const int have = min(rows - r0, kRows), blocks = (have + 31) / 32;
+        // the tiles of the run that some of the rows see; the others' weights only decay
+        const int tok0 = r0 >> v.lg, tok1 = (r0 + max(have, 1) - 1) >> v.lg;
+        const int hi = have > 0 ? key_range(s, prefix, tok0, tok1).hi : 0;
+        int lo = 0;
+        if (a.o.first && have > 0) {
+            lo = INT32_MAX;
+            for (int i = tok0 + lane; i <= tok1; i += 64) lo = min(lo, max(a.o.first[s.c0 + i], 0));
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) lo = min(lo, __shfl_xor(lo, d));
+            lo = __builtin_amdgcn_readfirstlane(lo);
+        }
+        const int s0 = max(t0, min(lo >> 5, t1)), s1 = max(s0, min(t1, (hi + 31) >> 5));
+        Operand<T> k[1];
+        uint32_t bad_now = 0;
+        if (s0 < s1) {
+            load_operand(k[0], (const T *)a.k_pages + (int64_t)rows_of(s0) * 128, half);
+            bad_now = bad;
+        }
         __syncthreads();
         for (int j = wave; j * kPer < have; j += 4) {
             const int r = j * kPer + lane / RowTile<T>::kChunks, c = (lane % RowTile<T>::kChunks) ^ swz<T>(r), row = r0 + min(r, have - 1);
             row_to_lds(lds0 + j * kPer * RowTile<T>::kRowBytes,
                        (const char *)((const T *)a.q + (int64_t)(s.c0 + (row >> v.lg)) * a.q_stride + ((kv << v.lg) + (row & ((1 << v.lg) - 1))) * 128) + 16 * c);
         }
-        Operand<T> k[1];
-        uint32_t bad_now = 0;
-        if (t0 < t1) {
-            load_operand(k[0], (const T *)a.k_pages + (int64_t)rows_of(t0) * 128, half);
-            bad_now = bad;
-        }
         for (int r = threadIdx.x; r < 32 * blocks; r += 256) part[r] = weight_row<OPT>(a, s, prefix, kv, r0 + r, rows);
+        auto before_of = [&](int key) {
+            if (r0 > 0) return key < s.len ? a.w_out[w0 + key] : 0.0f;
+            return a.w_in && key < min(s.old, s.len) ? a.decay * a.w_in[w0 + key] : 0.0f;
+        };
+        if (r0 == 0) {
+            for (int key = t0 * 32 + lane; key < min(s0 * 32, s.len); key += 64) a.w_out[w0 + key] = before_of(key);
+            for (int key = s1 * 32 + lane; key < min(t1 * 32, s.len); key += 64) a.w_out[w0 + key] = before_of(key);
+        }
         loads_landed<0>();
         __syncthreads();
-        for (int t = t0; t < t1; ++t) {
+        for (int t = s0; t < s1; ++t) {
             const int key = t * 32 + mine;
-            float before = 0.0f;
-            if (r0 > 0) before = key < s.len ? a.w_out[w0 + key] : 0.0f;
-            else if (a.w_in && key < min(s.old, s.len)) before = a.decay * a.w_in[w0 + key];
+            const float before = before_of(key);
             Operand<T> next;
-            if (sizeof(T) == 2 && t + 1 < t1) load_operand(next, (const T *)a.k_pages + (int64_t)rows_of(t + 1) * 128, half);
+            if (sizeof(T) == 2 && t + 1 < s1) load_operand(next, (const T *)a.k_pages + (int64_t)rows_of(t + 1) * 128, half);
             const uint32_t bad_next = bad;
             f32x16_t sum[1] = {};
             for (int rb = 0; rb < blocks; ++rb) {
@@ -997,7 +1085,7 @@ template <typename T, int OPT> __global__ __launch_bounds__(256, 2) void weights
                 tile_operand(q, smem, 32 * rb + (lane & 31), half);
                 add_weights<T, OPT, 1>(sum, k, q, part[32 * rb + (lane & 31)], a.o, t * 32, bad_now, half);
             }
-            if (sizeof(T) == 4 && t + 1 < t1) load_operand(k[0], (const T *)a.k_pages + (int64_t)rows_of(t + 1) * 128, half);
+            if (sizeof(T) == 4 && t + 1 < s1) load_operand(k[0], (const T *)a.k_pages + (int64_t)rows_of(t + 1) * 128, half);
             const float x = scattered_sum(sum[0], lane);
             if ((lane & 1) == 0 && key < s.len) a.w_out[w0 + key] = x + before;
             if constexpr (sizeof(T) == 2) {
@@ -1233,7 +1321,14 @@ template <int EACH> __global__ __launch_bounds__(1024) void evict_select_kernel(
             for (int i = 0; i < EACH; ++i)
                 if (64 * i < mine) f(rank[i], my0 + 64 * i + lane);
         } else {
-            for (int i = 0; i < mine; i += 64) f(i + lane < mine ? weight_rank(w[my0 + i + lane]) : 0u, my0 + i + lane);
+            for (int i0 = 0; i0 < mine; i0 += 512) {   // (eight loads in flight)
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = w[my0 + min(i0 + 64 * i + lane, mine - 1)];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i0 + 64 * i < mine) f(i0 + 64 * i + lane < mine ? weight_rank(x[i]) : 0u, my0 + i0 + 64 * i + lane);
+            }
         }
     };
     const uint32_t way = lane & 3;
@@ -1353,38 +1448,41 @@ template <typename T> __global__ __launch_bounds__(1024) void evict_move_kernel(
     char *pages = (char *)(piece < kPieces / 2 ? a.k_pages : a.v_pages) + 16 * (piece % (kPieces / 2));
     const int32_t *table = v.table + (size_t)b * v.max_pages;
     const int in_page = (1 << v.page_shift) - 1;
-    for (int j0 = 0; j0 < keep; j0 += lane_rows * kEach) {
+    const int round = lane_rows * kEach;
+    uint32_t src[kEach], dst[kEach];
+    // where the rows of the round from j0 on come from and go to
+    auto look_up = [&](int j0) {
         int id[kEach];
-        uint32_t src[kEach], dst[kEach];
-        u32x4_t x[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) id[i] = ids[min(j0 + i * lane_rows + my, keep - 1)];
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int j = j0 + i * lane_rows + my;
-            id[i] = j < keep ? ids[j] : 0;
-        }
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int j = min(j0 + i * lane_rows + my, keep - 1);
             src[i] = (uint32_t)table[id[i] >> v.page_shift];
-            dst[i] = (uint32_t)table[j >> v.page_shift];
+            dst[i] = (uint32_t)table[min(j0 + i * lane_rows + my, keep - 1) >> v.page_shift];
         }
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int j = j0 + i * lane_rows + my;
             const bool move = j < keep && id[i] != j && src[i] < v.num_pages && dst[i] < v.num_pages;
-            if (move) {
-                const uint32_t from = (uint32_t)((src[i] * (uint64_t)v.g + kv) << v.page_shift) + (id[i] & in_page);
-                dst[i] = (uint32_t)((dst[i] * (uint64_t)v.g + kv) << v.page_shift) + (j & in_page);
-                x[i] = *reinterpret_cast<const u32x4_t *>(pages + (int64_t)from * (128 * (int)sizeof(T)));
-            } else {
-                dst[i] = kNoRow;
-            }
+            src[i] = (uint32_t)((src[i] * (uint64_t)v.g + kv) << v.page_shift) + (id[i] & in_page);
+            dst[i] = move ? (uint32_t)((dst[i] * (uint64_t)v.g + kv) << v.page_shift) + (j & in_page) : kNoRow;
         }
+    };
+    look_up(0);
+    for (int j0 = 0; j0 < keep; j0 += round) {
+        u32x4_t x[kEach];
+        uint32_t to[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            to[i] = dst[i];
+            if (to[i] != kNoRow) x[i] = *reinterpret_cast<const u32x4_t *>(pages + (int64_t)src[i] * (128 * (int)sizeof(T)));
+        }
+        if (j0 + round < keep) look_up(j0 + round);   // in the shadow of the rows
         loads_landed<0>();
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
-            if (dst[i] != kNoRow) *reinterpret_cast<u32x4_t *>(pages + (int64_t)dst[i] * (128 * (int)sizeof(T))) = x[i];
+            if (to[i] != kNoRow) *reinterpret_cast<u32x4_t *>(pages + (int64_t)to[i] * (128 * (int)sizeof(T))) = x[i];
     }
     if (weights)
         for (int j0 = 0; j0 < keep; j0 += 1024) {
