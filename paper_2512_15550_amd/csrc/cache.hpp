@@ -804,7 +804,10 @@ template <int OPT> __device__ __forceinline__ WeightRow weight_row(const WeightA
     const float lse = a.lse[(size_t)(s.c0 + token) * a.v.h + head];
     w.nlse = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
     w.slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
-    if (row >= rows) w.sight.hi = 0;
+    if (row >= rows) {
+        w.sight.hi = 0;
+        w.nlse = -INFINITY;
+    }
     return w;
 }
 // sum += the probabilities of 32 NB keys from k0 on (their operands: k) under the lane's row (q)
@@ -841,6 +844,20 @@ template <typename T, int OPT, int NB> __device__ __forceinline__ void add_weigh
     for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sum[kb][i] += sc[kb][i];
+}
+// The same for bf16 rows that all see all of the 32 keys, in two parts, so that the matrix cores can have the next rows while the vector units have these
+__device__ __forceinline__ f32x16_t keys_dot(const Operand<bf16_t> &k, const Operand<bf16_t> &q)
+{
+    f32x16_t sc = {};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.c[i], q.c[i], sc, 0, 0, 0);
+    return sc;
+}
+template <int OPT> __device__ __forceinline__ void add_seen(f32x16_t &sum, f32x16_t sc, const WeightRow &w, const ScoreOpts &o, int k0, int half)
+{
+    score_regs<OPT>(sc, o, w.slope2, w.sight.pos - k0, half);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[i] += exp2_fast(OPT == 0 ? fmaf(sc[i], o.c2, w.nlse) : sc[i] + w.nlse);
 }
 // a row of a tile in shared memory as the second operand
 template <typename T> __device__ __forceinline__ void tile_operand(Operand<T> &q, const char *tile, int r, int half)
@@ -1049,6 +1066,7 @@ template <typename T, int OPT> __global__ __launch_bounds__(256, 2) void weights
             for (int d = 1; d < 64; d <<= 1) lo = min(lo, __shfl_xor(lo, d));
             lo = __builtin_amdgcn_readfirstlane(lo);
         }
+        const int all_hi = have > 0 ? key_range(s, prefix, tok0, tok1).all_hi : 0;
         const int s0 = max(t0, min(lo >> 5, t1)), s1 = max(s0, min(t1, (hi + 31) >> 5));
         Operand<T> k[1];
         uint32_t bad_now = 0;
@@ -1057,7 +1075,7 @@ template <typename T, int OPT> __global__ __launch_bounds__(256, 2) void weights
             bad_now = bad;
         }
         __syncthreads();
-        for (int j = wave; j * kPer < have; j += 4) {
+        for (int j = wave; j * kPer < 32 * blocks; j += 4) {   // (the last row again where they end)
             const int r = j * kPer + lane / RowTile<T>::kChunks, c = (lane % RowTile<T>::kChunks) ^ swz<T>(r), row = r0 + min(r, have - 1);
             row_to_lds(lds0 + j * kPer * RowTile<T>::kRowBytes,
                        (const char *)((const T *)a.q + (int64_t)(s.c0 + (row >> v.lg)) * a.q_stride + ((kv << v.lg) + (row & ((1 << v.lg) - 1))) * 128) + 16 * c);
@@ -1080,6 +1098,21 @@ template <typename T, int OPT> __global__ __launch_bounds__(256, 2) void weights
             if (sizeof(T) == 2 && t + 1 < s1) load_operand(next, (const T *)a.k_pages + (int64_t)rows_of(t + 1) * 128, half);
             const uint32_t bad_next = bad;
             f32x16_t sum[1] = {};
+            if (sizeof(T) == 2 && !a.o.first && t * 32 + 32 <= all_hi && bad_now == 0) {
+                if constexpr (sizeof(T) == 2) {
+                    Operand<T> q;
+                    tile_operand(q, smem, lane & 31, half);
+                    f32x16_t sc = keys_dot(k[0], q);
+                    for (int rb = 0; rb + 1 < blocks; ++rb) {
+                        tile_operand(q, smem, 32 * (rb + 1) + (lane & 31), half);
+                        const WeightRow w = part[32 * rb + (lane & 31)];
+                        const f32x16_t ahead = keys_dot(k[0], q);
+                        add_seen<OPT>(sum[0], sc, w, a.o, t * 32, half);
+                        sc = ahead;
+                    }
+                    add_seen<OPT>(sum[0], sc, part[32 * (blocks - 1) + (lane & 31)], a.o, t * 32, half);
+                }
+            } else
             for (int rb = 0; rb < blocks; ++rb) {
                 Operand<T> q;
                 tile_operand(q, smem, 32 * rb + (lane & 31), half);
