@@ -245,8 +245,9 @@ typedef struct {
     const uint8_t *rope_axis;    /* HOST [head_dim / 2] or NULL (all 0): the axis, 0 to 2, that turns each pair */
 } ctkvr_cache_params;
 
-/* A handle on the current device; params' arrays are copied.  Errors: EINVAL, EUNSUPPORTED (as the index), ENOMEM. */
-int ctkvr_cache_create(const ctkvr_cache_params *p, ctkvr_cache **out_cache);
+/* A handle on the current device; params' arrays are copied.  Clears words of its workspace on hip_stream and synchronises it.
+ * Errors: EINVAL, EUNSUPPORTED (as the index; a sequence of more than 2^20 tokens, a cache of 2^32 rows), ENOMEM. */
+int ctkvr_cache_create(const ctkvr_cache_params *p, void *hip_stream, ctkvr_cache **out_cache);
 /* Release a handle (NULL is allowed); synchronises its device first, as ctkvr_free does. */
 void ctkvr_cache_free(ctkvr_cache *c);
 

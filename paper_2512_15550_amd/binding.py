@@ -150,7 +150,7 @@ def load_library() -> ctypes.CDLL:
     L.ctkvr_selftest_exp.argtypes = [ctypes.POINTER(ctypes.c_uint64), vp]
     i32, i64, f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
     L.ctkvr_cache_create.restype = ctypes.c_int
-    L.ctkvr_cache_create.argtypes = [ctypes.POINTER(_CCacheParams), ctypes.POINTER(ctypes.c_void_p)]
+    L.ctkvr_cache_create.argtypes = [ctypes.POINTER(_CCacheParams), vp, ctypes.POINTER(ctypes.c_void_p)]
     L.ctkvr_cache_free.restype = None
     L.ctkvr_cache_free.argtypes = [vp]
     L.ctkvr_cache_append.restype = ctypes.c_int
@@ -483,7 +483,7 @@ def ctkvr_cache_create(params: CacheParams) -> Cache:
                        params.num_pages, params.max_pages, params.max_new, float(params.sm_scale), float(params.softcap),
                        float(params.rope_base), None if freq is None else freq.ctypes.data, None if axis is None else axis.ctypes.data)
     out = ctypes.c_void_p()
-    _check(L.ctkvr_cache_create(ctypes.byref(cp), ctypes.byref(out)))
+    _check(L.ctkvr_cache_create(ctypes.byref(cp), _stream(), ctypes.byref(out)))
     return Cache(out.value, params, torch.cuda.current_device())
 
 

@@ -160,6 +160,12 @@ template <int OPT> __device__ __forceinline__ void score_regs(f32x16_t &s, const
     }
 }
 
+__global__ void cache_clear_kernel(uint32_t *p, size_t n)
+{
+    const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i < n) p[i] = 0;
+}
+
 // ---- attention of new tokens --------------------------------------------------------------------------
 struct AttnArgs {
     CacheView v;
@@ -169,8 +175,11 @@ struct AttnArgs {
     const void *k_pages, *v_pages;
     void *out;                 // [total][h][128]
     float *lse;                // [total][h] or null
-    float *part_o, *part_lse;  // [nsplit][total][h][128] and [nsplit][total][h], where keys are split
-    int tiles, nsplit;
+    int tiles;
+    // attn_few_kernel, where keys are split into runs: [nsplit][total][h][128] and [nsplit][total][h], and how many of a tile's runs are done
+    float *part_o, *part_lse;
+    uint32_t *done;            // [tiles][g], zero between calls; null: attn_join_kernel joins the runs
+    int nsplit;
 };
 
 // A key that a row does not see has probability 0 there, but 0 times an infinity or NaN is no 0.  So where a tile has such keys for some row, values
@@ -340,11 +349,29 @@ template <typename T> __device__ __forceinline__ void store4(T *p, const f32x4_t
         *reinterpret_cast<f32x4_t *>(p) = x;
     }
 }
+// What blocks of a launch hand to each other goes past the caches that they do not share, word by word: a fence, which would write back and invalidate a whole L2
+// for each of them, made a step of 16 sequences take 770 us in place of 440.
+__device__ __forceinline__ void hand_over(float *p, const f32x4_t &x)
+{
+    union { f32x4_t f; unsigned long long w[2]; } u{x};
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        __hip_atomic_store(reinterpret_cast<unsigned long long *>(p) + i, u.w[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void hand_over(float *p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ f32x4_t handed4(const float *p)
+{
+    union { f32x4_t f; unsigned long long w[2]; } u;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        u.w[i] = __hip_atomic_load(reinterpret_cast<const unsigned long long *>(p) + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return u.f;
+}
+__device__ __forceinline__ float handed(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ float inv_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }   // (NaN stays)
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2; }
 
-// One block a tile of 32 NW rows of a unit and, where the keys are split, one of nsplit runs of their tiles; a wave has 32 rows.  Each
-// tile of keys goes straight to shared memory while the one before it is worked on; the maximum runs with them.
+// Many rows: one block a tile of 32 NW rows of a unit; a wave has 32 rows.  Each tile of keys goes straight to shared memory while the one before it is worked on; the maximum runs with them.
 template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void attn_kernel(AttnArgs a)
 {
     constexpr int kRowsLog = NW == 4 ? 7 : 8, kKeys = RowTile<T>::kRows, kBlocks = kKeys / 32, kTile = RowTile<T>::kBytes;
@@ -355,9 +382,9 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
     const CacheView &v = a.v;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     // (a KV head's tiles stay on an XCD where the heads are a multiple of 8; the tiles with most keys go first)
-    const int kv = blockIdx.x % v.g, rest = blockIdx.x / v.g, split = rest % a.nsplit;
+    const int kv = blockIdx.x % v.g;
     int b, at;
-    if (!locate_tile<kRowsLog>(v, a.tiles - 1 - rest / a.nsplit, &b, &at)) return;
+    if (!locate_tile<kRowsLog>(v, a.tiles - 1 - (int)(blockIdx.x / v.g), &b, &at)) return;
     const SeqSpan s = seq_span(v, b);
     const int rows = s.n << v.lg, r0 = at << kRowsLog, row = r0 + 32 * wave + (lane & 31);
     const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
@@ -392,11 +419,6 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
         __syncthreads();
     }
     int t0 = k_lo / kKeys, t1 = range.hi > k_lo ? (range.hi + kKeys - 1) / kKeys : t0;
-    if (a.nsplit > 1) {   // this block's run of them
-        const int n = t1 - t0, from = (int)((int64_t)n * split / a.nsplit), to = (int)((int64_t)n * (split + 1) / a.nsplit);
-        t1 = t0 + to;
-        t0 += from;
-    }
     t0 = __builtin_amdgcn_readfirstlane(t0);
     t1 = __builtin_amdgcn_readfirstlane(t1);
 
@@ -508,12 +530,7 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
     if (row >= rows) return;
     const float inv = inv_sum(l), lse = lse_of(m, l);
     const size_t at_row = (size_t)(s.c0 + token) * v.h + head;
-    const size_t n = (size_t)split * v.total * v.h + at_row;
-    if (half == 0) {
-        if (a.nsplit > 1) a.part_lse[n] = lse;
-        else if (a.lse) a.lse[at_row] = lse;
-    }
-    if (a.nsplit > 1 && t0 == t1) return;
+    if (a.lse && half == 0) a.lse[at_row] = lse;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -522,12 +539,11 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
             f32x4_t x;
 #pragma unroll
             for (int c = 0; c < 4; ++c) x[c] = o[db][4 * i + c] * inv;
-            if (a.nsplit > 1) store4(a.part_o + n * 128 + d, x);
-            else store4((T *)a.out + at_row * 128 + d, x);
+            store4((T *)a.out + at_row * 128 + d, x);
         }
 }
 
-// Few rows, many keys: one block a tile of 32 rows and a run of their keys, which its waves share out, each with a maximum and outputs of its own until
+// Few rows: one block a tile of 32 rows and a run of their keys, which its waves share out, each with a maximum and outputs of its own until
 // they are joined at the end; no wave waits for another before that.  Keys go to registers as operands, values to shared memory, a tile of 32 ahead.
 template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void attn_few_kernel(AttnArgs a)
 {
@@ -535,11 +551,12 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
     using Odd = OddValues<T, 32, 64>;
     __shared__ __align__(16) char smem[NW][2][kTile];
     __shared__ float join[NW][2][32];
+    __shared__ bool last;
     const CacheView &v = a.v;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int kv = blockIdx.x % v.g, rest = blockIdx.x / v.g, split = rest % a.nsplit;
+    const int kv = blockIdx.x % v.g, rest = blockIdx.x / v.g, split = rest % a.nsplit, tile = a.tiles - 1 - rest / a.nsplit;
     int b, at;
-    if (!locate_tile<5>(v, a.tiles - 1 - rest / a.nsplit, &b, &at)) return;
+    if (!locate_tile<5>(v, tile, &b, &at)) return;
     const SeqSpan s = seq_span(v, b);
     const int rows = s.n << v.lg, r0 = at << 5, row = r0 + (lane & 31);
     const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
@@ -564,9 +581,10 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
     const int per = sizeof(T) == 2 ? 2 * NW : NW, used = max(1, min(a.nsplit, (tiles + per - 1) / per));
     auto row_out = [&](int r) { return (size_t)(s.c0 + ((r0 + r) >> v.lg)) * v.h + (kv << v.lg) + ((r0 + r) & ((1 << v.lg) - 1)); };
     if (split >= used) {
-        if ((int)threadIdx.x < have) a.part_lse[(size_t)split * v.total * v.h + row_out(threadIdx.x)] = -INFINITY;
+        if (!a.done && (int)threadIdx.x < have) a.part_lse[(size_t)split * v.total * v.h + row_out(threadIdx.x)] = -INFINITY;
         return;
     }
+    const bool whole = a.nsplit == 1 || (a.done && used == 1);   // this block's outputs are the rows'
     const int64_t runs = (int64_t)used * NW, run = split * NW + wave;
     const int t0 = __builtin_amdgcn_readfirstlane(first_tile + (int)(tiles * run / runs));
     const int t1 = __builtin_amdgcn_readfirstlane(first_tile + (int)(tiles * (run + 1) / runs));
@@ -697,13 +715,70 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
         x *= inv_sum(sum);
         const float lse = lse_of(t, sum);
         const size_t at_row = row_out(r);
-        if (a.nsplit > 1) {
+        if (!whole) {
             const size_t n = (size_t)split * v.total * v.h + at_row;
-            if (c == 0) a.part_lse[n] = lse;
-            store4(a.part_o + n * 128 + 4 * c, x);
+            if (a.done) {
+                if (c == 0) hand_over(a.part_lse + n, lse);
+                hand_over(a.part_o + n * 128 + 4 * c, x);
+            } else {
+                if (c == 0) a.part_lse[n] = lse;
+                store4(a.part_o + n * 128 + 4 * c, x);
+            }
         } else {
             if (c == 0 && a.lse) a.lse[at_row] = lse;
             store4((T *)a.out + at_row * 128 + 4 * c, x);
+        }
+    }
+    if (whole || !a.done) return;
+
+    // The run that ends last joins the tile's runs, in their order, by their log-sum-exps: 32 lanes a row, four elements a lane, and where the
+    // rows are few several such groups a row, that take the runs in turn.
+    loads_landed<0>();   // (stores too)
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        uint32_t *done = a.done + (size_t)tile * v.g + kv;
+        last = atomicAdd(done, 1u) == (uint32_t)used - 1;
+        if (last) *done = 0;
+    }
+    __syncthreads();
+    if (!last) return;
+    constexpr int kGroups = 2 * NW;
+    f32x4_t(*sums)[33] = reinterpret_cast<f32x4_t(*)[33]>(smem);   // [group][lane, or the weights' sum]
+    int ways = kGroups;
+    while (ways > 1 && ways * have > kGroups) ways >>= 1;
+    const int group = threadIdx.x >> 5, l32 = threadIdx.x & 31, way = group % ways;
+    const size_t step = (size_t)v.total * v.h;
+    for (int base = 0; base < have; base += kGroups / ways) {
+        const int r = base + group / ways;
+        f32x4_t x = {};
+        float top_lse = -INFINITY, sum = 0.0f, ref = 0.0f;
+        if (r < have) {
+            const float *lses = a.part_lse + row_out(r), *outs = a.part_o + row_out(r) * 128 + 4 * l32;
+            for (int i = l32; i < used; i += 32) top_lse = fmaxf(top_lse, handed(lses + i * step));
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) top_lse = fmaxf(top_lse, __shfl_xor(top_lse, d));
+            ref = top_lse == -INFINITY ? 0.0f : top_lse;
+#pragma unroll 8
+            for (int i = way; i < used; i += ways) {
+                const float w = exp2_fast((handed(lses + i * step) - ref) * kLog2e);
+                sum += w;
+                x += handed4(outs + i * step * 128) * w;
+            }
+        }
+        if (ways > 1) {
+            sums[group][l32] = x;
+            if (l32 == 0) sums[group][32][0] = sum;
+            __syncthreads();
+            if (way == 0)
+                for (int w = 1; w < ways; ++w) {
+                    x += sums[group + w][l32];
+                    sum += sums[group + w][32][0];
+                }
+            __syncthreads();
+        }
+        if (r < have && way == 0) {
+            if (l32 == 0 && a.lse) a.lse[row_out(r)] = sum == 0.0f ? -INFINITY : ref + __builtin_amdgcn_logf(sum) * kLn2;
+            store4((T *)a.out + row_out(r) * 128 + 4 * l32, x * inv_sum(sum));
         }
     }
 }

@@ -25,7 +25,7 @@ class Host:
         p.update(over)
         cp = _CCacheParams(rope_freq=None if freq is None else freq.ctypes.data, rope_axis=None if axis is None else axis.ctypes.data, **p)
         out = ctypes.c_void_p(1)
-        rc = self.lib.ctkvr_cache_create(ctypes.byref(cp), ctypes.byref(out))
+        rc = self.lib.ctkvr_cache_create(ctypes.byref(cp), None, ctypes.byref(out))
         assert rc == expect, (over, rc, ck.ctkvr_last_error())
         assert (out.value is not None) == (rc == OK) and (rc == OK or ck.ctkvr_last_error())
         return out.value
@@ -74,7 +74,7 @@ def parameters(x):
     axis = np.zeros(64, np.uint8)
     axis[5] = 3
     x.create(expect=EINVAL, axis=axis)
-    assert x.lib.ctkvr_cache_create(None, ctypes.byref(ctypes.c_void_p())) == EINVAL and x.lib.ctkvr_cache_create(None, None) == EINVAL
+    assert x.lib.ctkvr_cache_create(None, None, ctypes.byref(ctypes.c_void_p())) == EINVAL and x.lib.ctkvr_cache_create(None, None, None) == EINVAL
     x.lib.ctkvr_cache_free(None)
     for fn in (x.append, x.attn, x.weights, x.evict):
         fn(None, expect=EINVAL)
