@@ -100,6 +100,8 @@ ScoreOpts score_opts(const ctkvr_cache *c, const float *slopes, const int32_t *p
     if (c->p.softcap > 0.0f) {
         o.cap_in = c->scale / c->p.softcap;
         o.cap_out = c->p.softcap * kLog2e;
+        o.cap_105 = o.cap_out * 105.0f;
+        o.cap_945 = o.cap_out * 945.0f;
     }
     return o;
 }
@@ -117,10 +119,14 @@ int check_rows(const ctkvr_cache *c, const char *name, const void *p, int64_t st
     return CTKVR_OK;
 }
 
-// How a call's rows and keys fall into blocks.  Tiles of 128 rows read a key once for all of them; where they are too few for the chip, or most of their
-// rows would be empty, tiles of 32 rows whose keys a block's waves share out, and where those leave CUs idle, several blocks, each a run of the keys: a block
-// a CU for one sequence in bf16, two in fp32 (500 tokens on 2 KV heads 36 -> 27 us), more for several, whose lengths differ.
-// The runs' outputs are joined by the block that ends last where it has little to read, by a launch of its own otherwise.  One token of 32 heads on 32K keys 31.6
+// How a call's rows and keys fall into blocks.
+//   Tiles of 128 rows read a key once for all of them; tiles of 32, whose keys a block's waves share out, where 128 would be mostly empty (64 rows a unit), and
+// where those would leave CUs without a block, unless the keys are many and the rows are too: 574 tokens of 8 heads a KV head on 13K keys 67 us with 128 rows a block
+// and the keys split, 101 with 32; but up to 122 tokens of 4 heads 45 and 30, and in fp32, where a row more is a row's products more, 42 tokens 64 and 31.
+//   Keys are split into runs where blocks would be too few: to a block a CU for one sequence in bf16, two in fp32 (500 tokens on 2 KV heads 36 -> 27 us), eight for
+// several, whose lengths differ.  A run has 256 keys at least, 64 in fp32, but 2048 where a unit has several tiles and they fill half the chip by
+// themselves: 93 tokens on 520 keys, two sequences, 23 us in three runs and 17 in one.
+//   The runs' outputs are joined by the block that ends last where it has little to read, by a launch of its own otherwise.  One token of 32 heads on 32K keys 31.6
 // and 32.6 us, and 6.6 and 10.4 where a document leaves one run; but 29 tokens on 856 keys 19.2 and 14.3, 2 tokens of 8 heads a KV head on 3769 keys in fp32 40 and 22,
 // one token of 13 sequences 33.0 and 31.1.
 struct AttnPlan {
@@ -133,15 +139,13 @@ AttnPlan attn_plan(const ctkvr_cache *c, int total)
     const int used = std::min(total, c->p.batch);   // sequences with new tokens, at most
     const bool bf16 = c->p.dtype == CTKVR_BF16;
     AttnPlan p{};
-    const int64_t wide = (rows >> 7) + used;
-    p.few = rows <= 64ll * used || wide * g < cus;
-    p.tiles = (int)(p.few ? (rows >> 5) + used : wide);
-    p.nsplit = 1;
-    if (p.few) {
-        const int64_t want = (used > 1 ? 8 : bf16 ? 1 : 2) * cus, least = bf16 ? 256 : 64;   // blocks; keys of a run
-        p.nsplit = (int)std::max<int64_t>(1, std::min({want / (p.tiles * g), (keys + least - 1) / least, (int64_t)kMaxSplit}));
-        p.join_inside = used == 1 && rows <= 8 && rows * p.nsplit <= (bf16 ? 256 : 128);
-    }
+    const int64_t wide = (rows >> 7) + used, narrow = (rows >> 5) + used;
+    p.few = rows <= 64ll * used || (wide * g < cus && (!bf16 || keys < 4096 || rows < 512ll * used));
+    p.tiles = (int)(p.few ? narrow : wide);
+    const bool enough = narrow >= 2 * used && narrow * g >= cus / 2;
+    const int64_t want = (!p.few ? 2 : used > 1 ? 8 : bf16 ? 1 : 2) * cus, least = !p.few ? 1024 : enough ? 2048 : bf16 ? 256 : 64;
+    p.nsplit = p.few || wide * g < cus ? (int)std::max<int64_t>(1, std::min({want / (p.tiles * g), (keys + least - 1) / least, (int64_t)kMaxSplit})) : 1;
+    p.join_inside = p.few && used == 1 && rows <= 8 && rows * p.nsplit <= (bf16 ? 256 : 128);
     return p;
 }
 
@@ -294,10 +298,7 @@ int ctkvr_cache_append(ctkvr_cache *c, const void *q, int64_t q_stride, const vo
     a.q_out = q_out;
     a.k_pages = k_pages;
     a.v_pages = v_pages;
-    const int rows = (q ? c->p.n_q_heads : 0) + (k ? 2 * c->p.n_kv_heads : 0);
-    a.parts = 1;
-    const unsigned grid = (unsigned)(((int64_t)total * a.parts + 3) / 4);
-    (void)rows;
+    const unsigned grid = (unsigned)((total + 3) / 4);
     if (c->p.dtype == CTKVR_BF16) append_kernel<bf16_t><<<dim3(grid), 256, 0, (hipStream_t)hip_stream>>>(a);
     else append_kernel<float><<<dim3(grid), 256, 0, (hipStream_t)hip_stream>>>(a);
     return launched("ctkvr_cache_append");

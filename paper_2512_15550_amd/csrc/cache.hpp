@@ -133,7 +133,7 @@ template <typename T> __device__ __forceinline__ f32x16_t rows_dot(const char *t
     return acc;
 }
 
-// tanh(x): a continued fraction's fifth convergent below 0.6 (off by 1e-9 of it), (1 - e) / (1 + e) with e = exp(-2 x) above, where that loses nothing
+// tanh(x): the continued fraction's fifth convergent below 0.6 (off by 1e-9 of it), (1 - e) / (1 + e) with e = exp(-2 x) above, where that loses nothing
 __device__ __forceinline__ float tanh_f(float x)
 {
     const float a = fabsf(x), y = x * x;
@@ -150,10 +150,27 @@ constexpr int kCap = 1, kBias = 2;
 template <int OPT> __device__ __forceinline__ void score_regs(f32x16_t &s, const ScoreOpts &o, float slope2, int pos_minus_key0, int half)
 {
     if constexpr (OPT != 0) {
+        if constexpr ((OPT & kCap) != 0) {
+            // Scores within the cap, as they are as a rule: the fifth convergent alone, off by 1e-7 of it at the cap, is half the instructions
+            float big = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) big = fmaxf(big, fabsf(s[i]));
+            if (__any(big * o.cap_in > 1.0f)) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = o.cap_out * tanh_f(s[i] * o.cap_in);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float x = s[i] * o.cap_in, y = x * x;
+                    const float n = x * fmaf(y, fmaf(y, o.cap_out, o.cap_105), o.cap_945), d = fmaf(y, fmaf(y, 15.0f, 420.0f), 945.0f);
+                    s[i] = n * __builtin_amdgcn_rcpf(d);
+                }
+            }
+        }
         const float far = (float)(pos_minus_key0 - 4 * half);   // (distances below 2^24 are exact)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            float z = (OPT & kCap) ? o.cap_out * tanh_f(s[i] * o.cap_in) : s[i] * o.c2;
+            float z = (OPT & kCap) ? s[i] : s[i] * o.c2;
             if constexpr ((OPT & kBias) != 0) z = fmaf(-slope2, fabsf(far - (float)(8 * (i >> 2) + (i & 3))), z);
             s[i] = z;
         }
@@ -176,7 +193,7 @@ struct AttnArgs {
     void *out;                 // [total][h][128]
     float *lse;                // [total][h] or null
     int tiles;
-    // attn_few_kernel, where keys are split into runs: [nsplit][total][h][128] and [nsplit][total][h], and how many of a tile's runs are done
+    // where keys are split into runs: [nsplit][total][h][128] and [nsplit][total][h]; how many of a tile's runs are done
     float *part_o, *part_lse;
     uint32_t *done;            // [tiles][g], zero between calls; null: attn_join_kernel joins the runs
     int nsplit;
@@ -370,7 +387,7 @@ __device__ __forceinline__ float handed(const float *p) { return __hip_atomic_lo
 __device__ __forceinline__ float inv_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }   // (NaN stays)
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2; }
 
-// Many rows: one block a tile of 32 NW rows of a unit; a wave has 32 rows.  Each tile of keys goes straight to shared memory while the one before it is worked on; the maximum runs with them.
+// Many rows: one block a tile of 32 NW rows of a unit and, where the keys are split, one of nsplit runs of them; a wave has 32 rows.  Each tile of keys goes straight to shared memory while the one before it is worked on; the maximum runs with them.
 template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void attn_kernel(AttnArgs a)
 {
     constexpr int kRowsLog = NW == 4 ? 7 : 8, kKeys = RowTile<T>::kRows, kBlocks = kKeys / 32, kTile = RowTile<T>::kBytes;
@@ -381,9 +398,9 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
     const CacheView &v = a.v;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     // (a KV head's tiles stay on an XCD where the heads are a multiple of 8; the tiles with most keys go first)
-    const int kv = blockIdx.x % v.g;
+    const int kv = blockIdx.x % v.g, rest = blockIdx.x / v.g, split = rest % a.nsplit;
     int b, at;
-    if (!locate_tile<kRowsLog>(v, a.tiles - 1 - (int)(blockIdx.x / v.g), &b, &at)) return;
+    if (!locate_tile<kRowsLog>(v, a.tiles - 1 - rest / a.nsplit, &b, &at)) return;
     const SeqSpan s = seq_span(v, b);
     const int rows = s.n << v.lg, r0 = at << kRowsLog, row = r0 + 32 * wave + (lane & 31);
     const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
@@ -418,6 +435,12 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
         __syncthreads();
     }
     int t0 = k_lo / kKeys, t1 = range.hi > k_lo ? (range.hi + kKeys - 1) / kKeys : t0;
+    if (a.nsplit > 1) {   // this block's run of them: as many runs as there are eight tiles for
+        const int n = t1 - t0, used = max(1, min(a.nsplit, n / 8)), at_run = min(split, used);
+        const int from = (int)((int64_t)n * at_run / used), to = (int)((int64_t)n * min(at_run + 1, used) / used);
+        t1 = t0 + to;
+        t0 += from;
+    }
     t0 = __builtin_amdgcn_readfirstlane(t0);
     t1 = __builtin_amdgcn_readfirstlane(t1);
 
@@ -529,7 +552,12 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
     if (row >= rows) return;
     const float inv = inv_sum(l), lse = lse_of(m, l);
     const size_t at_row = (size_t)(s.c0 + token) * v.h + head;
-    if (a.lse && half == 0) a.lse[at_row] = lse;
+    const size_t n = (size_t)split * v.total * v.h + at_row;
+    if (half == 0) {
+        if (a.nsplit > 1) a.part_lse[n] = lse;
+        else if (a.lse) a.lse[at_row] = lse;
+    }
+    if (a.nsplit > 1 && t0 == t1) return;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -538,7 +566,8 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
             f32x4_t x;
 #pragma unroll
             for (int c = 0; c < 4; ++c) x[c] = o[db][4 * i + c] * inv;
-            store4((T *)a.out + at_row * 128 + d, x);
+            if (a.nsplit > 1) store4(a.part_o + n * 128 + d, x);
+            else store4((T *)a.out + at_row * 128 + d, x);
         }
 }
 
@@ -1220,7 +1249,6 @@ struct AppendArgs {
     int64_t q_stride, k_stride, v_stride;
     const int32_t *positions;   // [axes][total] or null: the token's place in the cache on every axis
     void *q_out, *k_pages, *v_pages;
-    int parts;                  // blocks a token's rows are shared out over
 };
 
 // sine and cosine of u / 2^32 turns: an eighth of a turn either side of a quarter, by their series (off by 2e-9)
@@ -1255,14 +1283,13 @@ __device__ __forceinline__ void store_chunk(bf16_t *p, const float (&x)[8])
     *reinterpret_cast<bf16x8_t *>(p) = v;
 }
 
-// A wave has a token (or one of `parts` shares of its rows): lane i turns pair i's angle into sine and cosine, once for all heads, then 8 lanes
-// take a row, the chunks i and i + 8 of 8 elements each.
+// A wave has a token: lane i turns pair i's angle into sine and cosine, once for all heads, then 8 lanes take a row, the chunks i and i + 8 of 8
+// elements each.
 template <typename T> __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
 {
     __shared__ float2 turn[4][64];
     const CacheView &v = a.v;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, unit = blockIdx.x * 4 + wave;
-    const int token = unit / a.parts, part = unit % a.parts;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, token = blockIdx.x * 4 + wave;
     if (token >= v.total) return;
     // the token's sequence: the last one that begins at or before it
     int b = -1;
@@ -1294,12 +1321,12 @@ template <typename T> __global__ __launch_bounds__(256) void append_kernel(Appen
     const bool held = slot >= 0 && slot < s.len;
     uint32_t page = held ? (uint32_t)v.table[(size_t)b * v.max_pages + (slot >> v.page_shift)] : 0xffffffffu;
     const int nq = a.q ? v.h : 0, nk = a.k ? v.g : 0, rows = nq + 2 * nk;
-    for (int r = part * 8 + (lane >> 3); r < rows; r += 8 * a.parts) {
+    for (int r = lane >> 3; r < rows; r += 8) {
         const int kv = r - nq;
         const T *from = r < nq ? (const T *)a.q + (int64_t)token * a.q_stride + r * 128
                         : kv < nk ? (const T *)a.k + (int64_t)token * a.k_stride + kv * 128
                                   : (const T *)a.val + (int64_t)token * a.v_stride + (kv - nk) * 128;
-        const Chunk<T> lo = load_chunk(from, i8), hi = load_chunk(from, i8 + 8);
+        const Chunk<T> lo = load_chunk_nt(from, i8), hi = load_chunk_nt(from, i8 + 8);   // (read once: 8192 tokens 49 -> 41 us)
         T *to;
         if (r < nq) {
             to = (T *)a.q_out + ((size_t)token * v.h + r) * 128;

@@ -44,7 +44,7 @@ struct ScoreOpts {
     const int32_t *prefix;    // [batch] or null
     const int32_t *first;     // [total] or null
     float c2;                 // scale * log2 e
-    float cap_in, cap_out;    // scale / cap, cap * log2 e (cap != 0)
+    float cap_in, cap_out, cap_105, cap_945;   // scale / cap, cap * log2 e, the latter times 105 and 945 (cap != 0)
 };
 // What a row sees: keys from lo on, before hi
 struct RowSight {
