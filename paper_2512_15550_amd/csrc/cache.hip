@@ -238,6 +238,7 @@ int ctkvr_cache_create(const ctkvr_cache_params *p, void *hip_stream, ctkvr_cach
     size_t part_rows = 0, counts = 0;
     for (int total = 1; total <= p->max_new; ++total) {
         const AttnPlan plan = attn_plan(c, total);
+        if (plan.nsplit == 1 && (((int64_t)total << c->lg) >> 7) * p->n_kv_heads >= 8ll * c->num_cu) break;   // more tokens are never split again
         if (plan.nsplit == 1) continue;
         part_rows = std::max(part_rows, (size_t)plan.nsplit * total * p->n_q_heads);
         counts = std::max(counts, (size_t)plan.tiles * p->n_kv_heads);
