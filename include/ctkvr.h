@@ -238,8 +238,8 @@ typedef struct {
     int32_t num_pages;           /* pages in k_pages and in v_pages */
     int32_t max_pages;           /* columns of the block table; max_pages * page_size at most 2^20 */
     int32_t max_new;             /* new tokens of a call, at most (over all sequences) */
-    float   sm_scale;            /* factor of q.k; 0 => 1/sqrt(head_dim) */
-    float   softcap;             /* 0: none; else a score z becomes softcap * tanh(z / softcap) */
+    float   sm_scale;            /* factor of q.k, up to 1e15; 0 => 1/sqrt(head_dim) */
+    float   softcap;             /* 0: none; else 1e-6 to 1e15: a score z becomes softcap * tanh(z / softcap) */
     double  rope_base;           /* frequency of pair i: rope_base^(-2 i / head_dim) */
     const double *rope_freq;     /* HOST [head_dim / 2] or NULL: these frequencies (radians per position) instead */
     const uint8_t *rope_axis;    /* HOST [head_dim / 2] or NULL (all 0): the axis, 0 to 2, that turns each pair */

@@ -54,8 +54,9 @@ int check_cache_params(const ctkvr_cache_params *p)
         return fail(CTKVR_EUNSUPPORTED, "%d pages: a cache of 2^32 - 2 rows at most", p->num_pages);
     if ((((int64_t)p->max_pages * p->page_size + 127) / 128) * p->batch * p->n_kv_heads >= (1ll << 31))
         return fail(CTKVR_EUNSUPPORTED, "%d sequences of %d pages: too large a batch", p->batch, p->max_pages);
-    if (!(p->sm_scale >= 0.0f) || std::isinf(p->sm_scale)) return fail(CTKVR_EINVAL, "sm_scale must be finite and >= 0");
-    if (!(p->softcap >= 0.0f) || std::isinf(p->softcap)) return fail(CTKVR_EINVAL, "softcap must be finite and >= 0");
+    if (!(p->sm_scale >= 0.0f && p->sm_scale <= 1e15f)) return fail(CTKVR_EINVAL, "sm_scale must be 0 to 1e15");
+    // (so that its products with the scale and with the convergent's constants are finite)
+    if (!(p->softcap == 0.0f || (p->softcap >= 1e-6f && p->softcap <= 1e15f))) return fail(CTKVR_EINVAL, "softcap must be 0, or 1e-6 to 1e15");
     if (!p->rope_freq && !(p->rope_base > 0.0 && !std::isinf(p->rope_base))) return fail(CTKVR_EINVAL, "rope_base must be finite and > 0");
     for (int i = 0; i < 64; ++i) {
         if (p->rope_freq && !std::isfinite(p->rope_freq[i])) return fail(CTKVR_EINVAL, "rope_freq[%d] is not finite", i);

@@ -63,7 +63,7 @@ class Host:
 def parameters(x):
     for code, changes in ((EINVAL, (dict(batch=0), dict(n_q_heads=7), dict(n_kv_heads=0), dict(dtype=2), dict(num_pages=0), dict(max_pages=0),
                                     dict(max_new=0), dict(sm_scale=-1.0), dict(sm_scale=NAN), dict(sm_scale=INF), dict(softcap=-0.5), dict(softcap=NAN),
-                                    dict(softcap=INF), dict(rope_base=0.0), dict(rope_base=NAN), dict(rope_base=INF))),
+                                    dict(softcap=INF), dict(softcap=1e-7), dict(softcap=1e16), dict(sm_scale=1e16), dict(rope_base=0.0), dict(rope_base=NAN), dict(rope_base=INF))),
                           (EUNSUPPORTED, (dict(head_dim=64), dict(n_q_heads=6), dict(n_q_heads=32), dict(page_size=12), dict(page_size=512), dict(page_size=0),
                                           dict(max_pages=(1 << 16) + 1), dict(max_new=(1 << 20) + 1), dict(batch=(1 << 16) + 1)))):
         for over in changes:

@@ -262,6 +262,111 @@ def test_a_cache_beyond_32_bit_offsets():
         assert torch.equal(row, kn[t - 70, 0].cpu() if t >= 70 else st.v[int(st.table[0, t // page]), 0, t % page])
 
 
+# ---- forms of the kernels that larger calls take: rows of 128 a block, keys split or not, rows past the keys ----------------
+def many(seed, dtype, h=32, g=8, page=16, q_scale=1.5):
+    """16 sequences with enough new tokens that rows are taken 128 at a time and, for the weights, past the keys."""
+    r = np.random.RandomState(seed)
+    lens = [int(x) for x in r.randint(150, 420, size=16)]
+    new = [min(s, int(x)) for s, x in zip(lens, r.randint(140, 190, size=16))]
+    lens[3], new[3] = 64, 64
+    lens[5], new[5] = 300, 1
+    lens[7], new[7] = 0, 0
+    lens[8], new[8] = 129, 0
+    lens[9], new[9] = 400, 400
+    return O.Setup(seed, dtype, h, g, page, lens, new, behind=2, q_scale=q_scale)
+
+
+@pytest.mark.parametrize("kinds", [(), ("bias",), ("prefix",), ("docs",), ("window", "prefix", "bias")], ids=lambda k: "+".join(k) or "causal")
+@pytest.mark.parametrize("cap", [0.0, 4.0])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_rows(kinds, cap, dtype):
+    st = many(51 + len(kinds), dtype)
+    masks = masks_of(st, kinds)
+    cache, lse = check_attn(st, cap=cap, **masks)
+    check_weights(st, cache, lse, cap=cap, decay=0.75, **masks)
+
+
+@pytest.mark.parametrize("page", [1, 4, 64, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_rows_page_sizes_and_pages_that_are_none(page, dtype):
+    st = many(60 + page, dtype, page=page)
+    for b in (0, 4, 9):
+        cols = [c for c in (0, 1, 5, 70, 71) if c < -(-st.lens[b] // page)][:3]
+        for c in cols:
+            st.table[b, c] = st.num_pages if c % 2 else -1
+    cache, lse = check_attn(st)
+    check_weights(st, cache, lse, with_in=False)
+
+
+@pytest.mark.parametrize("value", [NAN, math.inf])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_rows_what_is_not_seen(value, dtype):
+    st, clean = many(71, dtype, h=8, g=8), many(71, dtype, h=8, g=8)
+    first = torch.zeros(st.total, dtype=torch.int32)
+    hidden = []
+    for b in (1, 9, 12):                     # one token's row is hidden from all others of its sequence: the earlier ones by position
+        s, n = st.lens[b], st.new[b]
+        t = s - n // 2
+        hidden.append(int(st.cu[b]) + n - n // 2)
+        for rows in (st.k, st.v):
+            rows[int(st.table[b, t // 16]), :, t % 16, 3:70:9] = value
+        first[hidden[-1] + 1:int(st.cu[b + 1])] = t + 1
+    for b, s in enumerate(st.lens):
+        if s % 16:
+            for rows in (st.k, st.v):
+                rows[int(st.table[b, (s - 1) // 16]), :, s % 16:] = value
+    out, lse = run_attn(st, cache_of(st), first=first)
+    want, want_lse, tol, tol_lse = O.attention(clean, first=first)
+    keep = [i for i in range(int(st.cu[-1])) if i not in hidden]
+    near(out[keep], want[keep], tol[keep], "out")
+    near(lse[keep], want_lse[keep], tol_lse[keep], "lse")
+
+
+@pytest.mark.parametrize("cap", [0.0, 5.0])
+@pytest.mark.parametrize("lens,new,h,g", [((4300, 5000), (140, 131), 8, 1), ((6000,), (70,), 16, 2)])
+def test_many_rows_with_their_keys_split(lens, new, h, g, cap):
+    st = O.Setup(81, "bf16", h, g, 16, lens, new, q_scale=2.0)
+    check_attn(st, cap=cap, **masks_of(st, ("prefix", "bias")))
+    check_attn(st, cap=cap, **masks_of(st, ("window",)))
+
+
+@pytest.mark.parametrize("scale", [0.5, 40.0])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_around_the_cap(scale, dtype):
+    """Below the cap and far beyond it, in one call."""
+    st = O.Setup(82, dtype, 8, 2, 16, (200, 90), (100, 1), q_scale=scale)
+    cache, lse = check_attn(st, cap=2.0)
+    check_weights(st, cache, lse, cap=2.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_few_rows_joined_in_the_launch_and_replayed(dtype):
+    """One sequence's single token over many keys: the runs' hand-over, in eager calls and in two graphs on one handle that take turns."""
+    st = O.Setup(83, dtype, 4, 1, 16, (3000,), (1,), q_scale=2.0)
+    cache, _ = check_attn(st)
+    want, want_lse, tol, tol_lse = O.attention(st)
+    args = [dev(x) for x in (st.k, st.v, st.cu, st.cur, st.table)]
+    q = dev(st.q).clone()
+    outs = [(torch.zeros((1, 4, 128), dtype=st.td, device=DEV), torch.zeros((1, 4), device=DEV)) for _ in range(2)]
+    graphs = []
+    torch.cuda.synchronize()
+    for o, l in outs:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            ck.ctkvr_cache_attn(cache, q, *args, o, out_lse=l)
+    first = None
+    for i in range(6):
+        o, l = outs[i % 2]
+        o.zero_(), l.zero_()
+        graphs[i % 2].replay()
+        near(o, want, tol, "out")
+        near(l, want_lse, tol_lse, "lse")
+        eager = torch.zeros_like(o)
+        ck.ctkvr_cache_attn(cache, q, *args, eager)
+        first = o.clone() if first is None else first
+        assert torch.equal(o, first) and torch.equal(eager, first)
+
+
 # ---- append ----------------------------------------------------------------------------------------------------
 def check_append(st, cache, freq, axis, positions, q=None, kn=None, vn=None, q_out=None):
     k, v = dev(st.k).clone(), dev(st.v).clone()
