@@ -488,6 +488,27 @@ def test_evict(case, dtype, values):
             assert np.array_equal(w_out[b, :, m:].cpu().numpy(), rest, equal_nan=True)
 
 
+@pytest.mark.parametrize("lens", [(20000, 9000), (50000, 33000), (70000, 65537)], ids=str)
+@pytest.mark.parametrize("values", ["spread", "narrow", "ties", "equal"])
+def test_evict_from_long_sequences(lens, values):
+    """Every number of ranks that a thread of the selection holds, none among them, and more weights that agree than shared memory has room for."""
+    st = O.Setup(23, "bf16", 1, 1, 64, lens, (0, 0))
+    w = torch.rand((2, 1, st.cols * 64), generator=st.gen)
+    if values == "narrow":                     # one bin of the first round
+        w = 1.0 + w / 4096
+    elif values == "ties":
+        w = (w * 5).floor()
+    elif values == "equal":
+        w[:] = 2.0
+    for budget, n_init, n_local in ((700, 4, 100), (12000, 0, 1)):
+        ids, lens_out, w_want, k_want, v_want = O.evicted(st, w, budget, n_init, n_local)
+        k, v, w_out = dev(st.k).clone(), dev(st.v).clone(), torch.zeros_like(w, device=DEV)
+        got = torch.zeros((2, 1, budget), dtype=torch.int32, device=DEV)
+        ck.ctkvr_cache_evict(cache_of(st), dev(w), k, v, dev(st.cur), dev(st.table), budget, got, n_init=n_init, n_local=n_local, weights_out=w_out)
+        assert np.array_equal(got.cpu().numpy(), ids)
+        assert torch.equal(k.cpu(), k_want) and torch.equal(v.cpu(), v_want) and torch.equal(w_out.cpu(), w_want)
+
+
 def test_evict_with_pages_that_are_none():
     st = O.Setup(22, "bf16", 4, 2, 16, (500, 300), (0, 0))
     st.table[0, 3], st.table[0, 20], st.table[1, 0], st.table[1, 18] = -1, st.num_pages, -7, 2 ** 31 - 1
