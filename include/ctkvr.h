@@ -300,7 +300,9 @@ int ctkvr_cache_weights(ctkvr_cache *c, const void *q, int64_t q_stride, const f
  * of those in between the budget - n_init - n_local with the largest weights, ties to the lowest slot (-0 equals +0, NaN is below
  * -infinity).  The kept rows of K and V move to the front in place, in order: slot j then holds what slot out_ids[b][kv][j] held.
  *   weights_in  as ctkvr_cache_weights leaves them;  weights_out  the same shape or NULL, may be weights_in: the kept weights, moved alike.
- *   out_ids     int32 [batch][g][budget] ascending, -1 padded;  out_lens  int32 [batch] or NULL: min(cur_lens[b], budget).
+ *   out_ids     int32 [batch][g][budget] ascending, -1 padded.
+ *   out_lens    int32 [batch] or NULL: min(cur_lens[b], budget).  May be cur_lens, so that a captured step keeps one array of lengths (one
+ *               more launch); an array that overlaps it otherwise is refused.
  * Pages that no kept token needs any more are the caller's again; slots from out_lens[b] on hold what they held before or moved rows.  A row whose
  * old or new page is no page is not moved.  Sequences must not share the pages.  Errors: EINVAL.
  */

@@ -539,7 +539,7 @@ def ctkvr_cache_weights(cache: Cache, q, lse, k_pages, cu_new, cur_lens, block_t
 
 def ctkvr_cache_evict(cache: Cache, weights_in, k_pages, v_pages, cur_lens, block_table, budget, out_ids, n_init=0, n_local=0,
                       weights_out=None, out_lens=None) -> None:
-    """out_ids: int32 [batch][g][budget]; out_lens: int32 [batch] or None."""
+    """out_ids: int32 [batch][g][budget]; out_lens: int32 [batch], cur_lens itself or None."""
     p = cache.params
     shape = (p.batch, p.n_kv_heads, weights_in.shape[-1])
     _check(cache._lib.ctkvr_cache_evict(

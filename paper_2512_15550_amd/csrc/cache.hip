@@ -381,6 +381,10 @@ int ctkvr_cache_evict(ctkvr_cache *c, const float *weights_in, int32_t weights_s
     if (n_init < 0 || n_local < 0 || (int64_t)n_init + n_local > budget)
         return fail(CTKVR_EINVAL, "n_init %d and n_local %d: not negative, and budget %d at most together", n_init, n_local, budget);
     if (!aligned16(k_pages) || !aligned16(v_pages)) return fail(CTKVR_EINVAL, "pages must begin on 16-byte boundaries");
+    const bool lens_in_place = out_lens == cur_lens;
+    const uintptr_t cur0 = (uintptr_t)cur_lens, lens0 = (uintptr_t)out_lens, lens_bytes = (uintptr_t)c->p.batch * 4;
+    if (out_lens && !lens_in_place && cur0 < lens0 + lens_bytes && lens0 < cur0 + lens_bytes)
+        return fail(CTKVR_EINVAL, "out_lens overlaps cur_lens: it may be cur_lens, or none of it");
     DeviceScope on(c->dev);
     HIP_TRY(on.err);
     EvictArgs a{};
@@ -392,7 +396,7 @@ int ctkvr_cache_evict(ctkvr_cache *c, const float *weights_in, int32_t weights_s
     a.n_init = n_init;
     a.n_local = n_local;
     a.ids = out_ids;
-    a.lens = out_lens;
+    a.lens = lens_in_place ? nullptr : out_lens;
     a.k_pages = k_pages;
     a.v_pages = v_pages;
     const int units = c->p.batch * c->p.n_kv_heads, keys = c->p.max_pages * c->p.page_size;
@@ -409,6 +413,10 @@ int ctkvr_cache_evict(ctkvr_cache *c, const float *weights_in, int32_t weights_s
     while (a.slices < pieces / 2 && 2 * units * a.slices <= c->num_cu) a.slices *= 2;
     if (c->p.dtype == CTKVR_BF16) evict_move_kernel<bf16_t><<<dim3((unsigned)(units * a.slices)), 1024, 0, st>>>(a);
     else evict_move_kernel<float><<<dim3((unsigned)(units * a.slices)), 1024, 0, st>>>(a);
+    if (lens_in_place) {   // (every block above reads the lengths as they were)
+        a.lens = out_lens;
+        evict_lens_kernel<<<dim3((unsigned)((c->p.batch + 255) / 256)), 256, 0, st>>>(a);
+    }
     return launched("ctkvr_cache_evict");
 }
 

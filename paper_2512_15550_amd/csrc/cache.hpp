@@ -1361,7 +1361,7 @@ struct EvictArgs {
     int w_stride;
     int budget, n_init, n_local;
     int32_t *ids;          // [batch][g][budget]
-    int32_t *lens;         // [batch] or null
+    int32_t *lens;         // [batch], another array than v.cur (evict_lens_kernel: any), or null
     void *k_pages, *v_pages;
     int slices;
 };
@@ -1559,6 +1559,13 @@ template <int EACH> __global__ __launch_bounds__(1024) void evict_select_kernel(
         if (kept >> lane & 1) ids[at + lanes_below(kept)] = key;
         at += __popcll(kept);
     });
+}
+
+// The lengths after an eviction into the array that holds those before it: behind the other kernels, whose blocks all read them
+__global__ void evict_lens_kernel(EvictArgs a)
+{
+    const int b = blockIdx.x * blockDim.x + threadIdx.x;
+    if (b < a.v.batch) a.lens[b] = min(min(max(a.v.cur[b], 0), a.v.max_pages << a.v.page_shift), a.budget);
 }
 
 // The kept rows to the front, in order and in place.  Row j comes from ids[j] >= j, so rounds of rows, read as a whole before the first of them is

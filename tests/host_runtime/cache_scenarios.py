@@ -145,7 +145,20 @@ def refused_wait(x):
     assert x.lib.ctkvr_release_scratch() == OK and x.fake.fake_live_bytes(0) == 0
 
 
-SCENARIOS = {f.__name__: f for f in (parameters, arguments, other_device, refused_wait)}
+def lengths_in_place(x):
+    """Eviction may write the lengths over those that it read, which takes a launch behind all that read them; arrays that overlap otherwise are
+    refused."""
+    c = x.create(batch=5)
+    apart = x.evict(c, lens=PTR + 20)
+    assert x.evict(c, cur=PTR + 20, lens=PTR) == apart and x.evict(c) == apart
+    assert x.evict(c, lens=PTR) == apart + 1
+    for off in (4, 8, 16, -4, -16):
+        x.evict(c, expect=EINVAL, lens=PTR + off)
+        assert "overlaps" in ck.ctkvr_last_error()
+    x.lib.ctkvr_cache_free(c)
+
+
+SCENARIOS = {f.__name__: f for f in (parameters, arguments, other_device, refused_wait, lengths_in_place)}
 
 if __name__ == "__main__":
     SCENARIOS[sys.argv[1]](Host(sys.argv[2]))

@@ -521,6 +521,36 @@ def test_evict_with_pages_that_are_none():
     assert torch.equal(k.cpu(), k_want) and torch.equal(v.cpu(), v_want)
 
 
+def test_evict_with_the_lengths_written_in_place():
+    """out_lens is cur_lens: every head and the move see the lengths before, eagerly and in a captured call whose lengths are set again."""
+    st = O.Setup(24, "bf16", 8, 8, 16, (700, 50, 0, 1300, 81, 80, 900, 1299), (0,) * 8)
+    w = torch.rand((8, 8, st.cols * 16), generator=st.gen)
+    ids, lens_out, w_want, k_want, v_want = O.evicted(st, w, 80, 4, 16)
+    k, v, wd, cur, table = dev(st.k).clone(), dev(st.v).clone(), dev(w).clone(), dev(st.cur).clone(), dev(st.table)
+    got, cache = torch.full((8, 8, 80), 77, dtype=torch.int32, device=DEV), cache_of(st)
+
+    def call():
+        ck.ctkvr_cache_evict(cache, wd, k, v, cur, table, 80, got, n_init=4, n_local=16, weights_out=wd, out_lens=cur)
+
+    def check():
+        assert cur.tolist() == lens_out
+        assert np.array_equal(got.cpu().numpy(), ids)
+        assert torch.equal(k.cpu(), k_want) and torch.equal(v.cpu(), v_want)
+        for b, m in enumerate(lens_out):
+            assert torch.equal(wd[b, :, :m].cpu(), w_want[b, :, :m])
+
+    call()
+    check()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(4):
+        k.copy_(st.k), v.copy_(st.v), wd.copy_(w), cur.copy_(st.cur), got.fill_(77)
+        graph.replay()
+        check()
+
+
 # ---- streams, graphs, repetition -----------------------------------------------------------------------------------
 @pytest.mark.parametrize("new", [1, 90])
 def test_the_same_call_gives_the_same_bits_on_any_stream(new):
