@@ -133,17 +133,6 @@ template <typename T> __device__ __forceinline__ f32x16_t rows_dot(const char *t
     return acc;
 }
 
-// tanh(x): the continued fraction's fifth convergent below 0.6 (off by 1e-9 of it), (1 - e) / (1 + e) with e = exp(-2 x) above, where that loses nothing
-__device__ __forceinline__ float tanh_f(float x)
-{
-    const float a = fabsf(x), y = x * x;
-    const float e = exp2_fast(a * (-2.0f * kLog2e));
-    const float ns = a * fmaf(y, 105.0f + y, 945.0f), ds = fmaf(y, fmaf(y, 15.0f, 420.0f), 945.0f);
-    const bool small = a < 0.6f;
-    const float n = small ? ns : 1.0f - e, d = small ? ds : 1.0f + e;
-    return copysignf(n * __builtin_amdgcn_rcpf(d), x);
-}
-
 // ---- scores ------------------------------------------------------------------------------------------
 constexpr int kCap = 1, kBias = 2;
 // scores times log2 e, from the dot products (without cap and bias the factor is left to the exponent)
@@ -151,20 +140,29 @@ template <int OPT> __device__ __forceinline__ void score_regs(f32x16_t &s, const
 {
     if constexpr (OPT != 0) {
         if constexpr ((OPT & kCap) != 0) {
-            // Scores within the cap, as they are as a rule: the fifth convergent alone, off by 1e-7 of it at the cap, is half the instructions
+            // cap tanh(x), x = score / cap: up to the cap, where scores are as a rule, by the fifth convergent of tanh's continued fraction, off by 1e-7 of it
+            // at most; beyond by (1 - e) / (1 + e), e = exp(-2 |x|), which loses nothing there.  Which of them a score gets is its own size's matter, so that no
+            // other key or row has a part in it; the wave only leaves the second out, half of the instructions, where none of its scores needs it.
             float big = 0.0f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) big = fmaxf(big, fabsf(s[i]));
+            auto capped = [&](float z, auto beyond) {
+                const float x = z * o.cap_in, y = x * x;
+                float n = x * fmaf(y, fmaf(y, o.cap_out, o.cap_105), o.cap_945), d = fmaf(y, fmaf(y, 15.0f, 420.0f), 945.0f);
+                if constexpr (decltype(beyond)::value) {
+                    const float e = exp2_fast(fabsf(x) * (-2.0f * kLog2e));
+                    const bool far = fabsf(x) > 1.0f;
+                    n = far ? copysignf(o.cap_out - o.cap_out * e, x) : n;
+                    d = far ? 1.0f + e : d;
+                }
+                return n * __builtin_amdgcn_rcpf(d);
+            };
             if (__any(big * o.cap_in > 1.0f)) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = o.cap_out * tanh_f(s[i] * o.cap_in);
+                for (int i = 0; i < 16; ++i) s[i] = capped(s[i], std::true_type());
             } else {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float x = s[i] * o.cap_in, y = x * x;
-                    const float n = x * fmaf(y, fmaf(y, o.cap_out, o.cap_105), o.cap_945), d = fmaf(y, fmaf(y, 15.0f, 420.0f), 945.0f);
-                    s[i] = n * __builtin_amdgcn_rcpf(d);
-                }
+                for (int i = 0; i < 16; ++i) s[i] = capped(s[i], std::false_type());
             }
         }
         const float far = (float)(pos_minus_key0 - 4 * half);   // (distances below 2^24 are exact)

@@ -339,6 +339,35 @@ def test_scores_around_the_cap(scale, dtype):
     check_weights(st, cache, lse, cap=2.0)
 
 
+@pytest.mark.parametrize("shape", ["few", "many"])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_capped_scores_are_a_matter_of_their_own_size(shape, bias, dtype):
+    """A token whose scores are far beyond the cap: the tokens before it, which do not see its key, and all keys' weights without its row are the
+    same to the bit."""
+    st = many(84, dtype, q_scale=1.0) if shape == "many" else O.Setup(84, dtype, 4, 2, 16, (200, 90, 700), (100, 90, 2))
+    masks = masks_of(st, ("bias",)) if bias else {}
+    slopes = dev(masks.get("slopes"))
+    loud = [int(st.cu[b + 1]) - 1 for b, n in enumerate(st.new) if n > 1]
+    quiet = [i for i in range(int(st.cu[-1])) if i not in loud]
+    got = []
+    for factor in (1.0, 100.0):
+        q, k = st.q.clone(), st.k.clone()
+        q[loud] *= factor
+        for b, n in enumerate(st.new):
+            if n > 1:
+                t = st.lens[b] - 1
+                k[int(st.table[b, t // 16]), :, t % 16] *= factor
+        cache = cache_of(st, softcap=30.0)
+        out, lse = torch.zeros((st.total, st.h, 128), dtype=st.td, device=DEV), torch.zeros((st.total, st.h), device=DEV)
+        ck.ctkvr_cache_attn(cache, dev(q), dev(k), dev(st.v), dev(st.cu), dev(st.cur), dev(st.table), out, out_lse=lse, slopes=slopes)
+        w, only = torch.zeros((st.batch, st.g, st.cols * 16), device=DEV), lse.clone()
+        only[loud] = -math.inf
+        ck.ctkvr_cache_weights(cache, dev(q), only, dev(k), dev(st.cu), dev(st.cur), dev(st.table), None, w, slopes=slopes)
+        got.append((out[quiet], lse[quiet], w))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_few_rows_joined_in_the_launch_and_replayed(dtype):
     """One sequence's single token over many keys: the runs' hand-over, in eager calls and in two graphs on one handle that take turns."""
