@@ -892,7 +892,8 @@ __device__ __forceinline__ int scattered_key(int lane)   // the key (of 32) whos
     const int i = (lane & 31) >> 1;
     return 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
 }
-// A row's part in the sums: what it sees and minus its log-sum-exp (in units of log2 e; a row that sees nothing adds nothing)
+// A row's part in the sums: what it sees and minus its log-sum-exp (in units of log2 e).  A row whose log-sum-exp is -infinity sees nothing: it may be one that
+// the caller leaves out, whose scores are anything, NaN included.
 struct WeightRow {
     RowSight sight;
     float nlse, slope2;
@@ -903,9 +904,9 @@ template <int OPT> __device__ __forceinline__ WeightRow weight_row(const WeightA
     WeightRow w;
     w.sight = row_sight(a.v, a.o, s, prefix, token);
     const float lse = a.lse[(size_t)(s.c0 + token) * a.v.h + head];
-    w.nlse = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
+    w.nlse = -lse * kLog2e;
     w.slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
-    if (row >= rows) {
+    if (row >= rows || lse == -INFINITY) {
         w.sight.hi = 0;
         w.nlse = -INFINITY;
     }
@@ -1181,7 +1182,12 @@ template <typename T, int OPT> __global__ __launch_bounds__(256, 2) void weights
             row_to_lds(lds0 + j * kPer * RowTile<T>::kRowBytes,
                        (const char *)((const T *)a.q + (int64_t)(s.c0 + (row >> v.lg)) * a.q_stride + ((kv << v.lg) + (row & ((1 << v.lg) - 1))) * 128) + 16 * c);
         }
-        for (int r = threadIdx.x; r < 32 * blocks; r += 256) part[r] = weight_row<OPT>(a, s, prefix, kv, r0 + r, rows);
+        bool left_out = false;
+        for (int r = threadIdx.x; r < 32 * blocks; r += 256) {
+            const WeightRow w = weight_row<OPT>(a, s, prefix, kv, r0 + r, rows);
+            left_out |= r < have && w.nlse == -INFINITY;
+            part[r] = w;
+        }
         auto before_of = [&](int key) {
             if (r0 > 0) return key < s.len ? a.w_out[w0 + key] : 0.0f;
             return a.w_in && key < min(s.old, s.len) ? a.decay * a.w_in[w0 + key] : 0.0f;
@@ -1191,7 +1197,7 @@ template <typename T, int OPT> __global__ __launch_bounds__(256, 2) void weights
             for (int key = s1 * 32 + lane; key < min(t1 * 32, s.len); key += 64) a.w_out[w0 + key] = before_of(key);
         }
         loads_landed<0>();
-        __syncthreads();
+        const bool all_count = !__syncthreads_or(left_out);
         for (int t = s0; t < s1; ++t) {
             const int key = t * 32 + mine;
             const float before = before_of(key);
@@ -1199,7 +1205,7 @@ template <typename T, int OPT> __global__ __launch_bounds__(256, 2) void weights
             if (sizeof(T) == 2 && t + 1 < s1) load_operand(next, (const T *)a.k_pages + (int64_t)rows_of(t + 1) * 128, half);
             const uint32_t bad_next = bad;
             f32x16_t sum[1] = {};
-            if (sizeof(T) == 2 && !a.o.first && t * 32 + 32 <= all_hi && bad_now == 0) {
+            if (sizeof(T) == 2 && all_count && !a.o.first && t * 32 + 32 <= all_hi && bad_now == 0) {
                 if constexpr (sizeof(T) == 2) {
                     Operand<T> q;
                     tile_operand(q, smem, lane & 31, half);

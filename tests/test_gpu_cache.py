@@ -185,6 +185,30 @@ def test_what_is_not_seen_does_not_matter(value, dtype):
     near(w[0][:, others], want_w[0][:, others], tol_w[0][:, others], "weights")
 
 
+@pytest.mark.parametrize("shape", ["single", "few", "turns", "rows", "many"])
+@pytest.mark.parametrize("value", [NAN, math.inf])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_left_out_of_the_weights(shape, value, dtype):
+    """A row of -infinity adds nothing, whatever its query holds (a batch padded with tokens of no request): in every form of the kernels."""
+    if shape == "many":
+        st = many(85, dtype)
+    else:
+        lens, new = {"single": ((500, 90, 33), (1, 1, 1)), "few": ((300, 129), (40, 3)), "turns": ((600,), (180,)), "rows": ((700,), (700,))}[shape]
+        st = O.Setup(85, dtype, 8, 2, 16, lens, new, q_scale=2.0)
+    cache = cache_of(st)
+    _, lse = run_attn(st, cache)
+    n, q = int(st.cu[-1]), dev(st.q).clone()
+    out = torch.rand((n, st.h), generator=st.gen) < 0.3     # single heads,
+    out[::7] = True                                         # whole tokens,
+    out[-1, 1:] = True                                      # and the last rows of all
+    lse[:n][out.to(DEV)] = -math.inf
+    q[:n][out.to(DEV)] = value
+    w_in, w = torch.rand((st.batch, st.g, st.cols * 16), generator=st.gen), torch.full((st.batch, st.g, st.cols * 16), 5.0, device=DEV)
+    ck.ctkvr_cache_weights(cache, q, lse, dev(st.k), dev(st.cu), dev(st.cur), dev(st.table), dev(w_in), w, decay=0.5)
+    want, tol = O.weights(st, lse.cpu(), w_in, torch.full(w.shape, 5.0), 0.5)
+    near(w, want, tol, "weights")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_values_that_are_seen_and_not_finite(dtype):
     """An infinite value reaches the rows that see its key, in its column, and no others."""
