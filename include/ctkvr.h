@@ -246,7 +246,8 @@ typedef struct {
 } ctkvr_cache_params;
 
 /* A handle on the current device; params' arrays are copied.  Clears words of its workspace on hip_stream and synchronises it.
- * Errors: EINVAL, EUNSUPPORTED (as the index; a sequence of more than 2^20 tokens, a cache of 2^32 rows), ENOMEM. */
+ * Errors: EINVAL, EUNSUPPORTED (as the index; a sequence of more than 2^20 tokens, a cache of 2^32 rows, more than 2^20 new tokens, 2^16
+ * sequences or 2^10 heads, 2^22 or more KV heads of all sequences), ENOMEM. */
 int ctkvr_cache_create(const ctkvr_cache_params *p, void *hip_stream, ctkvr_cache **out_cache);
 /* Release a handle (NULL is allowed); synchronises its device first, as ctkvr_free does. */
 void ctkvr_cache_free(ctkvr_cache *c);

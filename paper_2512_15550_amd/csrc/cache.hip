@@ -50,6 +50,10 @@ int check_cache_params(const ctkvr_cache_params *p)
         return fail(CTKVR_EUNSUPPORTED, "max_pages %d of %d tokens: sequences of 2^20 tokens at most", p->max_pages, p->page_size);
     if (p->max_new > (1 << 20) || p->batch > (1 << 16) || p->n_q_heads > (1 << 10))
         return fail(CTKVR_EUNSUPPORTED, "max_new %d, batch %d, n_q_heads %d: at most 2^20, 2^16, 2^10", p->max_new, p->batch, p->n_q_heads);
+    // A launch has fewer than 2^32 threads a dimension.  Units (a sequence's KV head) are one of weights and eviction, of up to 1024 threads; attention's blocks
+    // of 256 are max_new * n_q_heads / 128 + units at most, or three a unit, and those of split keys a few a CU.
+    if ((int64_t)p->batch * p->n_kv_heads >= 1 << 22)
+        return fail(CTKVR_EUNSUPPORTED, "%d sequences of %d KV heads: fewer than 2^22 together", p->batch, p->n_kv_heads);
     if ((int64_t)p->num_pages * p->page_size * p->n_kv_heads >= 0xffffffffll)
         return fail(CTKVR_EUNSUPPORTED, "%d pages: a cache of 2^32 - 2 rows at most", p->num_pages);
     if ((((int64_t)p->max_pages * p->page_size + 127) / 128) * p->batch * p->n_kv_heads >= (1ll << 31))
@@ -189,16 +193,16 @@ template <typename T> int weights_launch(const ctkvr_cache *c, WeightArgs &a, in
     if (((int64_t)a.v.total << c->lg) <= 2ll * held * used) {
         a.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>((c->p.batch > 1 ? 8 : 2) * c->num_cu / units, (keys + 127) / 128));
         with_opts(opt, [&](auto o) {
-            weights_few_kernel<T, decltype(o)::value><<<dim3((unsigned)(units * a.nsplit)), 256, 0, st>>>(a);
+            weights_few_kernel<T, decltype(o)::value><<<dim3((unsigned)units, (unsigned)a.nsplit), 256, 0, st>>>(a);
             return 0;
         });
     } else {
         // (rows go past 256 keys of a block, 128 in fp32, unless that leaves CUs without one)
         constexpr int kWide = sizeof(T) == 2 ? 256 : 128;
-        const int64_t wide = (keys + kWide - 1) / kWide * units, narrow = (keys + kWide / 4 - 1) / (kWide / 4) * units;
+        const unsigned wide = (unsigned)((keys + kWide - 1) / kWide), narrow = (unsigned)((keys + kWide / 4 - 1) / (kWide / 4));
         with_opts(opt, [&](auto o) {
-            if (wide >= c->num_cu) weights_kernel<T, decltype(o)::value><<<dim3((unsigned)wide), 512, 0, st>>>(a);
-            else weights_rows_kernel<T, decltype(o)::value><<<dim3((unsigned)narrow), 512, 0, st>>>(a);
+            if (wide * units >= c->num_cu) weights_kernel<T, decltype(o)::value><<<dim3((unsigned)units, wide), 512, 0, st>>>(a);
+            else weights_rows_kernel<T, decltype(o)::value><<<dim3((unsigned)units, narrow), 512, 0, st>>>(a);
             return 0;
         });
     }
@@ -411,8 +415,8 @@ int ctkvr_cache_evict(ctkvr_cache *c, const float *weights_in, int32_t weights_s
     const int pieces = c->p.dtype == CTKVR_BF16 ? 32 : 64;
     a.slices = pieces / 8;
     while (a.slices < pieces / 2 && 2 * units * a.slices <= c->num_cu) a.slices *= 2;
-    if (c->p.dtype == CTKVR_BF16) evict_move_kernel<bf16_t><<<dim3((unsigned)(units * a.slices)), 1024, 0, st>>>(a);
-    else evict_move_kernel<float><<<dim3((unsigned)(units * a.slices)), 1024, 0, st>>>(a);
+    if (c->p.dtype == CTKVR_BF16) evict_move_kernel<bf16_t><<<dim3((unsigned)units, (unsigned)a.slices), 1024, 0, st>>>(a);
+    else evict_move_kernel<float><<<dim3((unsigned)units, (unsigned)a.slices), 1024, 0, st>>>(a);
     if (lens_in_place) {   // (every block above reads the lengths as they were)
         a.lens = out_lens;
         evict_lens_kernel<<<dim3((unsigned)((c->p.batch + 255) / 256)), 256, 0, st>>>(a);

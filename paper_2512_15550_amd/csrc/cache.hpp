@@ -979,7 +979,7 @@ template <typename T, int OPT> __global__ __launch_bounds__(512, 2) void weights
     __shared__ __align__(16) char smem[2][kTile];
     const CacheView &v = a.v;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, side = wave >> 2;
-    const int kv = blockIdx.x % v.g, b = blockIdx.x / v.g % v.batch, key0 = blockIdx.x / v.g / v.batch * kKeys, mine0 = key0 + 32 * kBlocks * (wave & 3);
+    const int kv = blockIdx.x % v.g, b = blockIdx.x / v.g, key0 = blockIdx.y * kKeys, mine0 = key0 + 32 * kBlocks * (wave & 3);
     const SeqSpan s = seq_span(v, b);
     if (key0 >= s.len) return;
     const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
@@ -1065,7 +1065,7 @@ template <typename T, int OPT> __global__ __launch_bounds__(512, 2) void weights
     __shared__ float sums[8][kKeys];
     const CacheView &v = a.v;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int kv = blockIdx.x % v.g, b = blockIdx.x / v.g % v.batch, key0 = blockIdx.x / v.g / v.batch * kKeys;
+    const int kv = blockIdx.x % v.g, b = blockIdx.x / v.g, key0 = blockIdx.y * kKeys;
     const SeqSpan s = seq_span(v, b);
     if (key0 >= s.len) return;
     const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0, rows = s.n << v.lg;
@@ -1130,7 +1130,7 @@ template <typename T, int OPT> __global__ __launch_bounds__(256, 2) void weights
     __shared__ WeightRow part[kRows];
     const CacheView &v = a.v;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int units = v.batch * v.g, unit = blockIdx.x % units, split = blockIdx.x / units, b = unit / v.g, kv = unit % v.g;
+    const int unit = blockIdx.x, split = blockIdx.y, b = unit / v.g, kv = unit % v.g;
     const SeqSpan s = seq_span(v, b);
     const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0, rows = s.n << v.lg;
     const int64_t tiles = (s.len + 31) / 32, runs = (int64_t)a.nsplit * 4, run = split * 4 + wave;
@@ -1579,7 +1579,7 @@ template <typename T> __global__ __launch_bounds__(1024) void evict_move_kernel(
 {
     constexpr int kPieces = 2 * 128 * sizeof(T) / 16, kEach = 8;   // 16-byte pieces of a key's K and V rows
     const CacheView &v = a.v;
-    const int units = v.batch * v.g, unit = blockIdx.x % units, slice = blockIdx.x / units, b = unit / v.g, kv = unit % v.g;
+    const int unit = blockIdx.x, slice = blockIdx.y, b = unit / v.g, kv = unit % v.g;
     const int len = min(max(v.cur[b], 0), v.max_pages << v.page_shift), keep = min(len, a.budget);
     const int32_t *ids = a.ids + (size_t)unit * a.budget;
     const size_t w0 = (size_t)unit * a.w_stride;

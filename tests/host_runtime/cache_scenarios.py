@@ -158,7 +158,25 @@ def lengths_in_place(x):
     x.lib.ctkvr_cache_free(c)
 
 
-SCENARIOS = {f.__name__: f for f in (parameters, arguments, other_device, refused_wait, lengths_in_place)}
+def largest_batches(x):
+    """What creation admits can be launched (fewer than 2^32 threads a dimension of a grid); what cannot is refused there."""
+    for geometry in (dict(batch=1024, n_q_heads=8, n_kv_heads=8, page_size=256, max_pages=512, num_pages=2),
+                     dict(batch=8, n_q_heads=64, n_kv_heads=8, page_size=256, max_pages=4096, num_pages=2),
+                     dict(batch=(1 << 16) - 1, n_q_heads=64, n_kv_heads=64, page_size=1, max_pages=1, num_pages=2),
+                     dict(batch=(1 << 13) - 1, n_q_heads=1 << 10, n_kv_heads=1 << 9, page_size=16, max_pages=2, num_pages=2)):
+        for dtype in (ck.BF16, ck.F32):
+            h, g = geometry["n_q_heads"], geometry["n_kv_heads"]
+            c = x.create(dtype=dtype, max_new=1 << 20, **geometry)
+            for total in (1, 64, 1024, 1 << 14, 1 << 16, 1 << 18, 1 << 20):
+                rows = dict(total=total, qs=h * 128)
+                assert x.append(c, ks=g * 128, vs=g * 128, **rows) > 0 and x.attn(c, **rows) > 0 and x.weights(c, stride=1 << 20, **rows) > 0
+            assert x.evict(c, stride=1 << 20) > 0
+            x.lib.ctkvr_cache_free(c)
+    for batch, g in ((1 << 16, 64), (1 << 12, 1 << 10)):
+        x.create(expect=EUNSUPPORTED, batch=batch, n_q_heads=g, n_kv_heads=g, max_pages=1)
+
+
+SCENARIOS = {f.__name__: f for f in (parameters, arguments, other_device, refused_wait, lengths_in_place, largest_batches)}
 
 if __name__ == "__main__":
     SCENARIOS[sys.argv[1]](Host(sys.argv[2]))

@@ -9,7 +9,7 @@
 #include <mutex>
 
 namespace {
-enum { kOk = 0, kBadValue = 1, kBadDevice = 101, kBadHandle = 400, kCapturing = 900 };
+enum { kOk = 0, kBadValue = 1, kBadDevice = 101, kBadHandle = 400, kBadLaunch = 9, kCapturing = 900 };
 struct Stream {
     int dev;
 };
@@ -151,8 +151,11 @@ int hipGetSymbolAddress(void **p, const void *sym)
     *p = at;
     return kOk;
 }
-int hipLaunchKernel(const void *fn, Dim3, Dim3, void **args, size_t, void *)
+int hipLaunchKernel(const void *fn, Dim3 grid, Dim3 block, void **args, size_t, void *)
 {
+    if ((uint64_t)grid.x * block.x > UINT32_MAX || (uint64_t)grid.y * block.y > UINT32_MAX || (uint64_t)grid.z * block.z > UINT32_MAX ||
+        grid.y > 65535 || grid.z > 65535)
+        return ret(kBadLaunch);
     n_launch++;
     if (fn == fill_words) {
         uint32_t *p = *(uint32_t **)args[0], v = *(uint32_t *)args[1];

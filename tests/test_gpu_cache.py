@@ -420,6 +420,25 @@ def test_few_rows_joined_in_the_launch_and_replayed(dtype):
         assert torch.equal(o, first) and torch.equal(eager, first)
 
 
+def test_weights_of_a_large_batch_with_a_wide_table():
+    """Blocks for every 128 keys of 1024 sequences' tables of 2^17 tokens are 2^32 threads.  The sequences are one, again and again."""
+    batch, n, page = 1024, 300, 256
+    one = O.Setup(86, "f32", 8, 8, page, (n,), (n,), q_scale=2.0)
+    q = dev(one.q).repeat(batch, 1, 1)
+    table = torch.full((batch, 512), -1, dtype=torch.int32, device=DEV)
+    table[:, :2] = dev(one.table[0, :2])
+    cu = (n * torch.arange(batch + 1, device=DEV)).int()
+    cur = torch.full((batch,), n, dtype=torch.int32, device=DEV)
+    cache = ck.ctkvr_cache_create(ck.CacheParams(batch=batch, n_q_heads=8, n_kv_heads=8, num_pages=one.num_pages, max_pages=512, max_new=batch * n,
+                                                 page_size=page, dtype=ck.F32))
+    lse = run_attn(one, cache_of(one))[1]
+    w = torch.full((batch, 8, 512 * page), 5.0, device=DEV)
+    ck.ctkvr_cache_weights(cache, q, lse.repeat(batch, 1), dev(one.k), cu, cur, table, None, w)
+    want, tol = O.weights(one, lse.cpu(), None, torch.full((1, 8, n), 5.0), 1.0)
+    near(w[:1, :, :n], want, tol, "weights")
+    assert (w[:, :, :n] == w[:1, :, :n]).all() and (w[:, :, n:] == 5).all()
+
+
 # ---- append ----------------------------------------------------------------------------------------------------
 def check_append(st, cache, freq, axis, positions, q=None, kn=None, vn=None, q_out=None):
     k, v = dev(st.k).clone(), dev(st.v).clone()
