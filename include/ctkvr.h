@@ -255,7 +255,8 @@ void ctkvr_cache_free(ctkvr_cache *c);
 /*
  * Rotate new queries and keys to their positions and write keys and values into their slots:
  *   x'_i = x_i cos a_i - x_{i+64} sin a_i,  x'_{i+64} = x_{i+64} cos a_i + x_i sin a_i,  a_i = position[axis_i] * frequency_i,
- * in fp32 with angles exact to 2^-32 of a turn at any position, rounded once to `dtype`; values are copied.
+ * in fp32, rounded once to `dtype`; values are copied.  An angle is off by 2^-31 of a turn at any position (frequencies up to 2^32 radians), and by its
+ * rounding to fp32 modulo a quarter of a turn.
  *   q, q_out   [total][h][128] (q_out contiguous; may be q where q is) or both NULL;  k, v  [total][g][128] or both NULL.
  *   positions  DEVICE int32 [axes][total], any values, for the axes that rope_axis names (text: the same on all), or NULL:
  *              the token's slot on every axis.  After an eviction slots are no positions any more.

@@ -69,15 +69,6 @@ int check_cache_params(const ctkvr_cache_params *p)
     return CTKVR_OK;
 }
 
-// a frequency as a fraction of a turn, in 2^-64
-uint64_t turn_of(long double freq)
-{
-    long double t = freq / (2.0L * acosl(-1.0L));
-    t -= floorl(t);
-    const long double u = ldexpl(t, 64);
-    return u >= ldexpl(1.0L, 64) ? 0 : (uint64_t)u;
-}
-
 CacheView view(const ctkvr_cache *c, const int32_t *table, const int32_t *cu, const int32_t *cur, int total)
 {
     CacheView v{};
@@ -235,7 +226,7 @@ int ctkvr_cache_create(const ctkvr_cache_params *p, void *hip_stream, ctkvr_cach
     int cus = 0;
     if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, c->dev) == hipSuccess && cus > 0) c->num_cu = cus;
     for (int i = 0; i < 64; ++i) {
-        c->rope.turn[i] = turn_of(p->rope_freq ? (long double)p->rope_freq[i] : powl((long double)p->rope_base, -i / 64.0L));
+        c->rope.turn[i] = turn_of(p->rope_freq ? (long double)p->rope_freq[i] : rope_freq(p->rope_base, i));
         c->rope.axis[i] = p->rope_axis ? p->rope_axis[i] : 0;
         c->axes = std::max(c->axes, c->rope.axis[i] + 1);
     }

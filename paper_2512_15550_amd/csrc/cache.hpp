@@ -1241,7 +1241,8 @@ template <typename T, int OPT> __global__ __launch_bounds__(256, 2) void weights
 
 // ---- append with rotary positions -----------------------------------------------------------------------
 // Angles.  A pair's frequency is held as a 64-bit fraction of a turn, so that position times frequency modulo 2^64 is the angle modulo a
-// turn, exactly: a position of 2^31 is off by 2^-34 of a turn at most, where a product in 32 bits would have lost it.
+// turn, whatever the position, where a product in 32 bits would have lost it: a position of 2^31 is off by 2^-32 of a turn at most, and so much again goes with the low
+// half of the product.  What is left, an eighth of a turn at most from a quarter, is rounded to fp32 (by 2^-28 of a turn at most).
 struct RopeTable {
     uint64_t turn[64];
     uint8_t axis[64];

@@ -1,6 +1,7 @@
 // Where the operators on the paged KV cache find a sequence's tokens, its rows and what a token sees; plain functions, for the kernels and for the host.
 #pragma once
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -58,5 +59,19 @@ __host__ __device__ __forceinline__ RowSight row_sight(const CacheView &v, const
     r.lo = o.first ? max(o.first[s.c0 + token], 0) : 0;
     return r;
 }
+
+// A frequency (radians per position) as a fraction of a turn, in 2^-64: freq / (2 pi) modulo 1, off by one of them at most for frequencies up to 2^32.
+// 1 / (2 pi) is held as two long doubles, and what the product is off by is added back, so that a frequency of many turns keeps its fraction.
+inline uint64_t turn_of(long double freq)
+{
+    const long double hi = 0xa2f9836e4e44152ap-66L, lo = -0xf62a0b82b2c88fc9p-136L;
+    const long double p = freq * hi, off = fmal(freq, hi, -p) + freq * lo;
+    long double t = p - floorl(p) + off;
+    t -= floorl(t);
+    const long double u = roundl(ldexpl(t, 64));
+    return u >= ldexpl(1.0L, 64) ? 0 : (uint64_t)u;
+}
+// the frequency of pair i; for bases from 1 on its turn is off by 1.25 of 2^-64 at most
+inline long double rope_freq(double base, int i) { return powl((long double)base, -i / 64.0L); }
 
 }  // namespace ctkvr

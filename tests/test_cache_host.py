@@ -81,3 +81,47 @@ def test_page_ids_and_lengths_that_make_no_sense(tmp_path):
                     "-o", str(exe), str(src)], check=True, capture_output=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=60)
     assert r.returncode == 0 and r.stdout == "ok\n", r.stdout + r.stderr
+
+
+TURNS = r"""
+#include "cache_args.hpp"
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+int main(int n, char **args)
+{
+    for (int i = 1; i < n; ++i) {   // frequencies, and bases with the pair's number
+        const char *pair = strchr(args[i], ':');
+        const long double f = pair ? ctkvr::rope_freq(strtod(args[i], nullptr), atoi(pair + 1)) : (long double)strtod(args[i], nullptr);
+        printf("%llu\n", (unsigned long long)ctkvr::turn_of(f));
+    }
+}
+"""
+
+
+@pytest.mark.skipif(not os.path.exists(HIPCC), reason="no hipcc")
+def test_frequencies_as_fractions_of_a_turn(tmp_path):
+    """Against 150 digits: off by one of 2^-64 for a given frequency, 1.25 for one of a base (powl is off by 2^-63 of it at most, a sixth of a turn)."""
+    from decimal import Decimal as D, localcontext
+    src, exe = tmp_path / "turns.hip", tmp_path / "turns"
+    src.write_text(TURNS)
+    subprocess.run([HIPCC, "--offload-arch=gfx950", "--cuda-host-only", "-std=c++17", "-O1", "-I", os.path.join(ROOT, "paper_2512_15550_amd", "csrc"),
+                    "-o", str(exe), str(src)], check=True, capture_output=True)
+    given = [0.0, 1.0, -1.0, 0.1, 7.5, -3.7, 6.283185307179586, 3.141592653589793, 1e6 + 0.1, 123456789.123, -987654321.25, 2.0 ** 31 + 0.5, 2.0 ** 32,
+             1e-9, 1e-30, 5e-324, -1e-25] + [10000.0 ** (-i / 64) for i in range(64)]
+    bases = [(base, i) for base in (10000.0, 500000.0, 1e6, 1.0, 3.5) for i in range(64)]
+    r = subprocess.run([str(exe)] + [x.hex() for x in given] + [f"{x.hex()}:{i}" for x, i in bases], capture_output=True, text=True, timeout=60)
+    got = [int(x) for x in r.stdout.split()]
+    assert r.returncode == 0 and len(got) == len(given) + len(bases)
+    with localcontext() as ctx:
+        ctx.prec = 150
+        a, b, t, p = D(1), 1 / D(2).sqrt(), D(1) / 4, D(1)
+        for _ in range(8):                                  # pi by the arithmetic-geometric mean
+            mean = (a + b) / 2
+            b, t, a, p = (a * b).sqrt(), t - p * (a - mean) ** 2, mean, 2 * p
+        two_pi = (a + b) ** 2 / (2 * t)
+        want = [(D(f), D(1)) for f in given] + [(D(base) ** (D(-i) / 64), D("1.25")) for base, i in bases]
+        for (f, most), u in zip(want, got):
+            off = f / two_pi * 2 ** 64 - u
+            off -= (off / 2 ** 64).to_integral_value() * 2 ** 64
+            assert abs(off) <= most, (f, u, off)
