@@ -439,6 +439,68 @@ def test_weights_of_a_large_batch_with_a_wide_table():
     assert (w[:, :, :n] == w[:1, :, :n]).all() and (w[:, :, n:] == 5).all()
 
 
+@pytest.mark.parametrize("scale", [0.02, 0.31])
+@pytest.mark.parametrize("cap", [0.0, 4.0])
+@pytest.mark.parametrize("shape", ["few", "rows", "many"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_scale_of_ones_own(shape, cap, scale, dtype):
+    if shape == "many":
+        st = many(87, dtype)
+    else:
+        lens, new = {"few": ((300, 900, 50), (40, 1, 50)), "rows": ((600,), (600,))}[shape]
+        st = O.Setup(87, dtype, 8, 2, 16, lens, new, behind=2)
+    slopes = torch.tensor([2.0 ** -(i % 9 + 2) for i in range(st.h)])
+    for bias in (None, slopes):
+        cache = cache_of(st, softcap=cap, sm_scale=scale)
+        out, lse = run_attn(st, cache, slopes=bias)
+        n = int(st.cu[-1])
+        want, want_lse, tol, tol_lse = O.attention(st, cap=cap, slopes=bias, scale=float(np.float32(scale)))
+        near(out[:n], want, tol, "out")
+        near(lse[:n], want_lse, tol_lse, "lse")
+        check_weights(st, cache, lse, cap=cap, decay=0.5, slopes=bias, scale=float(np.float32(scale)))
+
+
+@pytest.mark.parametrize("batch", [65, 130])
+@pytest.mark.parametrize("new", [1, 20, 70])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_sequences_than_a_wave_has_lanes(batch, new, dtype):
+    """Sequences are looked up 64 at a time: empty ones and ones without new tokens around there, single tokens, chunks and prompts."""
+    r = np.random.RandomState(batch + new)
+    lens = [int(x) for x in r.randint(new, new + 60, size=batch)]
+    news = [new if new == 1 else int(x) for x in r.randint(new // 2 + 1, new + 1, size=batch)]
+    for b in (0, 62, 64, batch - 2):
+        news[b] = 0
+    lens[62], lens[3], lens[batch - 1] = 0, 3000, 2000
+    st = O.Setup(88, dtype, 8, 2, 16, lens, news, behind=3, q_scale=2.0)
+    cache, lse = check_attn(st)
+    check_weights(st, cache, lse, decay=0.75)
+    kn, vn = (torch.randn((st.total, 2, 128), generator=st.gen).to(st.td).to(DEV) for _ in range(2))
+    freq = 10000.0 ** (-np.arange(64) / 64.0)
+    k, v, n, slots, pos = check_append(st, cache, freq, np.zeros(64, int), None, None, kn, vn)
+    wk, tk = O.rotated(kn[:n].cpu(), pos, freq, np.zeros(64, int))
+    full_k, full_v, tol_k = st.k.to(O.F8), st.v.clone(), torch.zeros_like(st.k, dtype=O.F8)
+    pages = st.table[torch.repeat_interleave(torch.arange(batch), torch.tensor(news)), slots // 16].long()
+    full_k[pages, :, slots % 16], full_v[pages, :, slots % 16] = wk, vn[:n].cpu()
+    tol_k[pages, :, slots % 16] = tk + wk.abs() * O.HALF[dtype]
+    near(k, full_k, tol_k, "k_pages")
+    assert torch.equal(v.cpu(), full_v), "v_pages"
+
+
+@pytest.mark.parametrize("lens,new,h,g", [
+    ((1500,) + (40, 3000, 700, 1) * 4, (1024,) + (1,) * 16, 8, 2),        # the weights' rows in several turns
+    ((700, 9000, 5000, 33), (600, 1, 1, 1), 8, 2),                        # rows of 128, keys split
+    ((300, 5000, 1300, 4000), (1, 1, 1100, 1), 32, 8),                    # ... not split
+], ids=["turns", "split", "whole"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_chunk_beside_single_tokens(lens, new, h, g, dtype):
+    st = O.Setup(89, dtype, h, g, 16, lens, new, behind=1, q_scale=2.0)
+    cache, lse = check_attn(st)
+    check_weights(st, cache, lse, decay=0.75)
+    masks = masks_of(st, ("window", "prefix", "bias"))
+    cache, lse = check_attn(st, cap=5.0, **masks)
+    check_weights(st, cache, lse, cap=5.0, **masks)
+
+
 # ---- append ----------------------------------------------------------------------------------------------------
 def check_append(st, cache, freq, axis, positions, q=None, kn=None, vn=None, q_out=None):
     k, v = dev(st.k).clone(), dev(st.v).clone()
