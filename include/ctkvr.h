@@ -227,6 +227,8 @@ const char *ctkvr_last_error(void);
  * Each call is asynchronous on hip_stream, a stream of the device that was current when the handle was made (NULL: that device's default
  * stream; the calling thread's current device may be another), allocates nothing and can be captured into a HIP graph.
  * ctkvr_cache_attn uses the handle's workspace: two of its calls on one handle must not overlap, replays of graphs among them.
+ * How a call is split goes by the mean of its tokens over the sequences and by the table's width: a prompt's chunk beside single tokens of other sequences is served
+ * in one call, but faster in two, in each of which the other sequences have no new tokens.
  */
 typedef struct ctkvr_cache ctkvr_cache;   /* opaque: geometry, rotary frequencies, workspace */
 
@@ -269,10 +271,11 @@ int ctkvr_cache_append(ctkvr_cache *c, const void *q, int64_t q_stride, const vo
 /*
  * Attention of the new tokens over the cache (which holds them already): per token and query head softmax(z) V over the keys it sees,
  *   z = cap(q . k * sm_scale) - slope_h * |pos - t|,
- * for key t of the token at pos:  first_key <= t < cur_lens[b]  and  (t <= pos or t < prefix_lens[b]).
+ * for key t of the token at pos:  first_key <= t < cur_lens[b]  and  (t <= pos or t < prefix_lens[b]).  pos and t are slots: in a cache that was
+ * cut down the distance, first_key and prefix_lens count the tokens that are left, and those are others in each KV head.
  *   q           [total][h][128], rotated.
  *   slopes      DEVICE fp32 [h] or NULL: a bias by distance.
- *   prefix_lens DEVICE int32 [batch] or NULL: so many keys at the start are seen by every token, earlier ones too.
+ *   prefix_lens DEVICE int32 [batch] or NULL: so many keys at the start are seen by every token, earlier ones too, from its first_key on.
  *   first_key   DEVICE int32 [total] or NULL: where the token's document begins (packed documents), or its window.
  *   out         [total][h][128] of `dtype`;  out_lse  fp32 [total][h] or NULL, natural log.
  * A token that sees no key, or none with a score above -infinity, gets zeros and -infinity.  What a token does not see does not touch its result,
