@@ -226,7 +226,8 @@ const char *ctkvr_last_error(void);
  *
  * Each call is asynchronous on hip_stream, a stream of the device that was current when the handle was made (NULL: that device's default
  * stream; the calling thread's current device may be another), allocates nothing and can be captured into a HIP graph.
- * ctkvr_cache_attn uses the handle's workspace: two of its calls on one handle must not overlap, replays of graphs among them.
+ * Attention (ctkvr_cache_attn and the calls of the next section that attend) uses the handle's workspace: two such calls on one handle must not overlap,
+ * replays of graphs among them.
  * How a call is split goes by the mean of its tokens over the sequences and by the table's width: a prompt's chunk beside single tokens of other sequences is served
  * in one call, but faster in two, in each of which the other sequences have no new tokens.
  */
@@ -314,6 +315,70 @@ int ctkvr_cache_weights(ctkvr_cache *c, const void *q, int64_t q_stride, const f
 int ctkvr_cache_evict(ctkvr_cache *c, const float *weights_in, int32_t weights_stride, const int32_t *cur_lens, const int32_t *block_table,
                       int32_t budget, int32_t n_init, int32_t n_local, void *k_pages, void *v_pages, float *weights_out, int32_t *out_ids,
                       int32_t *out_lens, void *hip_stream);
+
+/* ---- the paged KV cache in 8 bits, in a window, with drafted tokens ------------------------------------ */
+/*
+ * Rows of 8 bits.  k_codes and v_codes [num_pages][g][page_size][128] hold a byte an element, k_scales and v_scales [num_pages][g][page_size] an fp32
+ * scale a row: element i of a row is its code times its scale.  A row x is held as
+ *   scale = max |x_i| / top,  code_i = x_i * top / max |x_i| to the nearest code, ties to even;  top = 127 (int8, -127 to 127) or 448 (e4m3),
+ * computed in fp32: a value is off by half a step of its row at most, max |x_i| / 254, or in e4m3 by 2^-4 of itself (from max |x_i| * 2^-14.8 on; below by
+ * max |x_i| * 2^-18.8).  A row that holds an infinity or NaN is NaN as a whole, with codes of 0 and a scale of NaN.  e4m3's codes for NaN are written by no
+ * call; what they are read as is not said.
+ * The calls below follow ctkvr_cache_*'s rules for tokens, rows, pages, streams, graphs and the workspace (which every attention uses), and take the
+ * same handle, whose dtype is that of q, k, v, out and of plain rows.
+ */
+typedef enum { CTKVR_KV_PLAIN = 0, CTKVR_KV_INT8 = 1, CTKVR_KV_FP8 = 2 } ctkvr_kv_format;
+
+/* ctkvr_cache_append into rows of 8 bits (format: INT8 or FP8).  Keys are rotated in fp32 and rounded once, to their codes; q and q_out may both be NULL, k and v
+ * may not.  No two sequences may write into one page's slot.  Errors: EINVAL. */
+int ctkvr_cache_quant_append(ctkvr_cache *c, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                             const int32_t *positions, const int32_t *cu_new, const int32_t *cur_lens, const int32_t *block_table, int32_t total,
+                             void *q_out, int32_t format, void *k_codes, float *k_scales, void *v_codes, float *v_scales, void *hip_stream);
+
+/*
+ * Read rows of 8 bits back into plain pages, of which the index, the decode step, the weights and eviction read: token t of sequence b, first_tokens[b] <= t <
+ * cur_lens[b], goes to slot t - first_tokens[b] of out_table's row b, code times scale in fp32, rounded once to `dtype`.
+ *   first_tokens  DEVICE int32 [batch] or NULL: zeros (negative ones count as 0).
+ *   out_table     DEVICE int32 [batch][out_max_pages], pages 0 .. out_num_pages - 1 of k_pages and v_pages [out_num_pages][g][page_size][128], of the handle's
+ *                 page_size.  Rows from or to a page that is none are left out, and tokens beyond either table.  No two tokens may go to one slot.
+ *   k_pages       or v_pages may be NULL: not read, nor its codes and scales.
+ * Errors: EINVAL.
+ */
+int ctkvr_cache_quant_read(ctkvr_cache *c, int32_t format, const void *k_codes, const float *k_scales, const void *v_codes, const float *v_scales,
+                           const int32_t *first_tokens, const int32_t *cur_lens, const int32_t *block_table, const int32_t *out_table, int32_t out_max_pages,
+                           int32_t out_num_pages, void *k_pages, void *v_pages, void *hip_stream);
+
+/* ctkvr_cache_attn over rows of 8 bits (format: INT8 or FP8): the same scores, masks and results, on the values that the codes stand for.  Queries are
+ * not rounded; with bf16 data a probability times its value's scale enters the product rounded to bf16.  Errors: EINVAL. */
+int ctkvr_cache_quant_attn(ctkvr_cache *c, const void *q, int64_t q_stride, int32_t format, const void *k_codes, const float *k_scales, const void *v_codes,
+                           const float *v_scales, const int32_t *cu_new, const int32_t *cur_lens, const int32_t *block_table, int32_t total,
+                           const float *slopes, const int32_t *prefix_lens, const int32_t *first_key, void *out, float *out_lse, void *hip_stream);
+
+/*
+ * ctkvr_cache_attn in a sliding window beside the first tokens: the token at pos sees key t where
+ *   t <= pos  and  (t > pos - window or t < n_sink),
+ * over plain rows (format PLAIN, scales NULL) or rows of 8 bits.  What it costs goes by the window, not by the cache.  Pages that lie before every
+ * window of a sequence and behind its first n_sink tokens are not needed any more: their entries of the table may be -1, or pages of other sequences.
+ *   window  1 or more (the token itself counts);  n_sink  0 or more.
+ * Errors: EINVAL.
+ */
+int ctkvr_cache_window_attn(ctkvr_cache *c, const void *q, int64_t q_stride, int32_t format, const void *k_pages, const float *k_scales, const void *v_pages,
+                            const float *v_scales, const int32_t *cu_new, const int32_t *cur_lens, const int32_t *block_table, int32_t total, int32_t window,
+                            int32_t n_sink, const float *slopes, void *out, float *out_lse, void *hip_stream);
+
+/*
+ * Attention of drafted tokens that branch: the new tokens of a sequence are a tree (or any order), each in a slot of its own, of which token i sees the
+ * keys before the new tokens, from its first_key on, and those new tokens whose bits it has:
+ *   tree_mask  DEVICE uint32 [total][mask_words]: bit j % 32 of word j / 32 of a token's row says that it sees the j-th new token of its sequence (itself
+ *              only with its own bit; tokens beyond 32 * mask_words are not seen).
+ *   first_key  DEVICE int32 [total] or NULL: it sees no key, new ones included, in an earlier slot.
+ * Over plain rows (format PLAIN, scales NULL) or rows of 8 bits.  The cache was appended to with the draft's own positions (a token's depth in its tree behind the
+ * tokens before it); the tokens that are kept in the end go to their slots in order by another append, of their k and v, with cur_lens counting them alone.
+ * A token that sees no key gets zeros and -infinity.  Errors: EINVAL.
+ */
+int ctkvr_cache_tree_attn(ctkvr_cache *c, const void *q, int64_t q_stride, int32_t format, const void *k_pages, const float *k_scales, const void *v_pages,
+                          const float *v_scales, const int32_t *cu_new, const int32_t *cur_lens, const int32_t *block_table, int32_t total,
+                          const uint32_t *tree_mask, int32_t mask_words, const int32_t *first_key, void *out, float *out_lse, void *hip_stream);
 
 /* ---- inspection (tests, tooling); each synchronises ----------------------- */
 typedef struct {

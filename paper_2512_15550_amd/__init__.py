@@ -13,4 +13,6 @@ from .binding import (CtkvrError, Index, Params, ctkvr_build_index, ctkvr_decode
                       ctkvr_centroid_update, ctkvr_decode_step_window, ctkvr_decode_step_static,
                       ctkvr_index_set_decode_path, ctkvr_index_decode_path, ctkvr_index_check, ctkvr_index_build_route, ctkvr_profile_phases,
                       ctkvr_measure_dispatch_floor, ctkvr_release_scratch, PATH_AUTO, PATH_STAGED, PATH_FUSED, Cache, CacheParams,
-                      ctkvr_cache_create, ctkvr_cache_free, ctkvr_cache_append, ctkvr_cache_attn, ctkvr_cache_weights, ctkvr_cache_evict)
+                      ctkvr_cache_create, ctkvr_cache_free, ctkvr_cache_append, ctkvr_cache_attn, ctkvr_cache_weights, ctkvr_cache_evict,
+                      ctkvr_cache_quant_append, ctkvr_cache_quant_read, ctkvr_cache_quant_attn, ctkvr_cache_window_attn, ctkvr_cache_tree_attn,
+                      KV_PLAIN, KV_INT8, KV_FP8)

@@ -16,6 +16,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libctkvr.so")
 
 F32, BF16 = 0, 1
+KV_PLAIN, KV_INT8, KV_FP8 = 0, 1, 2
 LAST_C, KMEANS = 0, 1
 BUILD_EXACT, BUILD_MFMA = 0, 1
 
@@ -86,7 +87,8 @@ EXPORTS = ["ctkvr_build_index", "ctkvr_index_load", "ctkvr_decode_step", "ctkvr_
            "ctkvr_profile_enable", "ctkvr_profile_collect", "ctkvr_centroid_update", "ctkvr_decode_step_window",
            "ctkvr_selftest_exp", "ctkvr_decode_step_static", "ctkvr_index_set_decode_path", "ctkvr_index_decode_path",
            "ctkvr_index_check", "ctkvr_profile_phases", "ctkvr_measure_dispatch_floor", "ctkvr_index_build_route", "ctkvr_release_scratch",
-           "ctkvr_cache_create", "ctkvr_cache_free", "ctkvr_cache_append", "ctkvr_cache_attn", "ctkvr_cache_weights", "ctkvr_cache_evict"]
+           "ctkvr_cache_create", "ctkvr_cache_free", "ctkvr_cache_append", "ctkvr_cache_attn", "ctkvr_cache_weights", "ctkvr_cache_evict",
+           "ctkvr_cache_quant_append", "ctkvr_cache_quant_read", "ctkvr_cache_quant_attn", "ctkvr_cache_window_attn", "ctkvr_cache_tree_attn"]
 PATH_AUTO, PATH_STAGED, PATH_FUSED = 0, 1, 2
 N_STAGES = 9
 STAGE_NAMES = ["centroid_cos", "recall_gather", "score", "denom", "keyhist", "classify",
@@ -161,6 +163,15 @@ def load_library() -> ctypes.CDLL:
     L.ctkvr_cache_weights.argtypes = [vp, vp, i64, fp, vp, ip, ip, ip, i32, fp, ip, ip, f32, fp, fp, i32, vp]
     L.ctkvr_cache_evict.restype = ctypes.c_int
     L.ctkvr_cache_evict.argtypes = [vp, fp, i32, ip, ip, i32, i32, i32, vp, vp, fp, ip, ip, vp]
+    rows = [i32, vp, fp, vp, fp]   # format, codes or pages and scales of K and of V
+    L.ctkvr_cache_quant_append.argtypes = [vp, vp, i64, vp, i64, vp, i64, ip, ip, ip, ip, i32, vp, *rows, vp]
+    L.ctkvr_cache_quant_read.argtypes = [vp, *rows, ip, ip, ip, ip, i32, i32, vp, vp, vp]
+    L.ctkvr_cache_quant_attn.argtypes = [vp, vp, i64, *rows, ip, ip, ip, i32, fp, ip, ip, vp, fp, vp]
+    L.ctkvr_cache_window_attn.argtypes = [vp, vp, i64, *rows, ip, ip, ip, i32, i32, i32, fp, vp, fp, vp]
+    L.ctkvr_cache_tree_attn.argtypes = [vp, vp, i64, *rows, ip, ip, ip, i32, ip, i32, ip, vp, fp, vp]
+    for name in ("append", "read", "attn"):
+        getattr(L, "ctkvr_cache_quant_" + name).restype = ctypes.c_int
+    L.ctkvr_cache_window_attn.restype = L.ctkvr_cache_tree_attn.restype = ctypes.c_int
     _lib = L
     return L
 
@@ -424,7 +435,8 @@ class Cache:
         self._lib = load_library()
         self._int, self._float = torch.int32, torch.float32
         self._shapes = {"pages": (p.num_pages, p.n_kv_heads, p.page_size, 128), "cu": (p.batch + 1,), "batch": (p.batch,),
-                        "table": (p.batch, p.max_pages), "heads": (p.n_q_heads,)}
+                        "table": (p.batch, p.max_pages), "heads": (p.n_q_heads,), "scales": (p.num_pages, p.n_kv_heads, p.page_size)}
+        self._formats = {self.torch_dtype: KV_PLAIN, torch.int8: KV_INT8, torch.float8_e4m3fn: KV_FP8}
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self._stream = raw if raw is not None else (lambda d: torch.cuda.current_stream(d).cuda_stream)
 
@@ -549,3 +561,79 @@ def ctkvr_cache_evict(cache: Cache, weights_in, k_pages, v_pages, cur_lens, bloc
         _on(cache, "weights_out", weights_out, cache._float, shape),
         _on(cache, "out_ids", out_ids, cache._int, (p.batch, p.n_kv_heads, int(budget))),
         _on(cache, "out_lens", out_lens, cache._int, cache._shapes["batch"]), cache.stream()))
+
+
+# ---- the paged KV cache in 8 bits, in a window, with drafted tokens ---------------
+def _format_of(cache: Cache, k, plain=False) -> int:
+    """What rows of k's type are: int8 or e4m3 codes, or plain rows where those are taken."""
+    f = cache._formats.get(k.dtype, -1)
+    if f < 0 or (f == KV_PLAIN and not plain):
+        raise ValueError(f"rows of {k.dtype}: expected torch.int8 or torch.float8_e4m3fn codes" + (f", or plain rows of {cache.torch_dtype}" if plain else ""))
+    return f
+
+
+def _quant_on(cache: Cache, format, k, k_scales, v, v_scales):
+    """Format, codes (or plain pages) and scales of K and of V; None passes NULL."""
+    dtype = (k if k is not None else v).dtype
+    return (format, _on(cache, "k", k, dtype, cache._shapes["pages"]), _on(cache, "k_scales", k_scales, cache._float, cache._shapes["scales"]),
+            _on(cache, "v", v, dtype, cache._shapes["pages"]), _on(cache, "v_scales", v_scales, cache._float, cache._shapes["scales"]))
+
+
+def ctkvr_cache_quant_append(cache: Cache, q, k, v, cu_new, cur_lens, block_table, q_out, k_codes, k_scales, v_codes, v_scales, positions=None) -> None:
+    """As ``ctkvr_cache_append``; the codes are torch.int8 or torch.float8_e4m3fn, the scales fp32 [num_pages][g][page].  q and q_out may be None."""
+    p, total = cache.params, k.shape[0]
+    cu, cur, table = _batch_on(cache, cu_new, cur_lens, block_table)
+    (qp, qs), (kp, ks) = _rows_on(cache, "q", q, total, p.n_q_heads), _rows_on(cache, "k", k, total, p.n_kv_heads)
+    vp, vs = _rows_on(cache, "v", v, total, p.n_kv_heads)
+    _check(cache._lib.ctkvr_cache_quant_append(
+        cache.handle, qp, qs, kp, ks, vp, vs, _on(cache, "positions", positions, cache._int, (cache.n_axes, total)), cu, cur, table, total,
+        _on(cache, "q_out", q_out, cache.torch_dtype, (total, p.n_q_heads, 128)),
+        *_quant_on(cache, _format_of(cache, k_codes), k_codes, k_scales, v_codes, v_scales), cache.stream()))
+
+
+def ctkvr_cache_quant_read(cache: Cache, k_codes, k_scales, v_codes, v_scales, cur_lens, block_table, out_table, k_pages, v_pages, first_tokens=None) -> None:
+    """Into plain pages [any number][g][page][128] by out_table int32 [batch][any number]; codes, scales and pages of K, or of V, may be None."""
+    s, some = cache._shapes, k_pages if k_pages is not None else v_pages
+    shape = (some.shape[0],) + s["pages"][1:]
+    _check(cache._lib.ctkvr_cache_quant_read(
+        cache.handle, *_quant_on(cache, _format_of(cache, k_codes if k_codes is not None else v_codes), k_codes, k_scales, v_codes, v_scales),
+        _on(cache, "first_tokens", first_tokens, cache._int, s["batch"]), _on(cache, "cur_lens", cur_lens, cache._int, s["batch"]),
+        _on(cache, "block_table", block_table, cache._int, s["table"]),
+        _on(cache, "out_table", out_table, cache._int, (cache.params.batch, out_table.shape[-1])), out_table.shape[-1], shape[0],
+        _on(cache, "k_pages", k_pages, cache.torch_dtype, shape), _on(cache, "v_pages", v_pages, cache.torch_dtype, shape), cache.stream()))
+
+
+def ctkvr_cache_quant_attn(cache: Cache, q, k_codes, k_scales, v_codes, v_scales, cu_new, cur_lens, block_table, out, out_lse=None, slopes=None,
+                           prefix_lens=None, first_key=None) -> None:
+    h, total = cache.params.n_q_heads, q.shape[0]
+    cu, cur, table = _batch_on(cache, cu_new, cur_lens, block_table)
+    qp, qs = _rows_on(cache, "q", q, total, h)
+    _check(cache._lib.ctkvr_cache_quant_attn(
+        cache.handle, qp, qs, *_quant_on(cache, _format_of(cache, k_codes), k_codes, k_scales, v_codes, v_scales), cu, cur, table, total,
+        *_masks_on(cache, total, slopes, prefix_lens, first_key), _on(cache, "out", out, cache.torch_dtype, (total, h, 128)),
+        _on(cache, "out_lse", out_lse, cache._float, (total, h)), cache.stream()))
+
+
+def ctkvr_cache_window_attn(cache: Cache, q, k_pages, v_pages, cu_new, cur_lens, block_table, window, out, n_sink=0, out_lse=None, slopes=None,
+                            k_scales=None, v_scales=None) -> None:
+    """k_pages and v_pages are plain, or codes with their scales."""
+    h, total = cache.params.n_q_heads, q.shape[0]
+    cu, cur, table = _batch_on(cache, cu_new, cur_lens, block_table)
+    qp, qs = _rows_on(cache, "q", q, total, h)
+    _check(cache._lib.ctkvr_cache_window_attn(
+        cache.handle, qp, qs, *_quant_on(cache, _format_of(cache, k_pages, True), k_pages, k_scales, v_pages, v_scales), cu, cur, table, total, int(window),
+        int(n_sink), _on(cache, "slopes", slopes, cache._float, cache._shapes["heads"]), _on(cache, "out", out, cache.torch_dtype, (total, h, 128)),
+        _on(cache, "out_lse", out_lse, cache._float, (total, h)), cache.stream()))
+
+
+def ctkvr_cache_tree_attn(cache: Cache, q, k_pages, v_pages, cu_new, cur_lens, block_table, tree_mask, out, out_lse=None, first_key=None, k_scales=None,
+                          v_scales=None) -> None:
+    """tree_mask: int32 [total][words], 32 drafted tokens a word; k_pages and v_pages are plain, or codes with their scales."""
+    h, total = cache.params.n_q_heads, q.shape[0]
+    cu, cur, table = _batch_on(cache, cu_new, cur_lens, block_table)
+    qp, qs = _rows_on(cache, "q", q, total, h)
+    words = tree_mask.shape[-1]
+    _check(cache._lib.ctkvr_cache_tree_attn(
+        cache.handle, qp, qs, *_quant_on(cache, _format_of(cache, k_pages, True), k_pages, k_scales, v_pages, v_scales), cu, cur, table, total,
+        _on(cache, "tree_mask", tree_mask, cache._int, (total, words)), words, _on(cache, "first_key", first_key, cache._int, (total,)),
+        _on(cache, "out", out, cache.torch_dtype, (total, h, 128)), _on(cache, "out_lse", out_lse, cache._float, (total, h)), cache.stream()))

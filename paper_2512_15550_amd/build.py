@@ -1,11 +1,12 @@
-"""Compile the HIP library for gfx950 with hipcc, in-tree: three translation units (the host side with
-the staged and build kernels; the single-launch decode kernel; the operators on the paged KV cache), compiled side by side, then linked."""
+"""Compile the HIP library for gfx950 with hipcc, in-tree: six translation units (the host side with the staged and build kernels; the
+single-launch decode kernel; the operators on the paged KV cache; those on 8-bit rows, windows and drafts, whose attention over 8-bit rows has one for
+each type of query), compiled side by side, then linked."""
 import os
 import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = ["ctkvr.hip", "fused.hip", "cache.hip"]
+SOURCES = ["ctkvr.hip", "fused.hip", "cache.hip", "quant.hip", "quant_bf16.hip", "quant_f32.hip"]
 LIB = os.path.join(HERE, "libctkvr.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 

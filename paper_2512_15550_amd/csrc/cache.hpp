@@ -175,7 +175,7 @@ template <int OPT> __device__ __forceinline__ void score_regs(f32x16_t &s, const
     }
 }
 
-__global__ void cache_clear_kernel(uint32_t *p, size_t n)
+static __global__ void cache_clear_kernel(uint32_t *p, size_t n)
 {
     const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (i < n) p[i] = 0;
@@ -229,12 +229,13 @@ template <typename T, int KEYS, int THREADS> struct OddValues {
             w[i * THREADS] = x;
         }
     }
-    static __device__ __forceinline__ void add(f32x16_t (&o)[4], const char *vt, const RowSight &sight, int key0, uint64_t bad, int half)
+    // sees(k): whether the lane's row sees key k of the tile
+    template <typename F> static __device__ __forceinline__ void add(f32x16_t (&o)[4], const char *vt, int half, F sees_key)
     {
         for (int n = 0; n < KEYS; ++n) {
             int k = n;
             asm volatile("" : "+s"(k));   // (its addresses are not worth registers in the loop over the tiles)
-            const bool sees = key0 + k >= sight.lo && key0 + k < sight.hi && !((bad >> k) & 1);
+            const bool sees = sees_key(k);
 #pragma unroll
             for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -264,6 +265,14 @@ __device__ __forceinline__ void mask_regs(f32x16_t &s, const RowSight &sight, in
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = (mine >> (8 * (i >> 2) + (i & 3))) & 1 ? none : s[i];
     }
+}
+
+// ... and where that is not a range
+__device__ __forceinline__ void mask_bits(f32x16_t &s, uint32_t seen, int half, float none)
+{
+    const uint32_t mine = seen >> (4 * half);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = (mine >> (8 * (i >> 2) + (i & 3))) & 1 ? s[i] : none;
 }
 
 // A tile's scores to probabilities under the running maximum m (in units of log2 e, as all exponents here), their sum to l, the outputs so far to the
@@ -351,6 +360,15 @@ __device__ __forceinline__ KeyRange key_range(const SeqSpan &s, int prefix, int 
     r.all_hi = pos0 < 0 ? 0 : min(max(pos0 + 1, prefix), s.len);
     return r;
 }
+template <int SIGHT> __device__ __forceinline__ KeyRange key_range_of(const SeqSpan &s, int prefix, int tok0, int tok1)
+{
+    KeyRange r = key_range(s, SIGHT == kRange ? prefix : 0, tok0, tok1);
+    if constexpr (SIGHT == kTree) {
+        r.hi = s.old + tok1 < 0 ? 0 : s.len;
+        r.all_hi = s.old + tok0 < 0 ? 0 : min(s.old, s.len);
+    }
+    return r;
+}
 
 template <typename T> __device__ __forceinline__ void store4(T *p, const f32x4_t &x)
 {
@@ -385,8 +403,36 @@ __device__ __forceinline__ float handed(const float *p) { return __hip_atomic_lo
 __device__ __forceinline__ float inv_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }   // (NaN stays)
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2; }
 
+// A row's outputs, or its run's, from its sum l and maximum m
+template <typename T>
+__device__ __forceinline__ void many_finish(const AttnArgs &a, const SeqSpan &s, int split, bool empty, bool live, int token, int head, float m, float l,
+                                            const f32x16_t (&o)[4], int half)
+{
+    const CacheView &v = a.v;
+    if (!live) return;
+    const float inv = inv_sum(l), lse = lse_of(m, l);
+    const size_t at_row = (size_t)(s.c0 + token) * v.h + head;
+    const size_t n = (size_t)split * v.total * v.h + at_row;
+    if (half == 0) {
+        if (a.nsplit > 1) a.part_lse[n] = lse;
+        else if (a.lse) a.lse[at_row] = lse;
+    }
+    if (a.nsplit > 1 && empty) return;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int d = 32 * db + 8 * i + 4 * half;
+            f32x4_t x;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) x[c] = o[db][4 * i + c] * inv;
+            if (a.nsplit > 1) store4(a.part_o + n * 128 + d, x);
+            else store4((T *)a.out + at_row * 128 + d, x);
+        }
+}
+
 // Many rows: one block a tile of 32 NW rows of a unit and, where the keys are split, one of nsplit runs of them; a wave has 32 rows.  Each tile of keys goes straight to shared memory while the one before it is worked on; the maximum runs with them.
-template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void attn_kernel(AttnArgs a)
+template <typename T, int OPT, int NW, int SIGHT = kRange> __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void attn_kernel(AttnArgs a)
 {
     constexpr int kRowsLog = NW == 4 ? 7 : 8, kKeys = RowTile<T>::kRows, kBlocks = kKeys / 32, kTile = RowTile<T>::kBytes;
     constexpr int kPer = RowTile<T>::kRowsPerLoad, kLoads = kKeys / (NW * kPer);   // loads a wave makes of a tile of K, and of V
@@ -403,14 +449,18 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
     const int rows = s.n << v.lg, r0 = at << kRowsLog, row = r0 + 32 * wave + (lane & 31);
     const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
     const int token = min(row, rows - 1) >> v.lg, head = (kv << v.lg) + (min(row, rows - 1) & ((1 << v.lg) - 1));
-    const RowSight sight = row_sight(v, a.o, s, prefix, token);
+    const RowSight sight = sight_of<SIGHT>(v, a.o, s, prefix, token);
 
     Operand<T> q;
     load_operand(q, (const T *)a.q + (int64_t)(s.c0 + token) * a.q_stride + head * 128, half);
 
-    const KeyRange range = key_range(s, prefix, r0 >> v.lg, (min(r0 + 32 * NW, rows) - 1) >> v.lg);
+    const int tok0 = r0 >> v.lg, tok1 = (min(r0 + 32 * NW, rows) - 1) >> v.lg;
+    const KeyRange range = key_range_of<SIGHT>(s, prefix, tok0, tok1);
     int k_lo = 0, all_lo = 0;
-    if (a.o.first) {
+    if (SIGHT == kWindow) {
+        k_lo = max(s.old + tok0 + 1 - a.o.window, 0);
+        all_lo = max(s.old + tok1 + 1 - a.o.window, 0);
+    } else if (a.o.first) {
         int lo = sight.lo, hi = sight.lo;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -433,6 +483,13 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
         __syncthreads();
     }
     int t0 = k_lo / kKeys, t1 = range.hi > k_lo ? (range.hi + kKeys - 1) / kKeys : t0;
+    KeyTiles kt{};
+    if constexpr (SIGHT == kWindow) {
+        kt = window_tiles(a.o, k_lo, range.hi, kKeys);
+        t0 = kt.from;
+        t1 = kt.to;
+    }
+    auto tile_of = [&](int i) { return SIGHT == kWindow ? kt.at(i) : i; };
     if (a.nsplit > 1) {   // this block's run of them: as many runs as there are eight tiles for
         const int n = t1 - t0, used = max(1, min(a.nsplit, n / 8)), at_run = min(split, used);
         const int from = (int)((int64_t)n * at_run / used), to = (int)((int64_t)n * min(at_run + 1, used) / used);
@@ -496,14 +553,21 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
     auto step = [&](auto buf, auto masked, int t) {
         const uint64_t bad_next = bad;
         if (t + 1 < t1) {
-            fetch(buf ^ 1, next, bad == 0 && (t + 2) * kKeys <= range.hi);
-            if (t + 2 < t1) next = rows_of(t + 2);
+            fetch(buf ^ 1, next, bad == 0 && (tile_of(t + 1) + 1) * kKeys <= range.hi);
+            if (t + 2 < t1) next = rows_of(tile_of(t + 2));
         }
         char *kt = smem[buf][0], *vt = smem[buf][1];
-        const int key0 = t * kKeys;
+        const int key0 = tile_of(t) * kKeys;
         if constexpr (decltype(masked)::value) {
             if (__syncthreads_or(Odd::any(vt, threadIdx.x))) {
-                Odd::add(o, vt, sight, key0, bad_now, half);
+                if constexpr (SIGHT == kRange) {
+                    Odd::add(o, vt, half, [&](int k) { return key0 + k >= sight.lo && key0 + k < sight.hi && !((bad_now >> k) & 1); });
+                } else {
+                    uint64_t seen = sight_bits<SIGHT>(a.o, s, sight, token, key0);
+                    if (kBlocks > 1) seen |= (uint64_t)sight_bits<SIGHT>(a.o, s, sight, token, key0 + 32) << 32;
+                    seen &= ~bad_now;
+                    Odd::add(o, vt, half, [&](int k) { return (bool)((seen >> k) & 1); });
+                }
                 __syncthreads();
                 Odd::clean(vt, threadIdx.x);
                 __syncthreads();
@@ -515,7 +579,11 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
 #pragma unroll
         for (int kb = 0; kb < kBlocks; ++kb) {
             score_regs<OPT>(sc[kb], a.o, slope2, sight.pos - (key0 + 32 * kb), half);
-            if constexpr (decltype(masked)::value) mask_regs(sc[kb], sight, key0 + 32 * kb, (uint32_t)(bad_now >> (32 * kb)), half, -INFINITY);
+            if constexpr (decltype(masked)::value) {
+                const uint32_t none = (uint32_t)(bad_now >> (32 * kb));
+                if constexpr (SIGHT == kRange) mask_regs(sc[kb], sight, key0 + 32 * kb, none, half, -INFINITY);
+                else mask_bits(sc[kb], sight_bits<SIGHT>(a.o, s, sight, token, key0 + 32 * kb) & ~none, half, -INFINITY);
+            }
         }
         softmax_regs<OPT, kBlocks>(sc, o, m, l, a.o.c2);
         values_dot<T, kBlocks>(o, vt, sc, lane);
@@ -524,14 +592,17 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
         __syncthreads();
     };
     if (t0 < t1) {
-        const uint32_t r = rows_of(t0);
+        const uint32_t r = rows_of(tile_of(t0));
         bad_now = bad;
-        fetch(0, r, bad == 0 && (t0 + 1) * kKeys <= range.hi);
-        if (t0 + 1 < t1) next = rows_of(t0 + 1);
+        fetch(0, r, bad == 0 && (tile_of(t0) + 1) * kKeys <= range.hi);
+        if (t0 + 1 < t1) next = rows_of(tile_of(t0 + 1));
         loads_landed<0>();
         __syncthreads();
     }
-    auto seen_by_all = [&](int t, uint64_t none) { return (t + 1) * kKeys <= range.all_hi && t * kKeys >= all_lo && none == 0; };
+    auto seen_by_all = [&](int i, uint64_t none) {
+        const int t = tile_of(i);
+        return (t + 1) * kKeys <= range.all_hi && (t * kKeys >= all_lo || (SIGHT == kWindow && (t + 1) * kKeys <= a.o.sinks)) && none == 0;
+    };
     int t = t0;
     while (t < t1) {
         // (two at a time: where a tile is in shared memory is then part of the instructions)
@@ -546,32 +617,128 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
         ++t;
     }
 
+    many_finish<T>(a, s, split, t0 == t1, row < rows, token, head, m, half_sum(l), o, half);
+}
+
+// The end of a tile of few rows: its waves' maxima, sums and outputs become one, the rows' or this run's, and the run that ends last joins the runs.
+// smem: 32 rows of fp32 outputs a wave.
+template <typename T, int NW>
+__device__ __forceinline__ void few_finish(const AttnArgs &a, const SeqSpan &s, int kv, int r0, int have, int tile, int split, int used, bool whole, float m,
+                                           float l, const f32x16_t (&o)[4], char *smem, float (&join)[NW][2][32], bool *last)
+{
+    const CacheView &v = a.v;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    auto row_out = [&](int r) { return (size_t)(s.c0 + ((r0 + r) >> v.lg)) * v.h + (kv << v.lg) + ((r0 + r) & ((1 << v.lg) - 1)); };
+    // the waves' outputs to one maximum, through shared memory (16-byte chunks at chunk ^ row)
     l = half_sum(l);
-    if (row >= rows) return;
-    const float inv = inv_sum(l), lse = lse_of(m, l);
-    const size_t at_row = (size_t)(s.c0 + token) * v.h + head;
-    const size_t n = (size_t)split * v.total * v.h + at_row;
     if (half == 0) {
-        if (a.nsplit > 1) a.part_lse[n] = lse;
-        else if (a.lse) a.lse[at_row] = lse;
+        join[wave][0][lane] = m;
+        join[wave][1][lane] = l;
     }
-    if (a.nsplit > 1 && t0 == t1) return;
+    loads_landed<0>();
+    __syncthreads();   // (and nobody needs its values any more)
+    const int r32 = lane & 31;
+    float top = join[0][0][r32];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) top = fmaxf(top, join[w][0][r32]);
+    const float scale = m == -INFINITY ? 1.0f : exp2_fast(m - top);
+    char *mine = smem + wave * 32 * 512;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int d = 32 * db + 8 * i + 4 * half;
             f32x4_t x;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) x[c] = o[db][4 * i + c] * inv;
-            if (a.nsplit > 1) store4(a.part_o + n * 128 + d, x);
-            else store4((T *)a.out + at_row * 128 + d, x);
+            for (int c = 0; c < 4; ++c) x[c] = o[db][4 * i + c] * scale;
+            *reinterpret_cast<f32x4_t *>(mine + r32 * 512 + (((8 * db + 2 * i + half) ^ r32) << 4)) = x;
         }
+    __syncthreads();
+    for (int j = threadIdx.x; j < have * 32; j += 64 * NW) {   // (row, four elements)
+        const int r = j >> 5, c = j & 31;
+        float t = join[0][0][r], sum = 0.0f;
+#pragma unroll
+        for (int w = 1; w < NW; ++w) t = fmaxf(t, join[w][0][r]);
+        f32x4_t x = {};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float mw = join[w][0][r];
+            sum += join[w][1][r] * (mw == -INFINITY ? 1.0f : exp2_fast(mw - t));
+            x += *reinterpret_cast<const f32x4_t *>(smem + w * 32 * 512 + r * 512 + ((c ^ r) << 4));
+        }
+        x *= inv_sum(sum);
+        const float lse = lse_of(t, sum);
+        const size_t at_row = row_out(r);
+        if (!whole) {
+            const size_t n = (size_t)split * v.total * v.h + at_row;
+            if (a.done) {
+                if (c == 0) hand_over(a.part_lse + n, lse);
+                hand_over(a.part_o + n * 128 + 4 * c, x);
+            } else {
+                if (c == 0) a.part_lse[n] = lse;
+                store4(a.part_o + n * 128 + 4 * c, x);
+            }
+        } else {
+            if (c == 0 && a.lse) a.lse[at_row] = lse;
+            store4((T *)a.out + at_row * 128 + 4 * c, x);
+        }
+    }
+    if (whole || !a.done) return;
+
+    // The run that ends last joins the tile's runs, in their order, by their log-sum-exps: 32 lanes a row, four elements a lane, and where the
+    // rows are few several such groups a row, that take the runs in turn.
+    loads_landed<0>();   // (stores too)
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        uint32_t *done = a.done + (size_t)tile * v.g + kv;
+        *last = atomicAdd(done, 1u) == (uint32_t)used - 1;
+        if (*last) *done = 0;
+    }
+    __syncthreads();
+    if (!*last) return;
+    constexpr int kGroups = 2 * NW;
+    f32x4_t(*sums)[33] = reinterpret_cast<f32x4_t(*)[33]>(smem);   // [group][lane, or the weights' sum]
+    int ways = kGroups;
+    while (ways > 1 && ways * have > kGroups) ways >>= 1;
+    const int group = threadIdx.x >> 5, l32 = threadIdx.x & 31, way = group % ways;
+    const size_t step = (size_t)v.total * v.h;
+    for (int base = 0; base < have; base += kGroups / ways) {
+        const int r = base + group / ways;
+        f32x4_t x = {};
+        float top_lse = -INFINITY, sum = 0.0f, ref = 0.0f;
+        if (r < have) {
+            const float *lses = a.part_lse + row_out(r), *outs = a.part_o + row_out(r) * 128 + 4 * l32;
+            for (int i = l32; i < used; i += 32) top_lse = fmaxf(top_lse, handed(lses + i * step));
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) top_lse = fmaxf(top_lse, __shfl_xor(top_lse, d));
+            ref = top_lse == -INFINITY ? 0.0f : top_lse;
+#pragma unroll 8
+            for (int i = way; i < used; i += ways) {
+                const float w = exp2_fast((handed(lses + i * step) - ref) * kLog2e);
+                sum += w;
+                x += handed4(outs + i * step * 128) * w;
+            }
+        }
+        if (ways > 1) {
+            sums[group][l32] = x;
+            if (l32 == 0) sums[group][32][0] = sum;
+            __syncthreads();
+            if (way == 0)
+                for (int w = 1; w < ways; ++w) {
+                    x += sums[group + w][l32];
+                    sum += sums[group + w][32][0];
+                }
+            __syncthreads();
+        }
+        if (r < have && way == 0) {
+            if (l32 == 0 && a.lse) a.lse[row_out(r)] = sum == 0.0f ? -INFINITY : ref + __builtin_amdgcn_logf(sum) * kLn2;
+            store4((T *)a.out + row_out(r) * 128 + 4 * l32, x * inv_sum(sum));
+        }
+    }
 }
 
 // Few rows: one block a tile of 32 rows and a run of their keys, which its waves share out, each with a maximum and outputs of its own until
 // they are joined at the end; no wave waits for another before that.  Keys go to registers as operands, values to shared memory, a tile of 32 ahead.
-template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void attn_few_kernel(AttnArgs a)
+template <typename T, int OPT, int NW, int SIGHT = kRange> __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void attn_few_kernel(AttnArgs a)
 {
     constexpr int kTile = 32 * RowTile<T>::kRowBytes, kPer = RowTile<T>::kRowsPerLoad, kLoads = 32 / kPer;
     using Odd = OddValues<T, 32, 64>;
@@ -587,14 +754,18 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
     const int rows = s.n << v.lg, r0 = at << 5, row = r0 + (lane & 31);
     const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
     const int token = min(row, rows - 1) >> v.lg, head = (kv << v.lg) + (min(row, rows - 1) & ((1 << v.lg) - 1));
-    const RowSight sight = row_sight(v, a.o, s, prefix, token);
+    const RowSight sight = sight_of<SIGHT>(v, a.o, s, prefix, token);
 
     Operand<T> q;
     load_operand(q, (const T *)a.q + (int64_t)(s.c0 + token) * a.q_stride + head * 128, half);
 
-    const KeyRange range = key_range(s, prefix, r0 >> v.lg, (min(r0 + 32, rows) - 1) >> v.lg);
+    const int tok0 = r0 >> v.lg, tok1 = (min(r0 + 32, rows) - 1) >> v.lg;
+    const KeyRange range = key_range_of<SIGHT>(s, prefix, tok0, tok1);
     int k_lo = 0, all_lo = 0;
-    if (a.o.first) {
+    if (SIGHT == kWindow) {
+        k_lo = max(s.old + tok0 + 1 - a.o.window, 0);
+        all_lo = max(s.old + tok1 + 1 - a.o.window, 0);
+    } else if (a.o.first) {
         k_lo = all_lo = sight.lo;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -602,7 +773,15 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
             all_lo = max(all_lo, __shfl_xor(all_lo, d));
         }
     }
-    const int first_tile = k_lo / 32, tiles = range.hi > k_lo ? (range.hi + 31) / 32 - first_tile : 0, have = min(32, rows - r0);
+    int first_tile = k_lo / 32, tiles = range.hi > k_lo ? (range.hi + 31) / 32 - first_tile : 0;
+    KeyTiles kt{};
+    if constexpr (SIGHT == kWindow) {
+        kt = window_tiles(a.o, k_lo, range.hi, 32);
+        first_tile = kt.from;
+        tiles = kt.to;
+    }
+    auto tile_of = [&](int i) { return SIGHT == kWindow ? kt.at(i) : i; };
+    const int have = min(32, rows - r0);
     // as many of the runs as the keys are worth: two tiles a wave (in fp32 one) at least; the other blocks have nothing to do
     const int per = sizeof(T) == 2 ? 2 * NW : NW, used = max(1, min(a.nsplit, (tiles + per - 1) / per));
     auto row_out = [&](int r) { return (size_t)(s.c0 + ((r0 + r) >> v.lg)) * v.h + (kv << v.lg) + ((r0 + r) & ((1 << v.lg) - 1)); };
@@ -654,15 +833,15 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
     Operand<T> k;
     uint64_t bad_now = 0;
     if (t0 < t1) {
-        const uint32_t r = rows_of(t0);
+        const uint32_t r = rows_of(tile_of(t0));
         bad_now = bad;
         fetch_values(0, r);
         load_operand(k, (const T *)a.k_pages + (int64_t)r * 128, half);
     }
     for (int t = t0; t < t1; ++t) {
-        const int buf = (t - t0) & 1, key0 = t * 32;
+        const int buf = (t - t0) & 1, key0 = tile_of(t) * 32;
         const bool more = t + 1 < t1;
-        const uint32_t r = more ? rows_of(t + 1) : 0;
+        const uint32_t r = more ? rows_of(tile_of(t + 1)) : 0;
         const uint64_t bad_next = bad;
         settled();   // this tile's keys and values are there, those of the last have been read
         f32x16_t sc[1] = {};
@@ -687,10 +866,18 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
         if constexpr (sizeof(T) == 2) k = k_next;
         char *vt = smem[wave][buf];
         score_regs<OPT>(sc[0], a.o, slope2, sight.pos - key0, half);
-        if (key0 + 32 > range.all_hi || key0 < all_lo || bad_now != 0) {
-            mask_regs(sc[0], sight, key0, (uint32_t)bad_now, half, -INFINITY);
+        if (key0 + 32 > range.all_hi || (key0 < all_lo && !(SIGHT == kWindow && key0 + 32 <= a.o.sinks)) || bad_now != 0) {
+            uint32_t seen = 0;
+            if constexpr (SIGHT == kRange) {
+                mask_regs(sc[0], sight, key0, (uint32_t)bad_now, half, -INFINITY);
+            } else {
+                seen = sight_bits<SIGHT>(a.o, s, sight, token, key0) & ~(uint32_t)bad_now;
+                mask_bits(sc[0], seen, half, -INFINITY);
+            }
             if (__any(Odd::any(vt, lane))) {
-                Odd::add(o, vt, sight, key0, bad_now, half);
+                Odd::add(o, vt, half, [&](int k) {
+                    return SIGHT == kRange ? key0 + k >= sight.lo && key0 + k < sight.hi && !((bad_now >> k) & 1) : (bool)((seen >> k) & 1);
+                });
                 __builtin_amdgcn_wave_barrier();
                 Odd::clean(vt, lane);
                 __builtin_amdgcn_wave_barrier();
@@ -702,111 +889,7 @@ template <typename T, int OPT, int NW> __global__ __launch_bounds__(64 * NW, siz
         __builtin_amdgcn_wave_barrier();
     }
 
-    // the waves' outputs to one maximum, through shared memory (16-byte chunks at chunk ^ row)
-    l = half_sum(l);
-    if (half == 0) {
-        join[wave][0][lane] = m;
-        join[wave][1][lane] = l;
-    }
-    loads_landed<0>();
-    __syncthreads();   // (and nobody needs its values any more)
-    const int r32 = lane & 31;
-    float top = join[0][0][r32];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) top = fmaxf(top, join[w][0][r32]);
-    const float scale = m == -INFINITY ? 1.0f : exp2_fast(m - top);
-    char *mine = smem[0][0] + wave * 32 * 512;
-#pragma unroll
-    for (int db = 0; db < 4; ++db)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f32x4_t x;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) x[c] = o[db][4 * i + c] * scale;
-            *reinterpret_cast<f32x4_t *>(mine + r32 * 512 + (((8 * db + 2 * i + half) ^ r32) << 4)) = x;
-        }
-    __syncthreads();
-    for (int j = threadIdx.x; j < have * 32; j += 64 * NW) {   // (row, four elements)
-        const int r = j >> 5, c = j & 31;
-        float t = join[0][0][r], sum = 0.0f;
-#pragma unroll
-        for (int w = 1; w < NW; ++w) t = fmaxf(t, join[w][0][r]);
-        f32x4_t x = {};
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const float mw = join[w][0][r];
-            sum += join[w][1][r] * (mw == -INFINITY ? 1.0f : exp2_fast(mw - t));
-            x += *reinterpret_cast<const f32x4_t *>(smem[0][0] + w * 32 * 512 + r * 512 + ((c ^ r) << 4));
-        }
-        x *= inv_sum(sum);
-        const float lse = lse_of(t, sum);
-        const size_t at_row = row_out(r);
-        if (!whole) {
-            const size_t n = (size_t)split * v.total * v.h + at_row;
-            if (a.done) {
-                if (c == 0) hand_over(a.part_lse + n, lse);
-                hand_over(a.part_o + n * 128 + 4 * c, x);
-            } else {
-                if (c == 0) a.part_lse[n] = lse;
-                store4(a.part_o + n * 128 + 4 * c, x);
-            }
-        } else {
-            if (c == 0 && a.lse) a.lse[at_row] = lse;
-            store4((T *)a.out + at_row * 128 + 4 * c, x);
-        }
-    }
-    if (whole || !a.done) return;
-
-    // The run that ends last joins the tile's runs, in their order, by their log-sum-exps: 32 lanes a row, four elements a lane, and where the
-    // rows are few several such groups a row, that take the runs in turn.
-    loads_landed<0>();   // (stores too)
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        uint32_t *done = a.done + (size_t)tile * v.g + kv;
-        last = atomicAdd(done, 1u) == (uint32_t)used - 1;
-        if (last) *done = 0;
-    }
-    __syncthreads();
-    if (!last) return;
-    constexpr int kGroups = 2 * NW;
-    f32x4_t(*sums)[33] = reinterpret_cast<f32x4_t(*)[33]>(smem);   // [group][lane, or the weights' sum]
-    int ways = kGroups;
-    while (ways > 1 && ways * have > kGroups) ways >>= 1;
-    const int group = threadIdx.x >> 5, l32 = threadIdx.x & 31, way = group % ways;
-    const size_t step = (size_t)v.total * v.h;
-    for (int base = 0; base < have; base += kGroups / ways) {
-        const int r = base + group / ways;
-        f32x4_t x = {};
-        float top_lse = -INFINITY, sum = 0.0f, ref = 0.0f;
-        if (r < have) {
-            const float *lses = a.part_lse + row_out(r), *outs = a.part_o + row_out(r) * 128 + 4 * l32;
-            for (int i = l32; i < used; i += 32) top_lse = fmaxf(top_lse, handed(lses + i * step));
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) top_lse = fmaxf(top_lse, __shfl_xor(top_lse, d));
-            ref = top_lse == -INFINITY ? 0.0f : top_lse;
-#pragma unroll 8
-            for (int i = way; i < used; i += ways) {
-                const float w = exp2_fast((handed(lses + i * step) - ref) * kLog2e);
-                sum += w;
-                x += handed4(outs + i * step * 128) * w;
-            }
-        }
-        if (ways > 1) {
-            sums[group][l32] = x;
-            if (l32 == 0) sums[group][32][0] = sum;
-            __syncthreads();
-            if (way == 0)
-                for (int w = 1; w < ways; ++w) {
-                    x += sums[group + w][l32];
-                    sum += sums[group + w][32][0];
-                }
-            __syncthreads();
-        }
-        if (r < have && way == 0) {
-            if (l32 == 0 && a.lse) a.lse[row_out(r)] = sum == 0.0f ? -INFINITY : ref + __builtin_amdgcn_logf(sum) * kLn2;
-            store4((T *)a.out + row_out(r) * 128 + 4 * l32, x * inv_sum(sum));
-        }
-    }
+    few_finish<T, NW>(a, s, kv, r0, have, tile, split, used, whole, m, l, o, smem[0][0], join, &last);
 }
 
 // The runs of a row joined by their log-sum-exps: a row has WAYS groups of 32 lanes, four elements a lane, that take the runs in turn
@@ -1288,14 +1371,16 @@ __device__ __forceinline__ void store_chunk(bf16_t *p, const float (&x)[8])
     *reinterpret_cast<bf16x8_t *>(p) = v;
 }
 
-// A wave has a token: lane i turns pair i's angle into sine and cosine, once for all heads, then 8 lanes take a row, the chunks i and i + 8 of 8
-// elements each.
-template <typename T> __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
+// A wave's token: its sequence, slot and page, and the sines and cosines of the lane's pairs 8 (lane % 8) on.  Lane i turns pair i's angle, once for all heads.
+struct AppendToken {
+    int slot;
+    uint32_t page;   // (of num_pages on: nothing is written)
+    float cs[8], sn[8];
+};
+__device__ __forceinline__ bool append_token(const AppendArgs &a, int token, int lane, float2 *turn, AppendToken *at)
 {
-    __shared__ float2 turn[4][64];
     const CacheView &v = a.v;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, token = blockIdx.x * 4 + wave;
-    if (token >= v.total) return;
+    if (token >= v.total) return false;
     // the token's sequence: the last one that begins at or before it
     int b = -1;
     for (int b0 = 0; b0 < v.batch; b0 += 64) {
@@ -1306,25 +1391,37 @@ template <typename T> __global__ __launch_bounds__(256) void append_kernel(Appen
             break;
         }
     }
-    if (b < 0) return;   // behind the last sequence
+    if (b < 0) return false;   // behind the last sequence
     const SeqSpan s = seq_span(v, b);
     const int slot = s.old + token - s.c0;
     const int pos = a.positions ? a.positions[(size_t)a.rope.axis[lane] * v.total + token] : slot;
     float2 t;
     sincos_turn((uint32_t)(((uint64_t)(int64_t)pos * a.rope.turn[lane]) >> 32), &t.y, &t.x);
-    turn[wave][lane] = t;
+    turn[lane] = t;
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     const int i8 = lane & 7;
-    float cs[8], sn[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float2 x = turn[wave][8 * i8 + i];
-        cs[i] = x.x;
-        sn[i] = x.y;
+        const float2 x = turn[8 * i8 + i];
+        at->cs[i] = x.x;
+        at->sn[i] = x.y;
     }
     const bool held = slot >= 0 && slot < s.len;
-    uint32_t page = held ? (uint32_t)v.table[(size_t)b * v.max_pages + (slot >> v.page_shift)] : 0xffffffffu;
+    at->slot = slot;
+    at->page = held ? (uint32_t)v.table[(size_t)b * v.max_pages + (slot >> v.page_shift)] : 0xffffffffu;
+    return true;
+}
+
+// A wave has a token, 8 lanes a row of it, the chunks i and i + 8 of 8 elements each.
+template <typename T> __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
+{
+    __shared__ float2 turn[4][64];
+    const CacheView &v = a.v;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, token = blockIdx.x * 4 + wave;
+    AppendToken t;
+    if (!append_token(a, token, lane, turn[wave], &t)) return;
+    const int i8 = lane & 7;
     const int nq = a.q ? v.h : 0, nk = a.k ? v.g : 0, rows = nq + 2 * nk;
     for (int r = lane >> 3; r < rows; r += 8) {
         const int kv = r - nq;
@@ -1336,8 +1433,8 @@ template <typename T> __global__ __launch_bounds__(256) void append_kernel(Appen
         if (r < nq) {
             to = (T *)a.q_out + ((size_t)token * v.h + r) * 128;
         } else {
-            if (page >= v.num_pages) continue;
-            const int64_t row = (((int64_t)page * v.g + (kv < nk ? kv : kv - nk)) << v.page_shift) + (slot & ((1 << v.page_shift) - 1));
+            if (t.page >= v.num_pages) continue;
+            const int64_t row = (((int64_t)t.page * v.g + (kv < nk ? kv : kv - nk)) << v.page_shift) + (t.slot & ((1 << v.page_shift) - 1));
             to = (T *)(kv < nk ? a.k_pages : a.v_pages) + row * 128;
         }
         if (kv >= nk) {   // values as they are
@@ -1350,8 +1447,8 @@ template <typename T> __global__ __launch_bounds__(256) void append_kernel(Appen
         unpack(hi, y);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            p[i] = fmaf(x[i], cs[i], -(y[i] * sn[i]));
-            q[i] = fmaf(y[i], cs[i], x[i] * sn[i]);
+            p[i] = fmaf(x[i], t.cs[i], -(y[i] * t.sn[i]));
+            q[i] = fmaf(y[i], t.cs[i], x[i] * t.sn[i]);
         }
         store_chunk(to + 8 * i8, p);
         store_chunk(to + 64 + 8 * i8, q);
@@ -1567,7 +1664,7 @@ template <int EACH> __global__ __launch_bounds__(1024) void evict_select_kernel(
 }
 
 // The lengths after an eviction into the array that holds those before it: behind the other kernels, whose blocks all read them
-__global__ void evict_lens_kernel(EvictArgs a)
+static __global__ void evict_lens_kernel(EvictArgs a)
 {
     const int b = blockIdx.x * blockDim.x + threadIdx.x;
     if (b < a.v.batch) a.lens[b] = min(min(max(a.v.cur[b], 0), a.v.max_pages << a.v.page_shift), a.budget);

@@ -46,7 +46,13 @@ struct ScoreOpts {
     const int32_t *first;     // [total] or null
     float c2;                 // scale * log2 e
     float cap_in, cap_out, cap_105, cap_945;   // scale / cap, cap * log2 e, the latter times 105 and 945 (cap != 0)
+    int window, sinks;        // kWindow: the last keys that a row sees, its own among them (2^21 at most), and the first ones
+    const uint32_t *drafts;   // kTree: [total][words], bit j of a token: it sees the j-th new token of its sequence
+    int words;
 };
+// What a row sees: keys by position and `first` (kRange); the last `window` up to its own and the first `sinks` (kWindow); those before the new tokens, and
+// of these the ones whose bit it has (kTree)
+constexpr int kRange = 0, kWindow = 1, kTree = 2;
 // What a row sees: keys from lo on, before hi
 struct RowSight {
     int pos, lo, hi;
@@ -58,6 +64,44 @@ __host__ __device__ __forceinline__ RowSight row_sight(const CacheView &v, const
     r.hi = r.pos < 0 ? 0 : min(max(r.pos + 1, prefix), s.len);
     r.lo = o.first ? max(o.first[s.c0 + token], 0) : 0;
     return r;
+}
+
+template <int SIGHT> __host__ __device__ __forceinline__ RowSight sight_of(const CacheView &v, const ScoreOpts &o, const SeqSpan &s, int prefix, int token)
+{
+    RowSight r = row_sight(v, o, s, SIGHT == kRange ? prefix : 0, token);
+    if constexpr (SIGHT == kWindow) r.lo = max(r.pos + 1 - o.window, 0);
+    if constexpr (SIGHT == kTree) r.hi = r.pos < 0 ? 0 : s.len;
+    return r;
+}
+// the lowest n of 32 bits
+__host__ __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+// Which of the 32 keys from key0 on the row of `token` sees, a bit each
+template <int SIGHT> __host__ __device__ __forceinline__ uint32_t sight_bits(const ScoreOpts &o, const SeqSpan &s, const RowSight &r, int token, int key0)
+{
+    uint32_t seen = ~low_bits(r.lo - key0);
+    if constexpr (SIGHT == kWindow) seen |= low_bits(o.sinks - key0);
+    if constexpr (SIGHT == kTree) {
+        const int64_t j = (int64_t)key0 - s.old;   // the draft's token that key0 is
+        if (j > -32) {
+            const uint32_t *row = o.drafts + (size_t)(s.c0 + token) * o.words;
+            const int64_t w = j >> 5;              // (-1 for keys before the draft: seen)
+            const uint32_t a = w < 0 ? ~0u : w < o.words ? row[w] : 0u, b = w + 1 < o.words ? row[w + 1] : 0u;
+            seen &= (uint32_t)((((uint64_t)b << 32) | a) >> (j & 31));
+        }
+    }
+    return seen & low_bits(r.hi - key0);
+}
+
+// The tiles of `keys` keys that a block of rows goes through: n of them, tile i of which is i, from `gap_at` on i + gap.  first and last: what the block's
+// first and last token see (kRange: lo is the least first key of its rows, end what key_range says).
+struct KeyTiles {
+    int from, to, gap_at, gap;
+    __host__ __device__ __forceinline__ int at(int i) const { return i < gap_at ? i : i + gap; }
+};
+__host__ __device__ __forceinline__ KeyTiles window_tiles(const ScoreOpts &o, int lo, int hi, int keys)
+{
+    const int w0 = min(lo, hi) / keys, sinks = min((min(o.sinks, hi) + keys - 1) / keys, w0);
+    return KeyTiles{0, sinks + (hi + keys - 1) / keys - w0, sinks, w0 - sinks};
 }
 
 // A frequency (radians per position) as a fraction of a turn, in 2^-64: freq / (2 pi) modulo 1, off by one of them at most for frequencies up to 2^32.

@@ -1,0 +1,599 @@
+// Kernels of a paged KV cache whose rows are held in 8 bits: append with rotary positions, reading back, attention.  gfx950, wave64, matrix cores.
+//
+// A row is 128 codes of one byte, int8 or e4m3, and an fp32 scale: its largest magnitude over the largest code.  Both kinds of code are exact in bf16, so that
+// the products take them as they are, two bytes each from the conversion on, and a key's scale multiplies its score, a value's its probability: nothing is
+// rounded that a bf16 cache would not round.  With fp32 queries a query and a probability are three bf16 parts each, which is all of their bits and still a
+// fifth of what fp32 products cost.
+#pragma once
+#include "cache.hpp"
+
+namespace ctkvr {
+
+constexpr int kInt8 = 1, kFp8 = 2;   // (ctkvr_kv_format)
+template <int STORE> constexpr float kTop = STORE == kInt8 ? 127.0f : 448.0f;
+
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+// ---- append -------------------------------------------------------------------------------------------------
+struct QuantRows {
+    uint8_t *codes;    // [num_pages][g][page][128]
+    float *scales;     // [num_pages][g][page]
+};
+struct QuantAppendArgs {
+    AppendArgs a;      // (k_pages, v_pages: null)
+    QuantRows k, v;
+};
+
+// A row's largest magnitude, as bits, over its 8 lanes (NaN above infinity above all numbers)
+__device__ __forceinline__ uint32_t largest_bits(const float (&p)[8], const float (&q)[8])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, max(__float_as_uint(p[i]) & 0x7fffffffu, __float_as_uint(q[i]) & 0x7fffffffu));
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
+    return m;
+}
+// x * top / amax, correctly rounded, so that what lies half way between two codes goes to the even one: a quotient from the reciprocal and one step of its
+// remainder (Markstein's division), four instructions a value where a division takes ten.  `inv`: 1 / amax.
+template <int STORE> __device__ __forceinline__ float in_codes(float x, float amax, float inv)
+{
+    const float n = x * kTop<STORE>, y = n * inv;
+    return fmaf(fmaf(-y, amax, n), inv, y);
+}
+template <int STORE> __device__ __forceinline__ uint2 encode(const float (&y)[8])
+{
+    uint2 c;
+    if constexpr (STORE == kInt8) {
+        uint32_t w[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i >> 2] |= ((uint32_t)(int)rintf(y[i]) & 0xffu) << (8 * (i & 3));
+        c = make_uint2(w[0], w[1]);
+    } else {
+        int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false);
+        lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
+        hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], hi, true);
+        c = make_uint2((uint32_t)lo, (uint32_t)hi);
+    }
+    return c;
+}
+// A row's chunks i8 and i8 + 8 of 8 elements, as codes.  A row that holds an infinity or NaN gets the scale NaN and codes of 0.
+template <int STORE> __device__ __forceinline__ void store_codes(const QuantRows &to, int64_t row, int i8, float (&p)[8], float (&q)[8])
+{
+    const uint32_t bits = largest_bits(p, q);
+    const float amax = __uint_as_float(bits);
+    const bool odd = bits >= 0x7f800000u, none = odd || bits == 0;
+    // (far from 1 the row is taken by a power of two, so that neither the products nor the reciprocal leave the range)
+    const float by = amax > 0x1p100f ? 0x1p-64f : amax < 0x1p-62f ? 0x1p64f : 1.0f, scaled = none ? 1.0f : amax * by, inv = 1.0f / scaled;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        p[i] = none ? 0.0f : in_codes<STORE>(p[i] * by, scaled, inv);
+        q[i] = none ? 0.0f : in_codes<STORE>(q[i] * by, scaled, inv);
+    }
+    uint8_t *at = to.codes + row * 128;
+    *reinterpret_cast<uint2 *>(at + 8 * i8) = encode<STORE>(p);
+    *reinterpret_cast<uint2 *>(at + 64 + 8 * i8) = encode<STORE>(q);
+    if (i8 == 0) to.scales[row] = odd ? __uint_as_float(0x7fc00000u) : amax / kTop<STORE>;
+}
+
+template <typename T, int STORE> __global__ __launch_bounds__(256) void quant_append_kernel(QuantAppendArgs qa)
+{
+    __shared__ float2 turn[4][64];
+    const AppendArgs &a = qa.a;
+    const CacheView &v = a.v;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, token = blockIdx.x * 4 + wave;
+    AppendToken t;
+    if (!append_token(a, token, lane, turn[wave], &t)) return;
+    const int i8 = lane & 7, nq = a.q ? v.h : 0, nk = a.k ? v.g : 0, rows = nq + 2 * nk;
+    for (int r = lane >> 3; r < rows; r += 8) {
+        const int kv = r - nq;
+        const T *from = r < nq ? (const T *)a.q + (int64_t)token * a.q_stride + r * 128
+                        : kv < nk ? (const T *)a.k + (int64_t)token * a.k_stride + kv * 128
+                                  : (const T *)a.val + (int64_t)token * a.v_stride + (kv - nk) * 128;
+        if (r >= nq && t.page >= v.num_pages) continue;
+        const Chunk<T> lo = load_chunk_nt(from, i8), hi = load_chunk_nt(from, i8 + 8);
+        float x[8], y[8], p[8], q[8];
+        unpack(lo, x);
+        unpack(hi, y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            p[i] = kv >= nk ? x[i] : fmaf(x[i], t.cs[i], -(y[i] * t.sn[i]));
+            q[i] = kv >= nk ? y[i] : fmaf(y[i], t.cs[i], x[i] * t.sn[i]);
+        }
+        if (r < nq) {
+            T *to = (T *)a.q_out + ((size_t)token * v.h + r) * 128;
+            store_chunk(to + 8 * i8, p);
+            store_chunk(to + 64 + 8 * i8, q);
+        } else {
+            const int64_t row = (((int64_t)t.page * v.g + (kv < nk ? kv : kv - nk)) << v.page_shift) + (t.slot & ((1 << v.page_shift) - 1));
+            store_codes<STORE>(kv < nk ? qa.k : qa.v, row, i8, p, q);
+        }
+    }
+}
+
+// ---- reading back -------------------------------------------------------------------------------------------
+struct QuantReadArgs {
+    CacheView v;              // (cu: null)
+    const int32_t *first;     // [batch] or null: the first token that is read
+    const uint8_t *codes[2];  // K, V; null: not read
+    const float *scales[2];
+    void *out[2];             // [out_pages][g][page][128]
+    const int32_t *out_table; // [batch][out_cols]
+    int out_cols;
+    uint32_t out_pages;
+};
+// 16 codes times their row's scale
+template <int STORE> __device__ __forceinline__ void decode(uint32_t w, float scale, float (&x)[4])
+{
+    if constexpr (STORE == kInt8) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(w >> (8 * i)) * scale;
+    } else {
+        const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+        x[0] = a[0] * scale;
+        x[1] = a[1] * scale;
+        x[2] = b[0] * scale;
+        x[3] = b[1] * scale;
+    }
+}
+// A block takes runs of 32 tokens of a unit, 8 lanes a row, 16 codes a lane
+template <typename T, int STORE> __global__ __launch_bounds__(256) void quant_read_kernel(QuantReadArgs a)
+{
+    const CacheView &v = a.v;
+    const int b = blockIdx.x / v.g, kv = blockIdx.x % v.g, i8 = threadIdx.x & 7;
+    const int len = min(max(v.cur[b], 0), v.max_pages << v.page_shift), from = a.first ? max(a.first[b], 0) : 0;
+    const int n = min(len - from, a.out_cols << v.page_shift), mask = (1 << v.page_shift) - 1;
+    for (int j = blockIdx.y * 32 + (threadIdx.x >> 3); j < n; j += gridDim.y * 32) {
+        const int64_t row = cache_row(v, b, kv, from + j);
+        const uint32_t page = (uint32_t)a.out_table[(size_t)b * a.out_cols + (j >> v.page_shift)];
+        if (row < 0 || page >= a.out_pages) continue;
+        const int64_t to = (((int64_t)page * v.g + kv) << v.page_shift) + (j & mask);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (!a.codes[i]) continue;
+            const uint4 c = *reinterpret_cast<const uint4 *>(a.codes[i] + row * 128 + 16 * i8);
+            const float scale = a.scales[i][row];
+            float x[4][4];
+            decode<STORE>(c.x, scale, x[0]);
+            decode<STORE>(c.y, scale, x[1]);
+            decode<STORE>(c.z, scale, x[2]);
+            decode<STORE>(c.w, scale, x[3]);
+            T *out = (T *)a.out[i] + to * 128 + 16 * i8;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) store4(out + 4 * e, f32x4_t{x[e][0], x[e][1], x[e][2], x[e][3]});
+        }
+    }
+}
+
+// ---- attention ----------------------------------------------------------------------------------------------
+struct QuantAttnArgs {
+    AttnArgs a;                         // (k_pages and v_pages are codes)
+    const float *k_scales, *v_scales;   // [num_pages][g][page]: a row's number is its scale's
+};
+
+// eight codes as bf16, exactly
+template <int STORE> __device__ __forceinline__ bf16x8_t codes8(uint32_t lo, uint32_t hi)
+{
+    bf16x8_t x;
+    if constexpr (STORE == kInt8) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = (__bf16)(float)(int8_t)(lo >> (8 * i));
+            x[4 + i] = (__bf16)(float)(int8_t)(hi >> (8 * i));
+        }
+    } else {
+        union { bf16x2_t h[4]; bf16x8_t w; } u;
+        u.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, 1.0f, false);
+        u.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, 1.0f, true);
+        u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, 1.0f, false);
+        u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, 1.0f, true);
+        x = u.w;
+    }
+    return x;
+}
+// e4m3's two NaN codes become 0: memory behind a sequence or before its window may hold them, and 0 times NaN is no 0
+template <int STORE> __device__ __forceinline__ uint32_t no_nan(uint32_t w)
+{
+    if constexpr (STORE == kInt8) return w;
+    const uint32_t nan = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    return w & ~(nan | (nan - (nan >> 7)));
+}
+
+// x as the sum of PARTS bf16 values, the first the nearest: three have all bits of an fp32 value
+template <int PARTS> __device__ __forceinline__ void split_parts(const float (&x)[8], bf16x8_t (&part)[PARTS])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        float rest = x[j];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            part[p][j] = (__bf16)rest;
+            if (p + 1 < PARTS) rest -= (float)part[p][j];
+        }
+    }
+}
+// The query's 8 elements from d on as parts
+template <typename T, int PARTS> __device__ __forceinline__ void query_parts(const T *row, int d, bf16x8_t (&part)[PARTS])
+{
+    if constexpr (sizeof(T) == 2) {
+        part[0] = *reinterpret_cast<const bf16x8_t *>(row + d);
+    } else {
+        const f32x4_t a = *reinterpret_cast<const f32x4_t *>(row + d), b = *reinterpret_cast<const f32x4_t *>(row + d + 4);
+        const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        split_parts(x, part);
+    }
+}
+
+// 32 keys' scores or probabilities times their scales, which stand in shared memory in the keys' order
+__device__ __forceinline__ void scale_regs(f32x16_t &s, const float *scales, int half)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(scales + 8 * i + 4 * half);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[4 * i + c] *= x[c];
+    }
+}
+
+// Rows of codes in shared memory: the 16-byte chunk c of row r stands at chunk c ^ code_swz(r), so that the eight rows of one chunk that 16 lanes of the transposing
+// load take (r, r + 1, r + 2, r + 3, r + 8 .. r + 11) fall on all banks once.
+__device__ __forceinline__ int code_swz(int row) { return (row & 3) | ((row >> 1) & 4); }
+
+// Few rows: one block a tile of 32 rows and a run of their keys, which its waves share out, 64 at a time; no wave waits for another before the end.  Keys go to
+// registers, values to shared memory, 64 ahead of those that are worked on.
+template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_few_kernel(QuantAttnArgs qa)
+{
+    constexpr int NW = 4, kKeys = 64, kTile = kKeys * 128, kParts = sizeof(T) == 2 ? 1 : 3;
+    __shared__ __align__(16) char smem[NW][2][kTile];
+    __shared__ __align__(16) float scales[NW][2][kKeys];   // [K, V]
+    __shared__ float join[NW][2][32];
+    __shared__ bool last;
+    const AttnArgs &a = qa.a;
+    const CacheView &v = a.v;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int kv = blockIdx.x % v.g, rest = blockIdx.x / v.g, split = rest % a.nsplit, tile = a.tiles - 1 - rest / a.nsplit;
+    int b, at;
+    if (!locate_tile<5>(v, tile, &b, &at)) return;
+    const SeqSpan s = seq_span(v, b);
+    const int rows = s.n << v.lg, r0 = at << 5, row = r0 + (lane & 31);
+    const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
+    const int token = min(row, rows - 1) >> v.lg, head = (kv << v.lg) + (min(row, rows - 1) & ((1 << v.lg) - 1));
+    const RowSight sight = sight_of<SIGHT>(v, a.o, s, prefix, token);
+
+    // step i of the product over 128 dimensions has those from 32 (i / 2) + 16 half + 8 (i % 2) on: a lane's 16 codes at a time
+    bf16x8_t q[8][kParts];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        query_parts<T, kParts>((const T *)a.q + (int64_t)(s.c0 + token) * a.q_stride + head * 128, 32 * (i >> 1) + 16 * half + 8 * (i & 1), q[i]);
+
+    const int tok0 = r0 >> v.lg, tok1 = (min(r0 + 32, rows) - 1) >> v.lg;
+    const KeyRange range = key_range_of<SIGHT>(s, prefix, tok0, tok1);
+    int k_lo = 0, all_lo = 0;
+    if (SIGHT == kWindow) {
+        k_lo = max(s.old + tok0 + 1 - a.o.window, 0);
+        all_lo = max(s.old + tok1 + 1 - a.o.window, 0);
+    } else if (a.o.first) {
+        k_lo = all_lo = sight.lo;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            k_lo = min(k_lo, __shfl_xor(k_lo, d));
+            all_lo = max(all_lo, __shfl_xor(all_lo, d));
+        }
+    }
+    int first_tile = k_lo / kKeys, tiles = range.hi > k_lo ? (range.hi + kKeys - 1) / kKeys - first_tile : 0;
+    KeyTiles kt{};
+    if constexpr (SIGHT == kWindow) {
+        kt = window_tiles(a.o, k_lo, range.hi, kKeys);
+        first_tile = kt.from;
+        tiles = kt.to;
+    }
+    auto tile_of = [&](int i) { return SIGHT == kWindow ? kt.at(i) : i; };
+    const int have = min(32, rows - r0), used = max(1, min(a.nsplit, (tiles + NW - 1) / NW));
+    if (split >= used) {
+        auto row_out = [&](int r) { return (size_t)(s.c0 + ((r0 + r) >> v.lg)) * v.h + (kv << v.lg) + ((r0 + r) & ((1 << v.lg) - 1)); };
+        if (!a.done && (int)threadIdx.x < have) a.part_lse[(size_t)split * v.total * v.h + row_out(threadIdx.x)] = -INFINITY;
+        return;
+    }
+    const bool whole = a.nsplit == 1 || (a.done && used == 1);   // this block's outputs are the rows'
+    const int64_t runs = (int64_t)used * NW, run = split * NW + wave;
+    const int t0 = __builtin_amdgcn_readfirstlane(first_tile + (int)(tiles * run / runs));
+    const int t1 = __builtin_amdgcn_readfirstlane(first_tile + (int)(tiles * (run + 1) / runs));
+
+    // the lane's key's row; 64 of the table's entries at a time
+    const int max_key = max(range.hi - 1, 0);
+    const int32_t *table = v.table + (size_t)b * v.max_pages;
+    int e0 = -64;
+    uint32_t page = 0;
+    uint64_t bad = 0;
+    auto rows_of = [&](int t) -> uint32_t {
+        const int key = min(t * kKeys + lane, max_key), e = key >> v.page_shift;
+        const int last_e = min(t * kKeys + kKeys - 1, max_key) >> v.page_shift;
+        if (last_e >= e0 + 64) {
+            e0 = (t * kKeys) >> v.page_shift;
+            page = (uint32_t)table[min(e0 + lane, v.max_pages - 1)];
+            loads_landed<0>();
+        }
+        const uint32_t p = (uint32_t)__shfl((int)page, e - e0);
+        const uint32_t r = p < v.num_pages ? (uint32_t)((p * (uint64_t)v.g + kv) << v.page_shift) + (key & ((1 << v.page_shift) - 1)) : kNoRow;
+        const uint64_t ok = __ballot(r != kNoRow);
+        bad = ~ok;
+        if (ok == ~0ull) return r;
+        if (!ok) return 0;
+        const uint32_t other = __builtin_amdgcn_readlane(r, __builtin_ctzll(ok));
+        return r != kNoRow ? r : other;
+    };
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_at(smem[wave]));
+    auto fetch_values = [&](int buf, uint32_t r) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {   // eight rows a load
+            const int key = 8 * j + (lane >> 3), c = (lane & 7) ^ code_swz(key);
+            row_to_lds(lds0 + buf * kTile + j * 1024, (const char *)a.v_pages + (int64_t)(uint32_t)__shfl((int)r, key) * 128 + 16 * c);
+        }
+    };
+    uint4 k[2][4];
+    float ks = 0.0f, vs = 0.0f;
+    auto fetch_keys = [&](uint32_t r) {
+        ks = qa.k_scales[r];
+        vs = qa.v_scales[r];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const char *from = (const char *)a.k_pages + (int64_t)(uint32_t)__shfl((int)r, 32 * kb + (lane & 31)) * 128 + 16 * half;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) k[kb][i] = *reinterpret_cast<const uint4 *>(from + 32 * i);
+        }
+    };
+
+    f32x16_t o[4] = {};
+    float m = -INFINITY, l = 0.0f;
+    const float slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
+    uint64_t bad_now = 0;
+    if (t0 < t1) {
+        const uint32_t r = rows_of(tile_of(t0));
+        bad_now = bad;
+        fetch_values(0, r);
+        fetch_keys(r);
+    }
+    for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1, key0 = tile_of(t) * kKeys;
+        const bool more = t + 1 < t1;
+        const uint32_t r = more ? rows_of(tile_of(t + 1)) : 0;
+        const uint64_t bad_next = bad;
+        settled();   // this tile's keys and values are there, those of the last have been read
+        scales[wave][0][lane] = ks;
+        scales[wave][1][lane] = vs;
+        if (more) fetch_values(buf ^ 1, r);
+        f32x16_t sc[2] = {};
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint4 &w = k[kb][i >> 1];
+                const bf16x8_t x = (i & 1) ? codes8<STORE>(w.z, w.w) : codes8<STORE>(w.x, w.y);
+#pragma unroll
+                for (int p = kParts - 1; p >= 0; --p) sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[i][p], sc[kb], 0, 0, 0);
+            }
+        if (more) fetch_keys(r);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const bool masked = key0 + kKeys > range.all_hi || (key0 < all_lo && !(SIGHT == kWindow && key0 + kKeys <= a.o.sinks)) || bad_now != 0;
+        uint32_t seen[2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            scale_regs(sc[kb], scales[wave][0] + 32 * kb, half);
+            score_regs<OPT>(sc[kb], a.o, slope2, sight.pos - key0 - 32 * kb, half);
+            if (masked) {
+                seen[kb] = sight_bits<SIGHT>(a.o, s, sight, token, key0 + 32 * kb) & ~(uint32_t)(bad_now >> (32 * kb));
+                mask_bits(sc[kb], seen[kb], half, -INFINITY);
+            }
+        }
+        softmax_regs<OPT, 2>(sc, o, m, l, a.o.c2);
+        const char *vt = smem[wave][buf];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            scale_regs(sc[kb], scales[wave][1] + 32 * kb, half);
+            if (masked) mask_bits(sc[kb], seen[kb], half, 0.0f);   // (a hidden row's scale may be anything)
+#pragma unroll
+            for (int k2 = 0; k2 < 2; ++k2) {
+                float y[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = sc[kb][8 * k2 + j];
+                bf16x8_t p[kParts];
+                split_parts(y, p);
+#pragma unroll
+                for (int db = 0; db < 4; ++db) {
+                    const int key = 32 * kb + 16 * k2 + 8 * ((lane >> 3) & 1) + 4 * half + ((lane >> 1) & 3), c = (2 * db + ((lane >> 4) & 1)) ^ code_swz(key);
+                    const i32x2_t w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((CTKVR_LDS i32x2_t *)(vt + key * 128 + 16 * c + 8 * (lane & 1)));
+                    uint32_t lo = (uint32_t)w[0], hi = (uint32_t)w[1];
+                    if (masked) lo = no_nan<STORE>(lo), hi = no_nan<STORE>(hi);
+                    const bf16x8_t x = codes8<STORE>(lo, hi);
+#pragma unroll
+                    for (int i = kParts - 1; i >= 0; --i) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[i], o[db], 0, 0, 0);
+                }
+            }
+        }
+        bad_now = bad_next;
+        __builtin_amdgcn_wave_barrier();
+    }
+    few_finish<T, NW>(a, s, kv, r0, have, tile, split, used, whole, m, l, o, smem[0][0], join, &last);
+}
+
+// Many rows: one block a tile of 128 rows of a unit and, where the keys are split, one of nsplit runs of them; a wave has 32 rows.  The block's threads turn each tile of
+// 64 keys into bf16 once, on its way to shared memory, while the tile before it is worked on.
+template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_many_kernel(QuantAttnArgs qa)
+{
+    constexpr int NW = 4, kRowsLog = 7, kKeys = 64, kTile = RowTile<bf16_t>::kBytes, kParts = sizeof(T) == 2 ? 1 : 3;
+    __shared__ __align__(16) char smem[2][2][kTile];   // [buffer][K, V]
+    __shared__ __align__(16) float scales[2][2][kKeys];
+    const AttnArgs &a = qa.a;
+    const CacheView &v = a.v;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int kv = blockIdx.x % v.g, rest = blockIdx.x / v.g, split = rest % a.nsplit;
+    int b, at;
+    if (!locate_tile<kRowsLog>(v, a.tiles - 1 - rest / a.nsplit, &b, &at)) return;
+    const SeqSpan s = seq_span(v, b);
+    const int rows = s.n << v.lg, r0 = at << kRowsLog, row = r0 + 32 * wave + (lane & 31);
+    const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
+    const int token = min(row, rows - 1) >> v.lg, head = (kv << v.lg) + (min(row, rows - 1) & ((1 << v.lg) - 1));
+    const RowSight sight = sight_of<SIGHT>(v, a.o, s, prefix, token);
+    bf16x8_t q[8][kParts];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) query_parts<T, kParts>((const T *)a.q + (int64_t)(s.c0 + token) * a.q_stride + head * 128, 16 * i + 8 * half, q[i]);
+
+    const int tok0 = r0 >> v.lg, tok1 = (min(r0 + 32 * NW, rows) - 1) >> v.lg;
+    const KeyRange range = key_range_of<SIGHT>(s, prefix, tok0, tok1);
+    int k_lo = 0, all_lo = 0;
+    if (SIGHT == kWindow) {
+        k_lo = max(s.old + tok0 + 1 - a.o.window, 0);
+        all_lo = max(s.old + tok1 + 1 - a.o.window, 0);
+    } else if (a.o.first) {
+        int lo = sight.lo, hi = sight.lo;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            lo = min(lo, __shfl_xor(lo, d));
+            hi = max(hi, __shfl_xor(hi, d));
+        }
+        int *ex = reinterpret_cast<int *>(smem);
+        if (lane == 0) {
+            ex[2 * wave] = lo;
+            ex[2 * wave + 1] = hi;
+        }
+        __syncthreads();
+        k_lo = ex[0];
+        all_lo = ex[1];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) {
+            k_lo = min(k_lo, ex[2 * w]);
+            all_lo = max(all_lo, ex[2 * w + 1]);
+        }
+        __syncthreads();
+    }
+    int t0 = k_lo / kKeys, t1 = range.hi > k_lo ? (range.hi + kKeys - 1) / kKeys : t0;
+    KeyTiles kt{};
+    if constexpr (SIGHT == kWindow) {
+        kt = window_tiles(a.o, k_lo, range.hi, kKeys);
+        t0 = kt.from;
+        t1 = kt.to;
+    }
+    auto tile_of = [&](int i) { return SIGHT == kWindow ? kt.at(i) : i; };
+    if (a.nsplit > 1) {   // this block's run of them: as many runs as there are eight tiles for
+        const int n = t1 - t0, used = max(1, min(a.nsplit, n / 8)), at_run = min(split, used);
+        const int from = (int)((int64_t)n * at_run / used), to = (int)((int64_t)n * min(at_run + 1, used) / used);
+        t1 = t0 + to;
+        t0 += from;
+    }
+    t0 = __builtin_amdgcn_readfirstlane(t0);
+    t1 = __builtin_amdgcn_readfirstlane(t1);
+
+    const int max_key = max(range.hi - 1, 0);
+    uint64_t bad = 0;
+    auto rows_of = [&](int t) -> uint32_t {
+        const uint32_t r = (uint32_t)cache_row(v, b, kv, min(t * kKeys + lane, max_key));
+        const uint64_t ok = __ballot(r != kNoRow);
+        bad = ~ok;
+        if (ok == ~0ull) return r;
+        if (!ok) return 0;
+        const uint32_t other = __builtin_amdgcn_readlane(r, __builtin_ctzll(ok));
+        return r != kNoRow ? r : other;
+    };
+    auto seen_by_all = [&](int t, uint64_t none) {
+        return (t + 1) * kKeys <= range.all_hi && (t * kKeys >= all_lo || (SIGHT == kWindow && (t + 1) * kKeys <= a.o.sinks)) && none == 0;
+    };
+    // a wave's share of a tile: 16 rows, 8 lanes a row, 16 codes a lane
+    uint4 codes[2][2];
+    float scale = 0.0f;
+    auto fetch = [&](uint32_t r) {
+        if (wave < 2) scale = (wave ? qa.v_scales : qa.k_scales)[r];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int64_t from = (int64_t)(uint32_t)__shfl((int)r, wave * 16 + 8 * j + (lane >> 3)) * 128 + 16 * (lane & 7);
+            codes[0][j] = *reinterpret_cast<const uint4 *>((const char *)a.k_pages + from);
+            codes[1][j] = *reinterpret_cast<const uint4 *>((const char *)a.v_pages + from);
+        }
+    };
+    auto put = [&](int buf, bool masked) {
+        if (wave < 2) scales[buf][wave][lane] = scale;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                uint4 w = codes[x][j];
+                if (x == 1 && masked) w = make_uint4(no_nan<STORE>(w.x), no_nan<STORE>(w.y), no_nan<STORE>(w.z), no_nan<STORE>(w.w));
+                const int key = wave * 16 + 8 * j + (lane >> 3), c = 2 * (lane & 7), z = swz<bf16_t>(key);
+                char *to = smem[buf][x] + key * 256;
+                *reinterpret_cast<bf16x8_t *>(to + ((c ^ z) << 4)) = codes8<STORE>(w.x, w.y);
+                *reinterpret_cast<bf16x8_t *>(to + (((c + 1) ^ z) << 4)) = codes8<STORE>(w.z, w.w);
+            }
+    };
+
+    f32x16_t o[4] = {};
+    float m = -INFINITY, l = 0.0f;
+    const float slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
+    uint64_t bad_now = 0;
+    if (t0 < t1) {
+        fetch(rows_of(tile_of(t0)));
+        bad_now = bad;
+        put(0, !seen_by_all(tile_of(t0), bad_now));
+        __syncthreads();
+    }
+    for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1, key0 = tile_of(t) * kKeys;
+        const bool more = t + 1 < t1, masked = !seen_by_all(tile_of(t), bad_now);
+        if (more) fetch(rows_of(tile_of(t + 1)));
+        const uint64_t bad_next = bad;
+        const char *kt_ = smem[buf][0], *vt = smem[buf][1];
+        f32x16_t sc[2] = {};
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const int r = 32 * kb + (lane & 31), z = swz<bf16_t>(r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bf16x8_t x = *reinterpret_cast<const bf16x8_t *>(kt_ + r * 256 + (((2 * i + half) ^ z) << 4));
+#pragma unroll
+                for (int p = kParts - 1; p >= 0; --p) sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[i][p], sc[kb], 0, 0, 0);
+            }
+        }
+        uint32_t seen[2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            scale_regs(sc[kb], scales[buf][0] + 32 * kb, half);
+            score_regs<OPT>(sc[kb], a.o, slope2, sight.pos - key0 - 32 * kb, half);
+            if (masked) {
+                seen[kb] = sight_bits<SIGHT>(a.o, s, sight, token, key0 + 32 * kb) & ~(uint32_t)(bad_now >> (32 * kb));
+                mask_bits(sc[kb], seen[kb], half, -INFINITY);
+            }
+        }
+        softmax_regs<OPT, 2>(sc, o, m, l, a.o.c2);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            scale_regs(sc[kb], scales[buf][1] + 32 * kb, half);
+            if (masked) mask_bits(sc[kb], seen[kb], half, 0.0f);   // (a hidden row's scale may be anything)
+#pragma unroll
+            for (int k2 = 0; k2 < 2; ++k2) {
+                float y[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = sc[kb][8 * k2 + j];
+                bf16x8_t p[kParts];
+                split_parts(y, p);
+#pragma unroll
+                for (int db = 0; db < 4; ++db) {
+                    union { s16x4_t h[2]; bf16x8_t w; } x;
+#pragma unroll
+                    for (int aa = 0; aa < 2; ++aa) {
+                        const int k = 32 * kb + 16 * k2 + 8 * aa + 4 * half + ((lane & 15) >> 2);
+                        const int c = (4 * db + 2 * ((lane & 31) >> 4) + ((lane & 3) >> 1)) ^ swz<bf16_t>(k);
+                        x.h[aa] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CTKVR_LDS s16x4_t *)(vt + k * 256 + (c << 4) + 8 * (lane & 1)));
+                    }
+#pragma unroll
+                    for (int i = kParts - 1; i >= 0; --i) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.w, p[i], o[db], 0, 0, 0);
+                }
+            }
+        }
+        if (more) put(buf ^ 1, !seen_by_all(tile_of(t + 1), bad_next));
+        bad_now = bad_next;
+        __syncthreads();
+    }
+    many_finish<T>(a, s, split, t0 == t1, row < rows, token, head, m, half_sum(l), o, half);
+}
+
+}  // namespace ctkvr

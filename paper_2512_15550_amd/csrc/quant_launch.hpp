@@ -1,0 +1,40 @@
+// Attention over 8-bit rows: the choice of the kernel's form.  Compiled for each type of query by itself (quant_bf16.hip, quant_f32.hip).
+#pragma once
+#include "cache_host.hpp"
+#include "quant.hpp"
+
+namespace ctkvr {
+
+template <typename T> int quant_attn_launch(const ctkvr_cache *c, QuantAttnArgs &q, const AttnPlan &plan, int store, int sight, int opt, hipStream_t st);
+
+#ifdef CTKVR_QUANT_TYPE
+template <typename T, int STORE, int SIGHT> void quant_attn_form(QuantAttnArgs &q, bool few, int opt, unsigned grid, hipStream_t st)
+{
+    with_opts(SIGHT == kTree ? opt & kCap : opt, [&](auto o) {
+        constexpr int kOpt = decltype(o)::value & (SIGHT == kTree ? kCap : ~0);   // (drafted tokens have no distance)
+        if (few) quant_few_kernel<STORE, T, kOpt, SIGHT><<<dim3(grid), 256, 0, st>>>(q);
+        else quant_many_kernel<STORE, T, kOpt, SIGHT><<<dim3(grid), 256, 0, st>>>(q);
+        return 0;
+    });
+}
+template <typename T> int quant_attn_launch(const ctkvr_cache *c, QuantAttnArgs &q, const AttnPlan &plan, int store, int sight, int opt, hipStream_t st)
+{
+    AttnArgs &a = q.a;
+    const unsigned grid = (unsigned)((int64_t)a.tiles * c->p.n_kv_heads * a.nsplit);
+    auto form = [&](auto store_, auto sight_) {
+        quant_attn_form<T, decltype(store_)::value, decltype(sight_)::value>(q, plan.few, opt, grid, st);
+    };
+    auto with_sight = [&](auto store_) {
+        if (sight == kRange) form(store_, std::integral_constant<int, kRange>());
+        else if (sight == kWindow) form(store_, std::integral_constant<int, kWindow>());
+        else form(store_, std::integral_constant<int, kTree>());
+    };
+    if (store == kInt8) with_sight(std::integral_constant<int, kInt8>());
+    else with_sight(std::integral_constant<int, kFp8>());
+    join_launch<T>(c, a, st);
+    return launched("attention over 8-bit rows");
+}
+template int quant_attn_launch<CTKVR_QUANT_TYPE>(const ctkvr_cache *, QuantAttnArgs &, const AttnPlan &, int, int, int, hipStream_t);
+#endif
+
+}  // namespace ctkvr
