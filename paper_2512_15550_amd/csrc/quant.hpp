@@ -1,9 +1,10 @@
 // Kernels of a paged KV cache whose rows are held in 8 bits: append with rotary positions, reading back, attention.  gfx950, wave64, matrix cores.
 //
-// A row is 128 codes of one byte, int8 or e4m3, and an fp32 scale: its largest magnitude over the largest code.  Both kinds of code are exact in bf16, so that
-// the products take them as they are, two bytes each from the conversion on, and a key's scale multiplies its score, a value's its probability: nothing is
-// rounded that a bf16 cache would not round.  With fp32 queries a query and a probability are three bf16 parts each, which is all of their bits and still a
-// fifth of what fp32 products cost.
+// A row is 128 codes of one byte, int8 or e4m3, and an fp32 scale: its largest magnitude over the largest code.  Both kinds of code are exact in bf16 and fp16, so that
+// the products take them as they are, two bytes each from the conversion on; a key's scale multiplies its score, a value's its probability.  Such a weight enters the
+// product in fp16, which has three bits more than bf16 (with weights in bf16 the outputs of a single token on 32K keys were 2.5e-3 off, of which their own rounding is
+// 1.6e-3), under a power of two that goes with the largest scale so far (ValueScale).  With fp32 queries a query is three bf16 parts and a weight two of
+// fp16: as exact as fp32 products, at a sixth of their cost.
 #pragma once
 #include "cache.hpp"
 
@@ -14,6 +15,8 @@ template <int STORE> constexpr float kTop = STORE == kInt8 ? 127.0f : 448.0f;
 
 typedef int i32x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
 // ---- append -------------------------------------------------------------------------------------------------
 struct QuantRows {
@@ -192,6 +195,27 @@ template <int STORE> __device__ __forceinline__ bf16x8_t codes8(uint32_t lo, uin
     }
     return x;
 }
+// ... as fp16
+template <int STORE> __device__ __forceinline__ f16x8_t codes8h(uint32_t lo, uint32_t hi)
+{
+    union { f16x2_t h[4]; f16x8_t w; } u;
+    if constexpr (STORE == kInt8) {
+        // the byte 128 + code as the last of the mantissa of 1024 + it, less 1152
+        lo ^= 0x80808080u;
+        hi ^= 0x80808080u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t pair = __builtin_amdgcn_perm(0x64646464u, i < 2 ? lo : hi, (i & 1) ? 0x04030402u : 0x04010400u);
+            u.h[i] = __builtin_bit_cast(f16x2_t, pair) - f16x2_t{(_Float16)1152.0f, (_Float16)1152.0f};
+        }
+    } else {
+        u.h[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.0f, false);
+        u.h[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.0f, true);
+        u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, false);
+        u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, true);
+    }
+    return u.w;
+}
 // e4m3's two NaN codes become 0: memory behind a sequence or before its window may hold them, and 0 times NaN is no 0
 template <int STORE> __device__ __forceinline__ uint32_t no_nan(uint32_t w)
 {
@@ -200,15 +224,16 @@ template <int STORE> __device__ __forceinline__ uint32_t no_nan(uint32_t w)
     return w & ~(nan | (nan - (nan >> 7)));
 }
 
-// x as the sum of PARTS bf16 values, the first the nearest: three have all bits of an fp32 value
-template <int PARTS> __device__ __forceinline__ void split_parts(const float (&x)[8], bf16x8_t (&part)[PARTS])
+// x as the sum of PARTS values, the first the nearest: three of bf16 have all bits of an fp32 value, two of fp16 all but two
+template <typename V, int PARTS> __device__ __forceinline__ void split_parts(const float (&x)[8], V (&part)[PARTS])
 {
+    using E = std::remove_reference_t<decltype(part[0][0] + part[0][0])>;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         float rest = x[j];
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
-            part[p][j] = (__bf16)rest;
+            part[p][j] = (E)rest;
             if (p + 1 < PARTS) rest -= (float)part[p][j];
         }
     }
@@ -236,6 +261,32 @@ __device__ __forceinline__ void scale_regs(f32x16_t &s, const float *scales, int
     }
 }
 
+// Values' scales as they multiply probabilities: times 2^(15 - exponent), where 2^exponent is above every scale so far, so that a weight is below 2^15 and has all of
+// fp16's bits down to 2^-14, which is 2^-29 of the largest that it could be; what is left of smaller ones is off by 2^-40 of that at most.  The outputs are
+// scaled as the exponent grows, once or twice in a run of keys as a rule.
+struct ValueScale {
+    int exponent = -100;
+    __device__ __forceinline__ float top() const { return ldexpf(1.0f, exponent); }
+    __device__ __forceinline__ float factor() const { return ldexpf(1.0f, 15 - exponent); }
+    // makes room for a wave's scales; the same in all lanes.  (NaN is above nothing: a row that sees it becomes NaN anyway.)
+    __device__ __forceinline__ void admit(float scale)
+    {
+        if (!__any(scale > top())) return;
+        uint32_t bits = scale > top() ? __float_as_uint(scale) : 0u;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) bits = max(bits, (uint32_t)__shfl_xor((int)bits, d));
+        exponent = max(__builtin_amdgcn_readfirstlane((int)(bits >> 23)) - 126, -100);
+    }
+};
+__device__ __forceinline__ void scale_outputs(f32x16_t (&o)[4], int by)   // by 2^by
+{
+    const float f = ldexpf(1.0f, by);
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] *= f;
+}
+
 // Rows of codes in shared memory: the 16-byte chunk c of row r stands at chunk c ^ code_swz(r), so that the eight rows of one chunk that 16 lanes of the transposing
 // load take (r, r + 1, r + 2, r + 3, r + 8 .. r + 11) fall on all banks once.
 __device__ __forceinline__ int code_swz(int row) { return (row & 3) | ((row >> 1) & 4); }
@@ -244,7 +295,7 @@ __device__ __forceinline__ int code_swz(int row) { return (row & 3) | ((row >> 1
 // registers, values to shared memory, 64 ahead of those that are worked on.
 template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_few_kernel(QuantAttnArgs qa)
 {
-    constexpr int NW = 4, kKeys = 64, kTile = kKeys * 128, kParts = sizeof(T) == 2 ? 1 : 3;
+    constexpr int NW = 4, kKeys = 64, kTile = kKeys * 128, kParts = sizeof(T) == 2 ? 1 : 3, kWeights = sizeof(T) == 2 ? 1 : 2;
     __shared__ __align__(16) char smem[NW][2][kTile];
     __shared__ __align__(16) float scales[NW][2][kKeys];   // [K, V]
     __shared__ float join[NW][2][32];
@@ -346,6 +397,7 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
 
     f32x16_t o[4] = {};
     float m = -INFINITY, l = 0.0f;
+    ValueScale value_scale;
     const float slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
     uint64_t bad_now = 0;
     if (t0 < t1) {
@@ -360,8 +412,15 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
         const uint32_t r = more ? rows_of(tile_of(t + 1)) : 0;
         const uint64_t bad_next = bad;
         settled();   // this tile's keys and values are there, those of the last have been read
-        scales[wave][0][lane] = ks;
-        scales[wave][1][lane] = vs;
+        {   // (the scales of keys that no row sees are whatever stands there)
+            const int key = key0 + lane;
+            const bool in = key < range.hi && (key >= k_lo || (SIGHT == kWindow && key < a.o.sinks)) && !((bad_now >> lane) & 1);
+            const int before = value_scale.exponent;
+            value_scale.admit(in ? vs : 0.0f);
+            if (value_scale.exponent != before) scale_outputs(o, before - value_scale.exponent);
+            scales[wave][0][lane] = ks;
+            scales[wave][1][lane] = vs * value_scale.factor();
+        }
         if (more) fetch_values(buf ^ 1, r);
         f32x16_t sc[2] = {};
 #pragma unroll
@@ -398,7 +457,7 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
                 float y[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[j] = sc[kb][8 * k2 + j];
-                bf16x8_t p[kParts];
+                f16x8_t p[kWeights];
                 split_parts(y, p);
 #pragma unroll
                 for (int db = 0; db < 4; ++db) {
@@ -406,15 +465,16 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
                     const i32x2_t w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((CTKVR_LDS i32x2_t *)(vt + key * 128 + 16 * c + 8 * (lane & 1)));
                     uint32_t lo = (uint32_t)w[0], hi = (uint32_t)w[1];
                     if (masked) lo = no_nan<STORE>(lo), hi = no_nan<STORE>(hi);
-                    const bf16x8_t x = codes8<STORE>(lo, hi);
+                    const f16x8_t x = codes8h<STORE>(lo, hi);
 #pragma unroll
-                    for (int i = kParts - 1; i >= 0; --i) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[i], o[db], 0, 0, 0);
+                    for (int i = kWeights - 1; i >= 0; --i) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, p[i], o[db], 0, 0, 0);
                 }
             }
         }
         bad_now = bad_next;
         __builtin_amdgcn_wave_barrier();
     }
+    scale_outputs(o, value_scale.exponent - 15);
     few_finish<T, NW>(a, s, kv, r0, have, tile, split, used, whole, m, l, o, smem[0][0], join, &last);
 }
 
@@ -422,9 +482,10 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
 // 64 keys into bf16 once, on its way to shared memory, while the tile before it is worked on.
 template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_many_kernel(QuantAttnArgs qa)
 {
-    constexpr int NW = 4, kRowsLog = 7, kKeys = 64, kTile = RowTile<bf16_t>::kBytes, kParts = sizeof(T) == 2 ? 1 : 3;
+    constexpr int NW = 4, kRowsLog = 7, kKeys = 64, kTile = RowTile<bf16_t>::kBytes, kParts = sizeof(T) == 2 ? 1 : 3, kWeights = sizeof(T) == 2 ? 1 : 2;
     __shared__ __align__(16) char smem[2][2][kTile];   // [buffer][K, V]
     __shared__ __align__(16) float scales[2][2][kKeys];
+    __shared__ int exponents[2];
     const AttnArgs &a = qa.a;
     const CacheView &v = a.v;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
@@ -511,8 +572,16 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
             codes[1][j] = *reinterpret_cast<const uint4 *>((const char *)a.v_pages + from);
         }
     };
-    auto put = [&](int buf, bool masked) {
-        if (wave < 2) scales[buf][wave][lane] = scale;
+    ValueScale value_scale;   // (wave 1's; the others follow the exponents that it leaves with the tiles)
+    auto put = [&](int buf, int t, bool masked) {
+        if (wave == 0) scales[buf][0][lane] = scale;
+        if (wave == 1) {   // (the scales of keys that no row sees are whatever stands there)
+            const int key = t * kKeys + lane;
+            const bool in = key < range.hi && (key >= k_lo || (SIGHT == kWindow && key < a.o.sinks)) && !((bad >> lane) & 1);
+            value_scale.admit(in ? scale : 0.0f);
+            scales[buf][1][lane] = scale * value_scale.factor();
+            if (lane == 0) exponents[buf] = value_scale.exponent;
+        }
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -521,19 +590,25 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
                 if (x == 1 && masked) w = make_uint4(no_nan<STORE>(w.x), no_nan<STORE>(w.y), no_nan<STORE>(w.z), no_nan<STORE>(w.w));
                 const int key = wave * 16 + 8 * j + (lane >> 3), c = 2 * (lane & 7), z = swz<bf16_t>(key);
                 char *to = smem[buf][x] + key * 256;
-                *reinterpret_cast<bf16x8_t *>(to + ((c ^ z) << 4)) = codes8<STORE>(w.x, w.y);
-                *reinterpret_cast<bf16x8_t *>(to + (((c + 1) ^ z) << 4)) = codes8<STORE>(w.z, w.w);
+                if (x == 0) {
+                    *reinterpret_cast<bf16x8_t *>(to + ((c ^ z) << 4)) = codes8<STORE>(w.x, w.y);
+                    *reinterpret_cast<bf16x8_t *>(to + (((c + 1) ^ z) << 4)) = codes8<STORE>(w.z, w.w);
+                } else {
+                    *reinterpret_cast<f16x8_t *>(to + ((c ^ z) << 4)) = codes8h<STORE>(w.x, w.y);
+                    *reinterpret_cast<f16x8_t *>(to + (((c + 1) ^ z) << 4)) = codes8h<STORE>(w.z, w.w);
+                }
             }
     };
 
     f32x16_t o[4] = {};
     float m = -INFINITY, l = 0.0f;
+    int exponent = -100;
     const float slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
     uint64_t bad_now = 0;
     if (t0 < t1) {
         fetch(rows_of(tile_of(t0)));
         bad_now = bad;
-        put(0, !seen_by_all(tile_of(t0), bad_now));
+        put(0, tile_of(t0), !seen_by_all(tile_of(t0), bad_now));
         __syncthreads();
     }
     for (int t = t0; t < t1; ++t) {
@@ -542,6 +617,10 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
         if (more) fetch(rows_of(tile_of(t + 1)));
         const uint64_t bad_next = bad;
         const char *kt_ = smem[buf][0], *vt = smem[buf][1];
+        if (const int e = __builtin_amdgcn_readfirstlane(exponents[buf]); e != exponent) {
+            scale_outputs(o, exponent - e);
+            exponent = e;
+        }
         f32x16_t sc[2] = {};
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
@@ -573,11 +652,11 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
                 float y[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[j] = sc[kb][8 * k2 + j];
-                bf16x8_t p[kParts];
+                f16x8_t p[kWeights];
                 split_parts(y, p);
 #pragma unroll
                 for (int db = 0; db < 4; ++db) {
-                    union { s16x4_t h[2]; bf16x8_t w; } x;
+                    union { s16x4_t h[2]; f16x8_t w; } x;
 #pragma unroll
                     for (int aa = 0; aa < 2; ++aa) {
                         const int k = 32 * kb + 16 * k2 + 8 * aa + 4 * half + ((lane & 15) >> 2);
@@ -585,14 +664,15 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
                         x.h[aa] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CTKVR_LDS s16x4_t *)(vt + k * 256 + (c << 4) + 8 * (lane & 1)));
                     }
 #pragma unroll
-                    for (int i = kParts - 1; i >= 0; --i) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.w, p[i], o[db], 0, 0, 0);
+                    for (int i = kWeights - 1; i >= 0; --i) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x.w, p[i], o[db], 0, 0, 0);
                 }
             }
         }
-        if (more) put(buf ^ 1, !seen_by_all(tile_of(t + 1), bad_next));
+        if (more) put(buf ^ 1, tile_of(t + 1), !seen_by_all(tile_of(t + 1), bad_next));
         bad_now = bad_next;
         __syncthreads();
     }
+    scale_outputs(o, exponent - 15);
     many_finish<T>(a, s, split, t0 == t1, row < rows, token, head, m, half_sum(l), o, half);
 }
 

@@ -85,8 +85,9 @@ def sees_tree(st, b, mask, first=None):
     return seen
 
 
-def attention(st, sees, cap=0.0, slopes=None, scale=1.0 / math.sqrt(128.0)):
-    """out, lse and per-element bounds on a kernel's deviation.  sees(b): which key [len] each of b's new tokens sees."""
+def attention(st, sees, cap=0.0, slopes=None, scale=1.0 / math.sqrt(128.0), spread=False):
+    """out, lse and per-element bounds on a kernel's deviation.  sees(b): which key [len] each of b's new tokens sees.  spread: rows of values of very
+    different sizes."""
     n_all, G = int(st.cu[-1]), st.h // st.g
     out, lse = torch.zeros((n_all, st.h, 128), dtype=F8), torch.full((n_all, st.h), -math.inf, dtype=F8)
     tol, tol_lse = torch.zeros_like(out), torch.zeros_like(lse)
@@ -121,6 +122,8 @@ def attention(st, sees, cap=0.0, slopes=None, scale=1.0 / math.sqrt(128.0)):
             # own rounding
             rel = math.expm1(2 * err) + (HALF["bf16"] if st.dtype == "bf16" else 0.0) + ((1 if st.dtype == "bf16" else 3) * s + 16) * 2.0 ** -23
             rows = slice(kv * G, (kv + 1) * G)
+            if spread:   # a weight is held to 2^-40 of what the largest value would have; twice that, for the rounding of the largest scale to a power of two
+                size = size + (s * 2.0 ** -39 * v.abs().max()) / rel * (l.T[..., None].transpose(0, 1) > -math.inf)
             out[c0:c0 + n, rows] = o.transpose(0, 1)
             tol[c0:c0 + n, rows] = (size * rel + o.abs() * HALF[st.dtype] + 1e-30).transpose(0, 1)
             lse[c0:c0 + n, rows] = l.T

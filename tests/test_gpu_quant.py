@@ -410,6 +410,29 @@ def test_keys_split(store, dtype, lens, new, h, g):
 
 @pytest.mark.parametrize("store", STORES)
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("powers", [3, 12, 60])
+@pytest.mark.parametrize("shape", ["few", "split", "many"])
+def test_values_of_very_different_sizes(store, dtype, powers, shape):
+    """Rows of values apart by up to 2^120, in any order, some of them zeros; bytes on free pages that would be larger still."""
+    if shape == "many":
+        st = many(83, store, dtype, h=16, g=4)
+    else:
+        st = Q.QuantSetup(83, store, dtype, 8, 2, 16, (2500, 40, 600) if shape == "split" else (150, 64, 1), (1, 3, 2) if shape == "split" else (100, 1, 1), q_scale=2.0)
+    by = torch.randint(-powers, powers + 1, st.v_scales.shape, generator=st.gen)
+    st.v_scales = st.v_scales * torch.exp2(by.float())
+    zero = torch.rand(st.v_scales.shape, generator=st.gen) < 0.05
+    st.v_scales[zero] = 0.0
+    st.v.view(torch.uint8)[zero] = 0
+    free = sorted(set(range(st.num_pages)) - set(st.table[st.table >= 0].tolist()))
+    st.v_scales[free] = 1e38
+    for b, s in enumerate(st.lens):
+        if s % st.page:
+            st.v_scales[int(st.table[b, (s - 1) // st.page]), :, s % st.page:] = 1e38
+    check(st, run_quant(st, cache_of(st)), lambda b: Q.sees_range(st, b), spread=True)
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_views_of_a_fused_projection_and_a_scale_of_ones_own(store, dtype):
     st = Q.QuantSetup(7, store, dtype, 8, 2, 16, (70, 90), (70, 40))
     fused = torch.full((st.total, 12 * 128 + 64), NAN, dtype=st.td, device=DEV)
@@ -609,13 +632,10 @@ def test_trees_on_pages_that_are_none_and_beyond_the_table(store):
 
 
 # ---- streams, graphs, repetition ------------------------------------------------------------------------------
-@pytest.mark.parametrize("kind", ["quant", "window", "tree"])
-@pytest.mark.parametrize("store", ALL_STORES)
+@pytest.mark.parametrize("kind,store", [("quant", "int8"), ("quant", "fp8")] + [(kind, store) for kind in ("window", "tree") for store in ALL_STORES])
 @pytest.mark.parametrize("new", [1, 33])
 def test_the_same_call_gives_the_same_bits_on_any_stream_and_in_graphs(kind, store, new):
     """Eagerly, on another stream, and in two graphs on one handle that take turns, with eager work between."""
-    if kind == "quant" and store == "plain":
-        pytest.skip("8-bit rows only")
     st = Q.QuantSetup(31, store, "bf16", 4, 1, 16, (3000,) if new == 1 else (3000, 700), (new,) if new == 1 else (new, new), q_scale=2.0)
     cache, p, batch, q, mask = cache_of(st), pages_of(st), batch_of(st), dev(st.q), dev(trees_of(st))
 
