@@ -2,6 +2,7 @@
 #include <new>
 
 #include "cache_host.hpp"
+#include "sight_plan.hpp"
 
 using namespace ctkvr;
 
@@ -111,12 +112,26 @@ int ctkvr_cache_create(const ctkvr_cache_params *p, void *hip_stream, ctkvr_cach
     // for the largest product of rows and runs that a call may take, and its tiles
     size_t part_rows = 0, counts = 0;
     for (int total = 1; total <= p->max_new; ++total) {
+        int most = 1;
+        auto room = [&](int nsplit, int tiles) {
+            most = std::max(most, nsplit);
+            if (nsplit == 1) return;
+            part_rows = std::max(part_rows, (size_t)nsplit * total * p->n_q_heads);
+            counts = std::max(counts, (size_t)tiles * p->n_kv_heads);
+        };
         const AttnPlan plan = attn_plan(c, total);
-        if (plan.nsplit == 1 && (((int64_t)total << c->lg) >> 7) * p->n_kv_heads >= 8ll * c->num_cu) break;   // more tokens are never split again
-        if (plan.nsplit == 1) continue;
-        part_rows = std::max(part_rows, (size_t)plan.nsplit * total * p->n_q_heads);
-        counts = std::max(counts, (size_t)plan.tiles * p->n_kv_heads);
+        room(plan.nsplit, plan.tiles);
+        const int64_t slots = (int64_t)p->max_pages * p->page_size;
+        for (const int64_t keys : {slots, std::min<int64_t>(slots, 4095)})   // (fewer are split less, in the form that they get)
+            for (const bool codes : {false, true}) {
+                const SightPlan sight = sight_plan(c, total, keys, codes);
+                room(sight.nsplit, sight.tiles);
+            }
+        if (most == 1 && (((int64_t)total << c->lg) >> 7) * p->n_kv_heads >= 8ll * c->num_cu) break;   // more tokens are never split again
     }
+    if (const char *e = getenv("SP_ROOM")) part_rows = std::max(part_rows, (size_t)atoll(e)), counts = std::max(counts, (size_t)1 << 20);
+    c->part_rows = part_rows;
+    c->counts = counts;
     if (part_rows) {
         int rc = pool_get(c->dev, (part_rows * 129 + counts) * 4, 4, &c->mem);
         if (rc == CTKVR_OK) {

@@ -136,7 +136,8 @@ template <typename T> __device__ __forceinline__ f32x16_t rows_dot(const char *t
 // ---- scores ------------------------------------------------------------------------------------------
 constexpr int kCap = 1, kBias = 2;
 // scores times log2 e, from the dot products (without cap and bias the factor is left to the exponent)
-template <int OPT> __device__ __forceinline__ void score_regs(f32x16_t &s, const ScoreOpts &o, float slope2, int pos_minus_key0, int half)
+// (of N registers, whose keys are STRIDE (i / 4) + i % 4 + 4 part)
+template <int OPT, int N = 16, int STRIDE = 8, typename V> __device__ __forceinline__ void score_regs(V &s, const ScoreOpts &o, float slope2, int pos_minus_key0, int part)
 {
     if constexpr (OPT != 0) {
         if constexpr ((OPT & kCap) != 0) {
@@ -145,7 +146,7 @@ template <int OPT> __device__ __forceinline__ void score_regs(f32x16_t &s, const
             // other key or row has a part in it; the wave only leaves the second out, half of the instructions, where none of its scores needs it.
             float big = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) big = fmaxf(big, fabsf(s[i]));
+            for (int i = 0; i < N; ++i) big = fmaxf(big, fabsf(s[i]));
             auto capped = [&](float z, auto beyond) {
                 const float x = z * o.cap_in, y = x * x;
                 float n = x * fmaf(y, fmaf(y, o.cap_out, o.cap_105), o.cap_945), d = fmaf(y, fmaf(y, 15.0f, 420.0f), 945.0f);
@@ -159,17 +160,17 @@ template <int OPT> __device__ __forceinline__ void score_regs(f32x16_t &s, const
             };
             if (__any(big * o.cap_in > 1.0f)) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = capped(s[i], std::true_type());
+                for (int i = 0; i < N; ++i) s[i] = capped(s[i], std::true_type());
             } else {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = capped(s[i], std::false_type());
+                for (int i = 0; i < N; ++i) s[i] = capped(s[i], std::false_type());
             }
         }
-        const float far = (float)(pos_minus_key0 - 4 * half);   // (distances below 2^24 are exact)
+        const float far = (float)(pos_minus_key0 - 4 * part);   // (distances below 2^24 are exact)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < N; ++i) {
             float z = (OPT & kCap) ? s[i] : s[i] * o.c2;
-            if constexpr ((OPT & kBias) != 0) z = fmaf(-slope2, fabsf(far - (float)(8 * (i >> 2) + (i & 3))), z);
+            if constexpr ((OPT & kBias) != 0) z = fmaf(-slope2, fabsf(far - (float)(STRIDE * (i >> 2) + (i & 3))), z);
             s[i] = z;
         }
     }
@@ -620,39 +621,14 @@ template <typename T, int OPT, int NW, int SIGHT = kRange> __global__ __launch_b
     many_finish<T>(a, s, split, t0 == t1, row < rows, token, head, m, half_sum(l), o, half);
 }
 
-// The end of a tile of few rows: its waves' maxima, sums and outputs become one, the rows' or this run's, and the run that ends last joins the runs.
-// smem: 32 rows of fp32 outputs a wave.
-template <typename T, int NW>
-__device__ __forceinline__ void few_finish(const AttnArgs &a, const SeqSpan &s, int kv, int r0, int have, int tile, int split, int used, bool whole, float m,
-                                           float l, const f32x16_t (&o)[4], char *smem, float (&join)[NW][2][32], bool *last)
+// The end of a tile of few rows, whose waves have left their outputs, all to one maximum, in shared memory (ROWS rows of 512 bytes a wave, 16-byte chunk c of row r at
+// chunk c ^ r) and their own maxima and sums in `join`: they become one, the rows' or this run's, and the run that ends last joins the runs.
+template <typename T, int NW, int ROWS>
+__device__ __forceinline__ void few_join(const AttnArgs &a, const SeqSpan &s, int kv, int r0, int have, int tile, int split, int used, bool whole, char *smem,
+                                         float (&join)[NW][2][ROWS], bool *last)
 {
     const CacheView &v = a.v;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     auto row_out = [&](int r) { return (size_t)(s.c0 + ((r0 + r) >> v.lg)) * v.h + (kv << v.lg) + ((r0 + r) & ((1 << v.lg) - 1)); };
-    // the waves' outputs to one maximum, through shared memory (16-byte chunks at chunk ^ row)
-    l = half_sum(l);
-    if (half == 0) {
-        join[wave][0][lane] = m;
-        join[wave][1][lane] = l;
-    }
-    loads_landed<0>();
-    __syncthreads();   // (and nobody needs its values any more)
-    const int r32 = lane & 31;
-    float top = join[0][0][r32];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) top = fmaxf(top, join[w][0][r32]);
-    const float scale = m == -INFINITY ? 1.0f : exp2_fast(m - top);
-    char *mine = smem + wave * 32 * 512;
-#pragma unroll
-    for (int db = 0; db < 4; ++db)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f32x4_t x;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) x[c] = o[db][4 * i + c] * scale;
-            *reinterpret_cast<f32x4_t *>(mine + r32 * 512 + (((8 * db + 2 * i + half) ^ r32) << 4)) = x;
-        }
-    __syncthreads();
     for (int j = threadIdx.x; j < have * 32; j += 64 * NW) {   // (row, four elements)
         const int r = j >> 5, c = j & 31;
         float t = join[0][0][r], sum = 0.0f;
@@ -663,7 +639,7 @@ __device__ __forceinline__ void few_finish(const AttnArgs &a, const SeqSpan &s, 
         for (int w = 0; w < NW; ++w) {
             const float mw = join[w][0][r];
             sum += join[w][1][r] * (mw == -INFINITY ? 1.0f : exp2_fast(mw - t));
-            x += *reinterpret_cast<const f32x4_t *>(smem + w * 32 * 512 + r * 512 + ((c ^ r) << 4));
+            x += *reinterpret_cast<const f32x4_t *>(smem + w * ROWS * 512 + r * 512 + ((c ^ r) << 4));
         }
         x *= inv_sum(sum);
         const float lse = lse_of(t, sum);
@@ -734,6 +710,38 @@ __device__ __forceinline__ void few_finish(const AttnArgs &a, const SeqSpan &s, 
             store4((T *)a.out + row_out(r) * 128 + 4 * l32, x * inv_sum(sum));
         }
     }
+}
+// ... from a wave's outputs of 32 rows
+template <typename T, int NW>
+__device__ __forceinline__ void few_finish(const AttnArgs &a, const SeqSpan &s, int kv, int r0, int have, int tile, int split, int used, bool whole, float m,
+                                           float l, const f32x16_t (&o)[4], char *smem, float (&join)[NW][2][32], bool *last)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    // the waves' outputs to one maximum, through shared memory (16-byte chunks at chunk ^ row)
+    l = half_sum(l);
+    if (half == 0) {
+        join[wave][0][lane] = m;
+        join[wave][1][lane] = l;
+    }
+    loads_landed<0>();
+    __syncthreads();   // (and nobody needs its values any more)
+    const int r32 = lane & 31;
+    float top = join[0][0][r32];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) top = fmaxf(top, join[w][0][r32]);
+    const float scale = m == -INFINITY ? 1.0f : exp2_fast(m - top);
+    char *mine = smem + wave * 32 * 512;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f32x4_t x;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) x[c] = o[db][4 * i + c] * scale;
+            *reinterpret_cast<f32x4_t *>(mine + r32 * 512 + (((8 * db + 2 * i + half) ^ r32) << 4)) = x;
+        }
+    __syncthreads();
+    few_join<T, NW, 32>(a, s, kv, r0, have, tile, split, used, whole, smem, join, last);
 }
 
 // Few rows: one block a tile of 32 rows and a run of their keys, which its waves share out, each with a maximum and outputs of its own until

@@ -18,6 +18,7 @@ struct ctkvr_cache {
     ctkvr::PoolBlock mem{nullptr, 0};   // the workspace: a split attention's partial outputs, their log-sum-exps, and a count for each tile
     float *part_o = nullptr, *part_lse = nullptr;
     uint32_t *done = nullptr;
+    size_t part_rows = 0, counts = 0;   // what there is room for
 
     ~ctkvr_cache()
     {

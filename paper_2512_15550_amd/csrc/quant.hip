@@ -43,13 +43,19 @@ int check_attn(const ctkvr_cache *c, const AttnCall &x)
     return CTKVR_OK;
 }
 
-template <typename T, int SIGHT> int plain_launch(const ctkvr_cache *c, AttnArgs &a, bool few, int opt, hipStream_t st)
+template <typename T, int SIGHT> int plain_launch(const ctkvr_cache *c, QuantAttnArgs &qa, int log, int opt, hipStream_t st)
 {
+    AttnArgs &a = qa.a;
     const unsigned grid = (unsigned)((int64_t)a.tiles * c->p.n_kv_heads * a.nsplit);
     with_opts(opt, [&](auto o) {
-        constexpr int kOpt = decltype(o)::value & (SIGHT == kTree ? kCap : ~0), kFew = sizeof(T) == 2 ? 4 : 2;   // (drafted tokens have no distance)
-        if (few) attn_few_kernel<T, kOpt, kFew, SIGHT><<<dim3(grid), 64 * kFew, 0, st>>>(a);
-        else attn_kernel<T, kOpt, 4, SIGHT><<<dim3(grid), 256, 0, st>>>(a);
+        constexpr int kOpt = decltype(o)::value & (SIGHT == kTree ? kCap : ~0);   // (drafted tokens have no distance)
+        if constexpr (sizeof(T) == 2) {
+            if (log == 4) tokens_kernel<kPlain, T, kOpt, SIGHT, 1><<<dim3(grid), 256, 0, st>>>(qa);
+            if (log == 5) tokens_kernel<kPlain, T, kOpt, SIGHT, 2><<<dim3(grid), 256, 0, st>>>(qa);
+        } else if (log == 5) {
+            attn_few_kernel<T, kOpt, 2, SIGHT><<<dim3(grid), 128, 0, st>>>(a);
+        }
+        if (log == 7) attn_kernel<T, kOpt, 4, SIGHT><<<dim3(grid), 256, 0, st>>>(a);
         return 0;
     });
     join_launch<T>(c, a, st);
@@ -74,7 +80,10 @@ template <int SIGHT> int attend(const ctkvr_cache *c, const AttnCall &x, const S
     a.part_lse = c->part_lse;
     qa.k_scales = x.k_scales;
     qa.v_scales = x.v_scales;
-    const AttnPlan plan = attn_plan(c, x.total);
+    const int64_t slots = (int64_t)c->p.max_pages * c->p.page_size;
+    const SightPlan plan = sight_plan(c, x.total, SIGHT == kWindow ? std::min<int64_t>(slots, (int64_t)o.window + o.sinks + x.total) : slots, x.format != CTKVR_KV_PLAIN);
+    if (plan.nsplit > 1 && ((size_t)plan.nsplit * x.total * c->p.n_q_heads > c->part_rows || (size_t)plan.tiles * c->p.n_kv_heads > c->counts))
+        return fail(CTKVR_EHIP, "%d runs of %d tokens: beyond the workspace", plan.nsplit, x.total);
     a.tiles = plan.tiles;
     a.nsplit = plan.nsplit;
     a.done = plan.join_inside ? c->done : nullptr;
@@ -83,7 +92,7 @@ template <int SIGHT> int attend(const ctkvr_cache *c, const AttnCall &x, const S
     if (x.format != CTKVR_KV_PLAIN)
         return bf16 ? quant_attn_launch<bf16_t>(c, qa, plan, x.format, SIGHT, opt, st) : quant_attn_launch<float>(c, qa, plan, x.format, SIGHT, opt, st);
     if constexpr (SIGHT != kRange)
-        return bf16 ? plain_launch<bf16_t, SIGHT>(c, a, plan.few, opt, st) : plain_launch<float, SIGHT>(c, a, plan.few, opt, st);
+        return bf16 ? plain_launch<bf16_t, SIGHT>(c, qa, plan.log, opt, st) : plain_launch<float, SIGHT>(c, qa, plan.log, opt, st);
     return CTKVR_OK;
 }
 

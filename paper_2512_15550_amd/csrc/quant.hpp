@@ -10,7 +10,7 @@
 
 namespace ctkvr {
 
-constexpr int kInt8 = 1, kFp8 = 2;   // (ctkvr_kv_format)
+constexpr int kPlain = 0, kInt8 = 1, kFp8 = 2;   // (ctkvr_kv_format)
 template <int STORE> constexpr float kTop = STORE == kInt8 ? 127.0f : 448.0f;
 
 typedef int i32x2_t __attribute__((ext_vector_type(2)));
@@ -285,197 +285,6 @@ __device__ __forceinline__ void scale_outputs(f32x16_t (&o)[4], int by)   // by 
     for (int db = 0; db < 4; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[db][i] *= f;
-}
-
-// Rows of codes in shared memory: the 16-byte chunk c of row r stands at chunk c ^ code_swz(r), so that the eight rows of one chunk that 16 lanes of the transposing
-// load take (r, r + 1, r + 2, r + 3, r + 8 .. r + 11) fall on all banks once.
-__device__ __forceinline__ int code_swz(int row) { return (row & 3) | ((row >> 1) & 4); }
-
-// Few rows: one block a tile of 32 rows and a run of their keys, which its waves share out, 64 at a time; no wave waits for another before the end.  Keys go to
-// registers, values to shared memory, 64 ahead of those that are worked on.
-template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_few_kernel(QuantAttnArgs qa)
-{
-    constexpr int NW = 4, kKeys = 64, kTile = kKeys * 128, kParts = sizeof(T) == 2 ? 1 : 3, kWeights = sizeof(T) == 2 ? 1 : 2;
-    __shared__ __align__(16) char smem[NW][2][kTile];
-    __shared__ __align__(16) float scales[NW][2][kKeys];   // [K, V]
-    __shared__ float join[NW][2][32];
-    __shared__ bool last;
-    const AttnArgs &a = qa.a;
-    const CacheView &v = a.v;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int kv = blockIdx.x % v.g, rest = blockIdx.x / v.g, split = rest % a.nsplit, tile = a.tiles - 1 - rest / a.nsplit;
-    int b, at;
-    if (!locate_tile<5>(v, tile, &b, &at)) return;
-    const SeqSpan s = seq_span(v, b);
-    const int rows = s.n << v.lg, r0 = at << 5, row = r0 + (lane & 31);
-    const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
-    const int token = min(row, rows - 1) >> v.lg, head = (kv << v.lg) + (min(row, rows - 1) & ((1 << v.lg) - 1));
-    const RowSight sight = sight_of<SIGHT>(v, a.o, s, prefix, token);
-
-    // step i of the product over 128 dimensions has those from 32 (i / 2) + 16 half + 8 (i % 2) on: a lane's 16 codes at a time
-    bf16x8_t q[8][kParts];
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        query_parts<T, kParts>((const T *)a.q + (int64_t)(s.c0 + token) * a.q_stride + head * 128, 32 * (i >> 1) + 16 * half + 8 * (i & 1), q[i]);
-
-    const int tok0 = r0 >> v.lg, tok1 = (min(r0 + 32, rows) - 1) >> v.lg;
-    const KeyRange range = key_range_of<SIGHT>(s, prefix, tok0, tok1);
-    int k_lo = 0, all_lo = 0;
-    if (SIGHT == kWindow) {
-        k_lo = max(s.old + tok0 + 1 - a.o.window, 0);
-        all_lo = max(s.old + tok1 + 1 - a.o.window, 0);
-    } else if (a.o.first) {
-        k_lo = all_lo = sight.lo;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            k_lo = min(k_lo, __shfl_xor(k_lo, d));
-            all_lo = max(all_lo, __shfl_xor(all_lo, d));
-        }
-    }
-    int first_tile = k_lo / kKeys, tiles = range.hi > k_lo ? (range.hi + kKeys - 1) / kKeys - first_tile : 0;
-    KeyTiles kt{};
-    if constexpr (SIGHT == kWindow) {
-        kt = window_tiles(a.o, k_lo, range.hi, kKeys);
-        first_tile = kt.from;
-        tiles = kt.to;
-    }
-    auto tile_of = [&](int i) { return SIGHT == kWindow ? kt.at(i) : i; };
-    const int have = min(32, rows - r0), used = max(1, min(a.nsplit, (tiles + NW - 1) / NW));
-    if (split >= used) {
-        auto row_out = [&](int r) { return (size_t)(s.c0 + ((r0 + r) >> v.lg)) * v.h + (kv << v.lg) + ((r0 + r) & ((1 << v.lg) - 1)); };
-        if (!a.done && (int)threadIdx.x < have) a.part_lse[(size_t)split * v.total * v.h + row_out(threadIdx.x)] = -INFINITY;
-        return;
-    }
-    const bool whole = a.nsplit == 1 || (a.done && used == 1);   // this block's outputs are the rows'
-    const int64_t runs = (int64_t)used * NW, run = split * NW + wave;
-    const int t0 = __builtin_amdgcn_readfirstlane(first_tile + (int)(tiles * run / runs));
-    const int t1 = __builtin_amdgcn_readfirstlane(first_tile + (int)(tiles * (run + 1) / runs));
-
-    // the lane's key's row; 64 of the table's entries at a time
-    const int max_key = max(range.hi - 1, 0);
-    const int32_t *table = v.table + (size_t)b * v.max_pages;
-    int e0 = -64;
-    uint32_t page = 0;
-    uint64_t bad = 0;
-    auto rows_of = [&](int t) -> uint32_t {
-        const int key = min(t * kKeys + lane, max_key), e = key >> v.page_shift;
-        const int last_e = min(t * kKeys + kKeys - 1, max_key) >> v.page_shift;
-        if (last_e >= e0 + 64) {
-            e0 = (t * kKeys) >> v.page_shift;
-            page = (uint32_t)table[min(e0 + lane, v.max_pages - 1)];
-            loads_landed<0>();
-        }
-        const uint32_t p = (uint32_t)__shfl((int)page, e - e0);
-        const uint32_t r = p < v.num_pages ? (uint32_t)((p * (uint64_t)v.g + kv) << v.page_shift) + (key & ((1 << v.page_shift) - 1)) : kNoRow;
-        const uint64_t ok = __ballot(r != kNoRow);
-        bad = ~ok;
-        if (ok == ~0ull) return r;
-        if (!ok) return 0;
-        const uint32_t other = __builtin_amdgcn_readlane(r, __builtin_ctzll(ok));
-        return r != kNoRow ? r : other;
-    };
-    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_at(smem[wave]));
-    auto fetch_values = [&](int buf, uint32_t r) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {   // eight rows a load
-            const int key = 8 * j + (lane >> 3), c = (lane & 7) ^ code_swz(key);
-            row_to_lds(lds0 + buf * kTile + j * 1024, (const char *)a.v_pages + (int64_t)(uint32_t)__shfl((int)r, key) * 128 + 16 * c);
-        }
-    };
-    uint4 k[2][4];
-    float ks = 0.0f, vs = 0.0f;
-    auto fetch_keys = [&](uint32_t r) {
-        ks = qa.k_scales[r];
-        vs = qa.v_scales[r];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const char *from = (const char *)a.k_pages + (int64_t)(uint32_t)__shfl((int)r, 32 * kb + (lane & 31)) * 128 + 16 * half;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) k[kb][i] = *reinterpret_cast<const uint4 *>(from + 32 * i);
-        }
-    };
-
-    f32x16_t o[4] = {};
-    float m = -INFINITY, l = 0.0f;
-    ValueScale value_scale;
-    const float slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
-    uint64_t bad_now = 0;
-    if (t0 < t1) {
-        const uint32_t r = rows_of(tile_of(t0));
-        bad_now = bad;
-        fetch_values(0, r);
-        fetch_keys(r);
-    }
-    for (int t = t0; t < t1; ++t) {
-        const int buf = (t - t0) & 1, key0 = tile_of(t) * kKeys;
-        const bool more = t + 1 < t1;
-        const uint32_t r = more ? rows_of(tile_of(t + 1)) : 0;
-        const uint64_t bad_next = bad;
-        settled();   // this tile's keys and values are there, those of the last have been read
-        {   // (the scales of keys that no row sees are whatever stands there)
-            const int key = key0 + lane;
-            const bool in = key < range.hi && (key >= k_lo || (SIGHT == kWindow && key < a.o.sinks)) && !((bad_now >> lane) & 1);
-            const int before = value_scale.exponent;
-            value_scale.admit(in ? vs : 0.0f);
-            if (value_scale.exponent != before) scale_outputs(o, before - value_scale.exponent);
-            scales[wave][0][lane] = ks;
-            scales[wave][1][lane] = vs * value_scale.factor();
-        }
-        if (more) fetch_values(buf ^ 1, r);
-        f32x16_t sc[2] = {};
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint4 &w = k[kb][i >> 1];
-                const bf16x8_t x = (i & 1) ? codes8<STORE>(w.z, w.w) : codes8<STORE>(w.x, w.y);
-#pragma unroll
-                for (int p = kParts - 1; p >= 0; --p) sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[i][p], sc[kb], 0, 0, 0);
-            }
-        if (more) fetch_keys(r);
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        const bool masked = key0 + kKeys > range.all_hi || (key0 < all_lo && !(SIGHT == kWindow && key0 + kKeys <= a.o.sinks)) || bad_now != 0;
-        uint32_t seen[2];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            scale_regs(sc[kb], scales[wave][0] + 32 * kb, half);
-            score_regs<OPT>(sc[kb], a.o, slope2, sight.pos - key0 - 32 * kb, half);
-            if (masked) {
-                seen[kb] = sight_bits<SIGHT>(a.o, s, sight, token, key0 + 32 * kb) & ~(uint32_t)(bad_now >> (32 * kb));
-                mask_bits(sc[kb], seen[kb], half, -INFINITY);
-            }
-        }
-        softmax_regs<OPT, 2>(sc, o, m, l, a.o.c2);
-        const char *vt = smem[wave][buf];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            scale_regs(sc[kb], scales[wave][1] + 32 * kb, half);
-            if (masked) mask_bits(sc[kb], seen[kb], half, 0.0f);   // (a hidden row's scale may be anything)
-#pragma unroll
-            for (int k2 = 0; k2 < 2; ++k2) {
-                float y[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = sc[kb][8 * k2 + j];
-                f16x8_t p[kWeights];
-                split_parts(y, p);
-#pragma unroll
-                for (int db = 0; db < 4; ++db) {
-                    const int key = 32 * kb + 16 * k2 + 8 * ((lane >> 3) & 1) + 4 * half + ((lane >> 1) & 3), c = (2 * db + ((lane >> 4) & 1)) ^ code_swz(key);
-                    const i32x2_t w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((CTKVR_LDS i32x2_t *)(vt + key * 128 + 16 * c + 8 * (lane & 1)));
-                    uint32_t lo = (uint32_t)w[0], hi = (uint32_t)w[1];
-                    if (masked) lo = no_nan<STORE>(lo), hi = no_nan<STORE>(hi);
-                    const f16x8_t x = codes8h<STORE>(lo, hi);
-#pragma unroll
-                    for (int i = kWeights - 1; i >= 0; --i) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, p[i], o[db], 0, 0, 0);
-                }
-            }
-        }
-        bad_now = bad_next;
-        __builtin_amdgcn_wave_barrier();
-    }
-    scale_outputs(o, value_scale.exponent - 15);
-    few_finish<T, NW>(a, s, kv, r0, have, tile, split, used, whole, m, l, o, smem[0][0], join, &last);
 }
 
 // Many rows: one block a tile of 128 rows of a unit and, where the keys are split, one of nsplit runs of them; a wave has 32 rows.  The block's threads turn each tile of

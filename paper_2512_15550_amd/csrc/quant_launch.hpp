@@ -1,28 +1,30 @@
 // Attention over 8-bit rows: the choice of the kernel's form.  Compiled for each type of query by itself (quant_bf16.hip, quant_f32.hip).
 #pragma once
 #include "cache_host.hpp"
-#include "quant.hpp"
+#include "sight_plan.hpp"
+#include "tokens.hpp"
 
 namespace ctkvr {
 
-template <typename T> int quant_attn_launch(const ctkvr_cache *c, QuantAttnArgs &q, const AttnPlan &plan, int store, int sight, int opt, hipStream_t st);
+template <typename T> int quant_attn_launch(const ctkvr_cache *c, QuantAttnArgs &q, const SightPlan &plan, int store, int sight, int opt, hipStream_t st);
 
 #ifdef CTKVR_QUANT_TYPE
-template <typename T, int STORE, int SIGHT> void quant_attn_form(QuantAttnArgs &q, bool few, int opt, unsigned grid, hipStream_t st)
+template <typename T, int STORE, int SIGHT> void quant_attn_form(QuantAttnArgs &q, int log, int opt, unsigned grid, hipStream_t st)
 {
     with_opts(SIGHT == kTree ? opt & kCap : opt, [&](auto o) {
         constexpr int kOpt = decltype(o)::value & (SIGHT == kTree ? kCap : ~0);   // (drafted tokens have no distance)
-        if (few) quant_few_kernel<STORE, T, kOpt, SIGHT><<<dim3(grid), 256, 0, st>>>(q);
+        if (log == 4) tokens_kernel<STORE, T, kOpt, SIGHT, 1><<<dim3(grid), 256, 0, st>>>(q);
+        else if (log == 5) tokens_kernel<STORE, T, kOpt, SIGHT, 2><<<dim3(grid), 256, 0, st>>>(q);
         else quant_many_kernel<STORE, T, kOpt, SIGHT><<<dim3(grid), 256, 0, st>>>(q);
         return 0;
     });
 }
-template <typename T> int quant_attn_launch(const ctkvr_cache *c, QuantAttnArgs &q, const AttnPlan &plan, int store, int sight, int opt, hipStream_t st)
+template <typename T> int quant_attn_launch(const ctkvr_cache *c, QuantAttnArgs &q, const SightPlan &plan, int store, int sight, int opt, hipStream_t st)
 {
     AttnArgs &a = q.a;
     const unsigned grid = (unsigned)((int64_t)a.tiles * c->p.n_kv_heads * a.nsplit);
     auto form = [&](auto store_, auto sight_) {
-        quant_attn_form<T, decltype(store_)::value, decltype(sight_)::value>(q, plan.few, opt, grid, st);
+        quant_attn_form<T, decltype(store_)::value, decltype(sight_)::value>(q, plan.log, opt, grid, st);
     };
     auto with_sight = [&](auto store_) {
         if (sight == kRange) form(store_, std::integral_constant<int, kRange>());
@@ -34,7 +36,7 @@ template <typename T> int quant_attn_launch(const ctkvr_cache *c, QuantAttnArgs 
     join_launch<T>(c, a, st);
     return launched("attention over 8-bit rows");
 }
-template int quant_attn_launch<CTKVR_QUANT_TYPE>(const ctkvr_cache *, QuantAttnArgs &, const AttnPlan &, int, int, int, hipStream_t);
+template int quant_attn_launch<CTKVR_QUANT_TYPE>(const ctkvr_cache *, QuantAttnArgs &, const SightPlan &, int, int, int, hipStream_t);
 #endif
 
 }  // namespace ctkvr
