@@ -287,202 +287,4 @@ __device__ __forceinline__ void scale_outputs(f32x16_t (&o)[4], int by)   // by 
         for (int i = 0; i < 16; ++i) o[db][i] *= f;
 }
 
-// Many rows: one block a tile of 128 rows of a unit and, where the keys are split, one of nsplit runs of them; a wave has 32 rows.  The block's threads turn each tile of
-// 64 keys into bf16 once, on its way to shared memory, while the tile before it is worked on.
-template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void quant_many_kernel(QuantAttnArgs qa)
-{
-    constexpr int NW = 4, kRowsLog = 7, kKeys = 64, kTile = RowTile<bf16_t>::kBytes, kParts = sizeof(T) == 2 ? 1 : 3, kWeights = sizeof(T) == 2 ? 1 : 2;
-    __shared__ __align__(16) char smem[2][2][kTile];   // [buffer][K, V]
-    __shared__ __align__(16) float scales[2][2][kKeys];
-    __shared__ int exponents[2];
-    const AttnArgs &a = qa.a;
-    const CacheView &v = a.v;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int kv = blockIdx.x % v.g, rest = blockIdx.x / v.g, split = rest % a.nsplit;
-    int b, at;
-    if (!locate_tile<kRowsLog>(v, a.tiles - 1 - rest / a.nsplit, &b, &at)) return;
-    const SeqSpan s = seq_span(v, b);
-    const int rows = s.n << v.lg, r0 = at << kRowsLog, row = r0 + 32 * wave + (lane & 31);
-    const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
-    const int token = min(row, rows - 1) >> v.lg, head = (kv << v.lg) + (min(row, rows - 1) & ((1 << v.lg) - 1));
-    const RowSight sight = sight_of<SIGHT>(v, a.o, s, prefix, token);
-    bf16x8_t q[8][kParts];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) query_parts<T, kParts>((const T *)a.q + (int64_t)(s.c0 + token) * a.q_stride + head * 128, 16 * i + 8 * half, q[i]);
-
-    const int tok0 = r0 >> v.lg, tok1 = (min(r0 + 32 * NW, rows) - 1) >> v.lg;
-    const KeyRange range = key_range_of<SIGHT>(s, prefix, tok0, tok1);
-    int k_lo = 0, all_lo = 0;
-    if (SIGHT == kWindow) {
-        k_lo = max(s.old + tok0 + 1 - a.o.window, 0);
-        all_lo = max(s.old + tok1 + 1 - a.o.window, 0);
-    } else if (a.o.first) {
-        int lo = sight.lo, hi = sight.lo;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            lo = min(lo, __shfl_xor(lo, d));
-            hi = max(hi, __shfl_xor(hi, d));
-        }
-        int *ex = reinterpret_cast<int *>(smem);
-        if (lane == 0) {
-            ex[2 * wave] = lo;
-            ex[2 * wave + 1] = hi;
-        }
-        __syncthreads();
-        k_lo = ex[0];
-        all_lo = ex[1];
-#pragma unroll
-        for (int w = 1; w < NW; ++w) {
-            k_lo = min(k_lo, ex[2 * w]);
-            all_lo = max(all_lo, ex[2 * w + 1]);
-        }
-        __syncthreads();
-    }
-    int t0 = k_lo / kKeys, t1 = range.hi > k_lo ? (range.hi + kKeys - 1) / kKeys : t0;
-    KeyTiles kt{};
-    if constexpr (SIGHT == kWindow) {
-        kt = window_tiles(a.o, k_lo, range.hi, kKeys);
-        t0 = kt.from;
-        t1 = kt.to;
-    }
-    auto tile_of = [&](int i) { return SIGHT == kWindow ? kt.at(i) : i; };
-    if (a.nsplit > 1) {   // this block's run of them: as many runs as there are eight tiles for
-        const int n = t1 - t0, used = max(1, min(a.nsplit, n / 8)), at_run = min(split, used);
-        const int from = (int)((int64_t)n * at_run / used), to = (int)((int64_t)n * min(at_run + 1, used) / used);
-        t1 = t0 + to;
-        t0 += from;
-    }
-    t0 = __builtin_amdgcn_readfirstlane(t0);
-    t1 = __builtin_amdgcn_readfirstlane(t1);
-
-    const int max_key = max(range.hi - 1, 0);
-    uint64_t bad = 0;
-    auto rows_of = [&](int t) -> uint32_t {
-        const uint32_t r = (uint32_t)cache_row(v, b, kv, min(t * kKeys + lane, max_key));
-        const uint64_t ok = __ballot(r != kNoRow);
-        bad = ~ok;
-        if (ok == ~0ull) return r;
-        if (!ok) return 0;
-        const uint32_t other = __builtin_amdgcn_readlane(r, __builtin_ctzll(ok));
-        return r != kNoRow ? r : other;
-    };
-    auto seen_by_all = [&](int t, uint64_t none) {
-        return (t + 1) * kKeys <= range.all_hi && (t * kKeys >= all_lo || (SIGHT == kWindow && (t + 1) * kKeys <= a.o.sinks)) && none == 0;
-    };
-    // a wave's share of a tile: 16 rows, 8 lanes a row, 16 codes a lane
-    uint4 codes[2][2];
-    float scale = 0.0f;
-    auto fetch = [&](uint32_t r) {
-        if (wave < 2) scale = (wave ? qa.v_scales : qa.k_scales)[r];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int64_t from = (int64_t)(uint32_t)__shfl((int)r, wave * 16 + 8 * j + (lane >> 3)) * 128 + 16 * (lane & 7);
-            codes[0][j] = *reinterpret_cast<const uint4 *>((const char *)a.k_pages + from);
-            codes[1][j] = *reinterpret_cast<const uint4 *>((const char *)a.v_pages + from);
-        }
-    };
-    ValueScale value_scale;   // (wave 1's; the others follow the exponents that it leaves with the tiles)
-    auto put = [&](int buf, int t, bool masked) {
-        if (wave == 0) scales[buf][0][lane] = scale;
-        if (wave == 1) {   // (the scales of keys that no row sees are whatever stands there)
-            const int key = t * kKeys + lane;
-            const bool in = key < range.hi && (key >= k_lo || (SIGHT == kWindow && key < a.o.sinks)) && !((bad >> lane) & 1);
-            value_scale.admit(in ? scale : 0.0f);
-            scales[buf][1][lane] = scale * value_scale.factor();
-            if (lane == 0) exponents[buf] = value_scale.exponent;
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                uint4 w = codes[x][j];
-                if (x == 1 && masked) w = make_uint4(no_nan<STORE>(w.x), no_nan<STORE>(w.y), no_nan<STORE>(w.z), no_nan<STORE>(w.w));
-                const int key = wave * 16 + 8 * j + (lane >> 3), c = 2 * (lane & 7), z = swz<bf16_t>(key);
-                char *to = smem[buf][x] + key * 256;
-                if (x == 0) {
-                    *reinterpret_cast<bf16x8_t *>(to + ((c ^ z) << 4)) = codes8<STORE>(w.x, w.y);
-                    *reinterpret_cast<bf16x8_t *>(to + (((c + 1) ^ z) << 4)) = codes8<STORE>(w.z, w.w);
-                } else {
-                    *reinterpret_cast<f16x8_t *>(to + ((c ^ z) << 4)) = codes8h<STORE>(w.x, w.y);
-                    *reinterpret_cast<f16x8_t *>(to + (((c + 1) ^ z) << 4)) = codes8h<STORE>(w.z, w.w);
-                }
-            }
-    };
-
-    f32x16_t o[4] = {};
-    float m = -INFINITY, l = 0.0f;
-    int exponent = -100;
-    const float slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
-    uint64_t bad_now = 0;
-    if (t0 < t1) {
-        fetch(rows_of(tile_of(t0)));
-        bad_now = bad;
-        put(0, tile_of(t0), !seen_by_all(tile_of(t0), bad_now));
-        __syncthreads();
-    }
-    for (int t = t0; t < t1; ++t) {
-        const int buf = (t - t0) & 1, key0 = tile_of(t) * kKeys;
-        const bool more = t + 1 < t1, masked = !seen_by_all(tile_of(t), bad_now);
-        if (more) fetch(rows_of(tile_of(t + 1)));
-        const uint64_t bad_next = bad;
-        const char *kt_ = smem[buf][0], *vt = smem[buf][1];
-        if (const int e = __builtin_amdgcn_readfirstlane(exponents[buf]); e != exponent) {
-            scale_outputs(o, exponent - e);
-            exponent = e;
-        }
-        f32x16_t sc[2] = {};
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const int r = 32 * kb + (lane & 31), z = swz<bf16_t>(r);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const bf16x8_t x = *reinterpret_cast<const bf16x8_t *>(kt_ + r * 256 + (((2 * i + half) ^ z) << 4));
-#pragma unroll
-                for (int p = kParts - 1; p >= 0; --p) sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[i][p], sc[kb], 0, 0, 0);
-            }
-        }
-        uint32_t seen[2];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            scale_regs(sc[kb], scales[buf][0] + 32 * kb, half);
-            score_regs<OPT>(sc[kb], a.o, slope2, sight.pos - key0 - 32 * kb, half);
-            if (masked) {
-                seen[kb] = sight_bits<SIGHT>(a.o, s, sight, token, key0 + 32 * kb) & ~(uint32_t)(bad_now >> (32 * kb));
-                mask_bits(sc[kb], seen[kb], half, -INFINITY);
-            }
-        }
-        softmax_regs<OPT, 2>(sc, o, m, l, a.o.c2);
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            scale_regs(sc[kb], scales[buf][1] + 32 * kb, half);
-            if (masked) mask_bits(sc[kb], seen[kb], half, 0.0f);   // (a hidden row's scale may be anything)
-#pragma unroll
-            for (int k2 = 0; k2 < 2; ++k2) {
-                float y[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = sc[kb][8 * k2 + j];
-                f16x8_t p[kWeights];
-                split_parts(y, p);
-#pragma unroll
-                for (int db = 0; db < 4; ++db) {
-                    union { s16x4_t h[2]; f16x8_t w; } x;
-#pragma unroll
-                    for (int aa = 0; aa < 2; ++aa) {
-                        const int k = 32 * kb + 16 * k2 + 8 * aa + 4 * half + ((lane & 15) >> 2);
-                        const int c = (4 * db + 2 * ((lane & 31) >> 4) + ((lane & 3) >> 1)) ^ swz<bf16_t>(k);
-                        x.h[aa] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CTKVR_LDS s16x4_t *)(vt + k * 256 + (c << 4) + 8 * (lane & 1)));
-                    }
-#pragma unroll
-                    for (int i = kWeights - 1; i >= 0; --i) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x.w, p[i], o[db], 0, 0, 0);
-                }
-            }
-        }
-        if (more) put(buf ^ 1, tile_of(t + 1), !seen_by_all(tile_of(t + 1), bad_next));
-        bad_now = bad_next;
-        __syncthreads();
-    }
-    scale_outputs(o, exponent - 15);
-    many_finish<T>(a, s, split, t0 == t1, row < rows, token, head, m, half_sum(l), o, half);
-}
-
 }  // namespace ctkvr

@@ -1,6 +1,7 @@
 // Attention over 8-bit rows: the choice of the kernel's form.  Compiled for each type of query by itself (quant_bf16.hip, quant_f32.hip).
 #pragma once
 #include "cache_host.hpp"
+#include "rows.hpp"
 #include "sight_plan.hpp"
 #include "tokens.hpp"
 
@@ -15,7 +16,7 @@ template <typename T, int STORE, int SIGHT> void quant_attn_form(QuantAttnArgs &
         constexpr int kOpt = decltype(o)::value & (SIGHT == kTree ? kCap : ~0);   // (drafted tokens have no distance)
         if (log == 4) tokens_kernel<STORE, T, kOpt, SIGHT, 1><<<dim3(grid), 256, 0, st>>>(q);
         else if (log == 5) tokens_kernel<STORE, T, kOpt, SIGHT, 2><<<dim3(grid), 256, 0, st>>>(q);
-        else quant_many_kernel<STORE, T, kOpt, SIGHT><<<dim3(grid), 256, 0, st>>>(q);
+        else rows_kernel<STORE, T, kOpt, SIGHT><<<dim3(grid), 256, 0, st>>>(q);
         return 0;
     });
 }
