@@ -404,8 +404,12 @@ __device__ __forceinline__ float handed(const float *p) { return __hip_atomic_lo
 __device__ __forceinline__ float inv_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }   // (NaN stays)
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2; }
 
+// the first dimension of a row's chunk c of 8, in order
+struct ColumnsInOrder {
+    static constexpr int column(int c) { return 8 * c; }
+};
 // A row's outputs, or its run's, from its sum l and maximum m
-template <typename T>
+template <typename T, typename ORDER = ColumnsInOrder>
 __device__ __forceinline__ void many_finish(const AttnArgs &a, const SeqSpan &s, int split, bool empty, bool live, int token, int head, float m, float l,
                                             const f32x16_t (&o)[4], int half)
 {
@@ -423,7 +427,7 @@ __device__ __forceinline__ void many_finish(const AttnArgs &a, const SeqSpan &s,
     for (int db = 0; db < 4; ++db)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int d = 32 * db + 8 * i + 4 * half;
+            const int d = ORDER::column(4 * db + i) + 4 * half;
             f32x4_t x;
 #pragma unroll
             for (int c = 0; c < 4; ++c) x[c] = o[db][4 * i + c] * inv;

@@ -4,26 +4,30 @@
 
 namespace ctkvr {
 
-// A tile of 64 keys and their values in shared memory, as bf16 (keys) and bf16 or, from codes, fp16 (values), and where a lane finds its operands.  Rows of codes are
-// turned into these on their way and stand in rows of 272 and 288 bytes, so that the eight rows that lanes take at one chunk of keys, and the four that 16 lanes of the
-// transposing load take at two chunks of values, fall on all banks once, at addresses that differ from a lane's first by constants.  Plain rows come straight
-// from memory, 16 bytes a lane, one row of 256 bytes behind the other: there the chunk c of row r stands at c ^ r % 8 (keys) or c ^ 2 (r % 4) (values), and a lane has four
-// and two first addresses.
+// A tile of 64 keys and their values in shared memory, as bf16 (keys) and bf16 or, from codes, fp16 (values), and where a lane finds its operands.  Shared memory
+// answers 16 lanes of 16 bytes or 32 of 8 at a time, from 64 banks: the 16 rows that lanes take at one chunk of keys, and the four rows that 16 lanes of the transposing
+// load take at two chunks of values, with the 16 lanes beside them at two more, have to fall on all banks once.
+//   Rows of codes are turned into 16 bits on their way.  The 16 codes of a lane become the chunks c and c + 8 of a row, c the lane of its eight, so that eight lanes write
+// a line; the queries and outputs follow this order (column()).  Rows of 272 and 320 bytes then put an operand at a constant distance from a lane's first.
+//   Plain rows come straight from memory, 16 bytes a lane, one row of 256 bytes behind the other: there the chunk c of row r stands at c ^ r % 16 (keys) or
+// c ^ 4 (r % 4) (values).
 template <bool CODES> struct RowsTile {
-    static constexpr int kKeyRow = CODES ? 272 : 256, kValueRow = CODES ? 288 : 256;
+    static constexpr int kKeyRow = CODES ? 272 : 256, kValueRow = CODES ? 320 : 256;
     static constexpr int kKeyBytes = 64 * kKeyRow, kBytes = kKeyBytes + 64 * kValueRow;
+    // the first of the 8 dimensions that chunk c of a row holds
+    static __host__ __device__ __forceinline__ constexpr int column(int c) { return CODES ? 16 * (c & 7) + 8 * (c >> 3) : 8 * c; }
     static __device__ __forceinline__ int key_at(int lane, int kb, int i)
     {
         const int r = lane & 31, half = lane >> 5;
         if constexpr (CODES) return r * kKeyRow + 16 * half + 32 * kb * kKeyRow + 32 * i;
-        else return r * 256 + (((2 * (i & 3) + half) ^ (r & 7)) << 4) + 32 * kb * 256 + 128 * (i >> 2);
+        else return r * 256 + (((2 * i + half) ^ (r & 15)) << 4) + 32 * kb * 256;
     }
-    // rows 8 aa + 4 (lane / 32) + 0 .. 3 of 16 from 32 kb + 16 k2 on, columns 32 db on
+    // rows 8 aa + 4 (lane / 32) + 0 .. 3 of 16 from 32 kb + 16 k2 on, chunks 4 db on
     static __device__ __forceinline__ int value_at(int lane, int kb, int k2, int aa, int db)
     {
-        const int half = lane >> 5, r = 4 * half + ((lane & 15) >> 2), rows = 32 * kb + 16 * k2 + 8 * aa;
+        const int half = lane >> 5, in = (lane & 15) >> 2, r = 4 * half + in, rows = 32 * kb + 16 * k2 + 8 * aa;
         if constexpr (CODES) return kKeyBytes + r * kValueRow + 32 * ((lane >> 4) & 1) + 8 * (lane & 3) + rows * kValueRow + 64 * db;
-        else return kKeyBytes + r * 256 + (((4 * (db & 1) + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (((lane & 15) >> 2) << 1)) << 4) + 8 * (lane & 1) + rows * 256 + 128 * (db >> 1);
+        else return kKeyBytes + r * 256 + ((db ^ in) << 6) + 32 * ((lane >> 4) & 1) + 8 * (lane & 3) + rows * 256;
     }
 };
 
@@ -52,7 +56,7 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
     const RowSight sight = sight_of<SIGHT>(v, a.o, s, prefix, token);
     bf16x8_t q[8][kParts];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) query_parts<T, kParts>((const T *)a.q + (int64_t)(s.c0 + token) * a.q_stride + head * 128, 16 * i + 8 * half, q[i]);
+    for (int i = 0; i < 8; ++i) query_parts<T, kParts>((const T *)a.q + (int64_t)(s.c0 + token) * a.q_stride + head * 128, Tile::column(2 * i + half), q[i]);
 
     const int tok0 = r0 >> v.lg, tok1 = (min(r0 + 32 * NW, rows) - 1) >> v.lg;
     const KeyRange range = key_range_of<SIGHT>(s, prefix, tok0, tok1);
@@ -154,11 +158,11 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int key = wave * 16 + 8 * j + (lane >> 3);
-            char *k_to = smem[buf] + key * Tile::kKeyRow + 32 * (lane & 7), *v_to = smem[buf] + Tile::kKeyBytes + key * Tile::kValueRow + 32 * (lane & 7);
+            char *k_to = smem[buf] + key * Tile::kKeyRow + 16 * (lane & 7), *v_to = smem[buf] + Tile::kKeyBytes + key * Tile::kValueRow + 16 * (lane & 7);
             *reinterpret_cast<bf16x8_t *>(k_to) = codes8<STORE>(codes[0][j].x, codes[0][j].y);
-            *reinterpret_cast<bf16x8_t *>(k_to + 16) = codes8<STORE>(codes[0][j].z, codes[0][j].w);
+            *reinterpret_cast<bf16x8_t *>(k_to + 128) = codes8<STORE>(codes[0][j].z, codes[0][j].w);
             *reinterpret_cast<f16x8_t *>(v_to) = codes8h<STORE>(codes[1][j].x, codes[1][j].y);
-            *reinterpret_cast<f16x8_t *>(v_to + 16) = codes8h<STORE>(codes[1][j].z, codes[1][j].w);
+            *reinterpret_cast<f16x8_t *>(v_to + 128) = codes8h<STORE>(codes[1][j].z, codes[1][j].w);
         }
     };
     // Plain rows: four a load, straight to shared memory.  Where a wave's 16 are in one page the address of the first is the wave's, not a lane's.
@@ -171,16 +175,16 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
             const int64_t from = (int64_t)(uint32_t)__builtin_amdgcn_readlane(r, wave * 16) * 256;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                load_to_lds(to + j * 1024, (const char *)a.k_pages + from, (4 * j + in4) * 256 + 16 * (c16 ^ ((4 * j + in4) & 7)));
-                load_to_lds(to + Tile::kKeyBytes + j * 1024, (const char *)a.v_pages + from, (4 * j + in4) * 256 + 16 * (c16 ^ (in4 << 1)));
+                load_to_lds(to + j * 1024, (const char *)a.k_pages + from, (4 * j + in4) * 256 + 16 * (c16 ^ (4 * j + in4)));
+                load_to_lds(to + Tile::kKeyBytes + j * 1024, (const char *)a.v_pages + from, (4 * j + in4) * 256 + 16 * (c16 ^ (in4 << 2)));
             }
             return;
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int64_t from = (int64_t)(uint32_t)__shfl((int)r, wave * 16 + 4 * j + in4) * 256;
-            row_to_lds(to + j * 1024, (const char *)a.k_pages + from + 16 * (c16 ^ ((4 * j + in4) & 7)));
-            row_to_lds(to + Tile::kKeyBytes + j * 1024, (const char *)a.v_pages + from + 16 * (c16 ^ (in4 << 1)));
+            row_to_lds(to + j * 1024, (const char *)a.k_pages + from + 16 * (c16 ^ (4 * j + in4)));
+            row_to_lds(to + Tile::kKeyBytes + j * 1024, (const char *)a.v_pages + from + 16 * (c16 ^ (in4 << 2)));
         }
     };
     auto whole = [&](int i, uint64_t none) { return none == 0 && (tile_of(i) + 1) * kKeys <= range.hi; };
@@ -238,7 +242,7 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
                                 const int d = 32 * db + 8 * (e >> 2) + 4 * half + (e & 3);
-                                const float x = __uint_as_float((uint32_t)*reinterpret_cast<const bf16_t *>(from + (((d >> 3) ^ ((k & 3) << 1)) << 4) + 2 * (d & 7)) << 16);
+                                const float x = __uint_as_float((uint32_t)*reinterpret_cast<const bf16_t *>(from + (((d >> 3) ^ ((k & 3) << 2)) << 4) + 2 * (d & 7)) << 16);
                                 if (sees && !(fabsf(x) < INFINITY)) o[db][e] += x;
                             }
                     }
@@ -336,7 +340,7 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
         ++i;
     }
     if constexpr (kCodes) scale_outputs(o, exponent - 15);
-    many_finish<T>(a, s, split, t0 == t1, row < rows, token, head, m, half_sum(l), o, half);
+    many_finish<T, RowsTile<kCodes>>(a, s, split, t0 == t1, row < rows, token, head, m, half_sum(l), o, half);
 }
 
 }  // namespace ctkvr

@@ -27,14 +27,14 @@ __device__ __forceinline__ float groups_sum(float x)
 
 // A tile of 32 keys in shared memory: their rows of codes, those of their values, and their scales (K's, then V's); of bf16 the values alone, since there is not the
 // room for twice as many blocks otherwise (16 sequences of 4100 keys 62 us with both, 57 so).  The 16-byte chunk c of row r stands at
-// chunk c ^ r % 8 (keys) or c ^ swz(r) (values), so that the rows that eight lanes take at one chunk, and those that 16 lanes of the transposing loads take, fall on all
-// banks once: eight of a chunk of codes (4 g .. 4 g + 3 and 16 more), four of two chunks of bf16 (4 g .. 4 g + 3).
+// chunk c ^ r / 2 % 8 (keys) or c ^ swz(r) (values), so that the 16 rows of keys that lanes take at one chunk, and those that 32 lanes of the transposing loads take, fall
+// on all 64 banks once: 16 of a chunk of codes (8 g .. 8 g + 7 and 16 more), eight of two chunks of bf16 (8 g .. 8 g + 7).
 template <int STORE> struct TokenTile {
     static constexpr int kRowBytes = STORE == kPlain ? 256 : 128, kHalf = 32 * kRowBytes, kChunks = kRowBytes / 16;
     static constexpr int kBytes = STORE == kPlain ? kHalf : 2 * kHalf + 256;
     static constexpr int kPer = 64 / kChunks, kRowLoads = 32 / kPer;   // rows of one load of a wave, and loads of K or V
     static constexpr int kLoads = 2 * kRowLoads + 1;   // of a tile of codes
-    static __device__ __forceinline__ int swz(int r) { return STORE == kPlain ? (r & 7) << 1 : (r & 3) | ((r >> 2) & 4); }
+    static __device__ __forceinline__ int swz(int r) { return STORE == kPlain ? (r & 7) << 1 : ((r >> 1) & 3) | ((r >> 2) & 4); }
 };
 // 4 bytes a lane from `from` into shared memory at byte `to` + 4 * lane
 __device__ __forceinline__ void word_to_lds(uint32_t to, const void *from)
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
         for (int j = 0; j < Tile::kRowLoads; ++j) {
             const int key = j * Tile::kPer + lane / Tile::kChunks, c = lane % Tile::kChunks;
             const int64_t from = (int64_t)(uint32_t)__shfl((int)r, key) * Tile::kRowBytes;
-            if constexpr (kCodes) row_to_lds(to + j * 1024, (const char *)a.k_pages + from + 16 * (c ^ (key & 7)));
+            if constexpr (kCodes) row_to_lds(to + j * 1024, (const char *)a.k_pages + from + 16 * (c ^ ((key >> 1) & 7)));
             row_to_lds(values_to + j * 1024, (const char *)a.v_pages + from + 16 * (c ^ Tile::swz(key)));
         }
         if constexpr (kCodes) word_to_lds(to + 2 * Tile::kHalf, (lane < 32 ? qa.k_scales : qa.v_scales) + r);
@@ -256,7 +256,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
                 bf16x8_t x;
                 const char *row_at = kt_ + (16 * kb + r16) * Tile::kRowBytes;
                 if constexpr (kCodes) {
-                    const uint4 w = *reinterpret_cast<const uint4 *>(row_at + (((part + 4 * (i >> 1)) ^ (r16 & 7)) << 4));
+                    const uint4 w = *reinterpret_cast<const uint4 *>(row_at + (((part + 4 * (i >> 1)) ^ (r16 >> 1)) << 4));
                     x = (i & 1) ? codes8<STORE>(w.z, w.w) : codes8<STORE>(w.x, w.y);
                 } else {
                     x = k[kb][i];
