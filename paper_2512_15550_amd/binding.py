@@ -431,8 +431,10 @@ class Cache:
         self.device = device
         self.torch_dtype = _torch_dtype(p.dtype)
         self.n_axes = 1 if p.rope_axis is None else int(np.max(p.rope_axis)) + 1
+        from . import _marshal   # compiled with the library; missing: build it, as that
         # what every call asks for; a step of one token is a few microseconds, of which looking these up again would be a fair part
         self._lib = load_library()
+        self._pointer, self._rows = _marshal.pointer, _marshal.rows
         self._int, self._float = torch.int32, torch.float32
         self._shapes = {"pages": (p.num_pages, p.n_kv_heads, p.page_size, 128), "cu": (p.batch + 1,), "batch": (p.batch,),
                         "table": (p.batch, p.max_pages), "heads": (p.n_q_heads,), "scales": (p.num_pages, p.n_kv_heads, p.page_size)}
@@ -455,8 +457,9 @@ def _on(cache: Cache, name, t, dtype, shape):
     """Device pointer of a contiguous tensor of this type and shape on the cache's device (None passes NULL)."""
     if t is None:
         return None
-    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == cache.device:
-        return t.data_ptr()
+    p = cache._pointer(t, dtype, shape, cache.device)
+    if p != -1:
+        return p
     raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on device {cache.device}, got "
                      f"{t.dtype}, {tuple(t.shape)}, strides {t.stride()}, {t.device}")
 
@@ -465,10 +468,9 @@ def _rows_on(cache: Cache, name, t, total, heads):
     """Device pointer and token stride of [total][heads][128], the heads of a token contiguous."""
     if t is None:
         return None, 0
-    if t.dtype is cache.torch_dtype and t.shape == (total, heads, 128) and t.get_device() == cache.device:
-        token, head, element = t.stride()
-        if total == 0 or (element == 1 and (heads == 1 or head == 128)):
-            return t.data_ptr(), (token if total > 1 else heads * 128)
+    p = cache._rows(t, cache.torch_dtype, total, heads, cache.device)
+    if p is not None:
+        return p
     raise ValueError(f"{name}: expected a {cache.torch_dtype} tensor of shape {(total, heads, 128)} on device {cache.device}, a token's heads "
                      f"contiguous, got {t.dtype}, {tuple(t.shape)}, strides {t.stride()}, {t.device}")
 

@@ -1,13 +1,15 @@
 """Compile the HIP library for gfx950 with hipcc, in-tree: six translation units (the host side with the staged and build kernels; the
 single-launch decode kernel; the operators on the paged KV cache; those on 8-bit rows, windows and drafts, whose attention over 8-bit rows has one for
-each type of query), compiled side by side, then linked."""
+each type of query), compiled side by side, then linked; and the binding's checks of tensors, an extension module of the interpreter."""
 import os
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = ["ctkvr.hip", "fused.hip", "cache.hip", "quant.hip", "quant_bf16.hip", "quant_f32.hip"]
 LIB = os.path.join(HERE, "libctkvr.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 
 HIPCC_FLAGS = [
@@ -24,6 +26,14 @@ HIPCC_FLAGS = [
 ]
 
 
+def marshal_command():
+    import torch
+    root = os.path.dirname(os.path.abspath(torch.__file__))
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(root, "include"), "-I" + os.path.join(root, "include", "torch", "csrc", "api", "include"),
+            "-o", MARSHAL, os.path.join(CSRC, "marshal.cpp"), "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+
+
 def build_library(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     os.makedirs(OBJ_DIR, exist_ok=True)
@@ -34,12 +44,17 @@ def build_library(verbose: bool = False) -> str:
         if verbose:
             print(" ".join(cmd))
         jobs.append((obj, cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    cmd = marshal_command()
+    if verbose:
+        print(" ".join(cmd))
+    jobs.append((None, cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     objs = []
     for obj, cmd, proc in jobs:
         out, _ = proc.communicate()
         if proc.returncode != 0:
-            raise RuntimeError("hipcc failed: " + " ".join(cmd) + "\n" + out)
-        objs.append(obj)
+            raise RuntimeError("compilation failed: " + " ".join(cmd) + "\n" + out)
+        if obj:
+            objs.append(obj)
     link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     if verbose:
         print(" ".join(link))

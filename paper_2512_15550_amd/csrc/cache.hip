@@ -123,13 +123,12 @@ int ctkvr_cache_create(const ctkvr_cache_params *p, void *hip_stream, ctkvr_cach
         room(plan.nsplit, plan.tiles);
         const int64_t slots = (int64_t)p->max_pages * p->page_size;
         for (const int64_t keys : {slots, std::min<int64_t>(slots, 4095)})   // (fewer are split less, in the form that they get)
-            for (const bool codes : {false, true}) {
-                const SightPlan sight = sight_plan(c, total, keys, codes);
+            for (const int form : {0, 1, 2, 3}) {
+                const SightPlan sight = sight_plan(c, total, keys, form & 1, form & 2);
                 room(sight.nsplit, sight.tiles);
             }
         if (most == 1 && (((int64_t)total << c->lg) >> 7) * p->n_kv_heads >= 8ll * c->num_cu) break;   // more tokens are never split again
     }
-    if (const char *e = getenv("SP_ROOM")) part_rows = std::max(part_rows, (size_t)atoll(e)), counts = std::max(counts, (size_t)1 << 20);
     c->part_rows = part_rows;
     c->counts = counts;
     if (part_rows) {

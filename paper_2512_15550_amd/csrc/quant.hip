@@ -82,7 +82,8 @@ template <int SIGHT> int attend(const ctkvr_cache *c, const AttnCall &x, const S
     qa.k_scales = x.k_scales;
     qa.v_scales = x.v_scales;
     const int64_t slots = (int64_t)c->p.max_pages * c->p.page_size;
-    const SightPlan plan = sight_plan(c, x.total, SIGHT == kWindow ? std::min<int64_t>(slots, (int64_t)o.window + o.sinks + x.total) : slots, x.format != CTKVR_KV_PLAIN);
+    const SightPlan plan = sight_plan(c, x.total, SIGHT == kWindow ? std::min<int64_t>(slots, (int64_t)o.window + o.sinks + x.total) : slots,
+                                      x.format != CTKVR_KV_PLAIN, SIGHT == kWindow);
     if (plan.nsplit > 1 && ((size_t)plan.nsplit * x.total * c->p.n_q_heads > c->part_rows || (size_t)plan.tiles * c->p.n_kv_heads > c->counts))
         return fail(CTKVR_EHIP, "%d runs of %d tokens: beyond the workspace", plan.nsplit, x.total);
     a.tiles = plan.tiles;
@@ -176,9 +177,9 @@ int ctkvr_cache_quant_read(ctkvr_cache *c, int32_t format, const void *k_codes, 
     a.out_table = out_table;
     a.out_cols = out_max_pages;
     a.out_pages = (uint32_t)out_num_pages;
-    // (a run of 32 tokens a block, up to 16 blocks a CU; the rest of a wide table goes round)
+    // (a run of 64 tokens a block, up to 16 blocks a CU; the rest of a wide table goes round)
     const int64_t units = (int64_t)c->p.batch * c->p.n_kv_heads, most = (int64_t)std::min(c->p.max_pages, out_max_pages) * c->p.page_size;
-    const dim3 grid((unsigned)units, (unsigned)std::max<int64_t>(1, std::min<int64_t>((most + 31) / 32, 16ll * c->num_cu / units)));
+    const dim3 grid((unsigned)units, (unsigned)std::max<int64_t>(1, std::min<int64_t>((most + 63) / 64, 16ll * c->num_cu / units)));
     hipStream_t st = (hipStream_t)hip_stream;
     if (c->p.dtype == CTKVR_BF16) {
         if (format == CTKVR_KV_INT8) quant_read_kernel<bf16_t, kInt8><<<grid, 256, 0, st>>>(a);

@@ -126,46 +126,58 @@ struct QuantReadArgs {
     int out_cols;
     uint32_t out_pages;
 };
-// 16 codes times their row's scale
-template <int STORE> __device__ __forceinline__ void decode(uint32_t w, float scale, float (&x)[4])
+// four codes times their row's scale
+template <int STORE> __device__ __forceinline__ f32x4_t decode(uint32_t w, float scale)
 {
     if constexpr (STORE == kInt8) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(w >> (8 * i)) * scale;
+        return f32x4_t{(float)(int8_t)w, (float)(int8_t)(w >> 8), (float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24)} * scale;
     } else {
         const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-        x[0] = a[0] * scale;
-        x[1] = a[1] * scale;
-        x[2] = b[0] * scale;
-        x[3] = b[1] * scale;
+        return f32x4_t{a[0], a[1], b[0], b[1]} * scale;
     }
 }
-// A block takes runs of 32 tokens of a unit, 8 lanes a row, 16 codes a lane
+// A block takes runs of 64 tokens of a unit: 16 lanes a row, 8 codes a lane, so that a row's values are written in a line, and four rows a lane on their way at once.
 template <typename T, int STORE> __global__ __launch_bounds__(256) void quant_read_kernel(QuantReadArgs a)
 {
+    constexpr int kRun = 64, kEach = 4;
     const CacheView &v = a.v;
-    const int b = blockIdx.x / v.g, kv = blockIdx.x % v.g, i8 = threadIdx.x & 7;
+    const int b = blockIdx.x / v.g, kv = blockIdx.x % v.g, i16 = threadIdx.x & 15;
     const int len = min(max(v.cur[b], 0), v.max_pages << v.page_shift), from = a.first ? max(a.first[b], 0) : 0;
     const int n = min(len - from, a.out_cols << v.page_shift), mask = (1 << v.page_shift) - 1;
-    for (int j = blockIdx.y * 32 + (threadIdx.x >> 3); j < n; j += gridDim.y * 32) {
-        const int64_t row = cache_row(v, b, kv, from + j);
-        const uint32_t page = (uint32_t)a.out_table[(size_t)b * a.out_cols + (j >> v.page_shift)];
-        if (row < 0 || page >= a.out_pages) continue;
-        const int64_t to = (((int64_t)page * v.g + kv) << v.page_shift) + (j & mask);
+    for (int run = blockIdx.y * kRun; run < n; run += gridDim.y * kRun) {
+        int64_t src[kEach], dst[kEach];
+        bool ok[kEach];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (!a.codes[i]) continue;
-            const uint4 c = *reinterpret_cast<const uint4 *>(a.codes[i] + row * 128 + 16 * i8);
-            const float scale = a.scales[i][row];
-            float x[4][4];
-            decode<STORE>(c.x, scale, x[0]);
-            decode<STORE>(c.y, scale, x[1]);
-            decode<STORE>(c.z, scale, x[2]);
-            decode<STORE>(c.w, scale, x[3]);
-            T *out = (T *)a.out[i] + to * 128 + 16 * i8;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) store4(out + 4 * e, f32x4_t{x[e][0], x[e][1], x[e][2], x[e][3]});
+        for (int e = 0; e < kEach; ++e) {
+            const int j = run + 16 * e + (threadIdx.x >> 4), at = min(j, n - 1);
+            const uint32_t page = (uint32_t)a.out_table[(size_t)b * a.out_cols + (at >> v.page_shift)];
+            src[e] = cache_row(v, b, kv, from + at);
+            dst[e] = (((int64_t)page * v.g + kv) << v.page_shift) + (at & mask);
+            ok[e] = j < n && src[e] >= 0 && page < a.out_pages;
+            if (!ok[e]) src[e] = 0;
         }
+        uint2 w[2][kEach];
+        float scale[2][kEach];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            if (a.codes[x]) {
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) {
+                    w[x][e] = *reinterpret_cast<const uint2 *>(a.codes[x] + src[e] * 128 + 8 * i16);
+                    scale[x][e] = a.scales[x][src[e]];
+                }
+            }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            if (a.codes[x]) {
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) {
+                    if (!ok[e]) continue;
+                    const f32x4_t lo = decode<STORE>(w[x][e].x, scale[x][e]), hi = decode<STORE>(w[x][e].y, scale[x][e]);
+                    const float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                    store_chunk((T *)a.out[x] + dst[e] * 128 + 8 * i16, y);
+                }
+            }
     }
 }
 

@@ -1,36 +1,45 @@
 // How attention over 8-bit rows, in windows and of drafted tokens falls into blocks.
 #pragma once
-#include <stdlib.h>
-
 #include "cache_host.hpp"
 
 namespace ctkvr {
 
-// How a call's rows and keys fall into blocks: tiles of 16, 32 or 128 rows
+// How a call's rows and keys fall into blocks: tiles of 16, 32 or 128 rows.  us, in that order, 32 heads on 8 KV heads in bf16:
+//   Up to 16 rows a unit take tiles of 16.  More take tiles of 128 where these fill the chip (2048 tokens on as many keys 129, 87, 69; four sequences of 300 in a
+// window of 1024 106, 65, 48) and where the keys are long enough to be split and the rows enough (one sequence's 16 / 32 tokens on 32K codes 40, 35, 44 / 68, 52, 48;
+// 64 rows a unit of eight sequences, codes 120 and 149, plain 180 and 161); else those of 32 (500 tokens on as many keys 20, 15, 23), or of 16 where that leaves half the
+// CUs idle (on 2 KV heads 11, 15, 23).
+//   With fp32 queries a tile of 32 rows has more registers than two waves a SIMD: 16 or 128 rows (100 / 512 tokens on 8192 keys 70, 83, 62 / 220, 266, 194; 8 on 32K 32,
+// 34, 57; 500 on as many, 2 KV heads, 13, 16, 35).  Over plain fp32 rows it is 32 or 128, as in ctkvr_cache_attn.
+//   Keys are split into runs where blocks would be too few, to so many blocks a CU: single tokens of one sequence, and in windows, whose runs are alike, one; of
+// several sequences, whose lengths differ, half as many as these, 2 to 8 (up to 64K keys, two sequences 25, 31, 36 with 2, 4, 8; four 63, 65, 69; sixteen 267, 248, 240); tiles
+// of 32 as many as the sequences (eight of 32 rows 110, 99, 93), tiles of 128 four; one sequence's larger tiles, and with fp32 queries, two.  A run has 256 keys at least, 1024
+// with tiles of 128, 2048 where the tiles fill half the chip by themselves: the join of the runs costs 4 us and more.  It is done by the block that ends last, without a
+// launch of its own, where that reads little and all blocks run at once (16 sequences in windows of 4096 55.4 -> 54.1, but causal in eight blocks a CU 239 -> 241).
 struct SightPlan {
     int log;   // of a tile's rows
     int tiles, nsplit;
-    bool join_inside;
+    bool join_inside;   // by the block that ends last, not by a launch of its own
 };
 // keys: those that a row may see, at most
-inline SightPlan sight_plan(const ctkvr_cache *c, int total, int64_t keys, bool codes)
+inline SightPlan sight_plan(const ctkvr_cache *c, int total, int64_t keys, bool codes, bool window)
 {
     const int64_t rows = (int64_t)total << c->lg, g = c->p.n_kv_heads, cus = c->num_cu;
     const int used = std::min(total, c->p.batch);   // sequences with new tokens, at most
-    const bool bf16 = c->p.dtype == CTKVR_BF16;
-    // a sequence's rows are a multiple of the group's size, so that rounding each up to tiles adds no more than that
+    const bool bf16 = c->p.dtype == CTKVR_BF16, is_long = keys >= 4096;
+    // (a sequence's rows are a multiple of the group's size, so that rounding each up to tiles adds no more than that)
     auto tiles = [&](int log) { return (rows + used * (int64_t)((1 << log) - c->G)) >> log; };
+    const bool wide = tiles(7) * g >= cus;
     SightPlan p{};
-    p.log = rows <= 16ll * used && (bf16 || codes) ? 4 : rows <= 64ll * used || (tiles(7) * g < cus && (!bf16 || keys < 4096 || rows < 512ll * used)) ? 5 : 7;
-    if (const char *e = getenv("SP_LOG")) p.log = atoi(e);
+    if (!bf16) p.log = codes ? (rows <= 64ll * used || (tiles(7) * g < cus / 2 && !is_long) ? 4 : 7) : rows <= 64ll * used || (!wide && (!is_long || rows < 512ll * used)) ? 5 : 7;
+    else if (rows <= 16ll * used) p.log = 4;
+    else if (wide || (is_long && rows > (codes ? 64ll : 48ll) * used)) p.log = 7;
+    else p.log = is_long || tiles(5) * g >= cus / 2 ? 5 : 4;
     p.tiles = (int)tiles(p.log);
-    const bool few = p.log < 7, enough = tiles(5) >= 2 * used && tiles(5) * g >= cus / 2;
-    int64_t want = (!few ? 2 : used > 1 ? 8 : bf16 ? 1 : 2) * cus, least = !few ? 1024 : enough ? 2048 : bf16 ? 256 : 64;
-    if (const char *e = getenv("SP_WANT")) want = atoi(e) * cus;
-    if (const char *e = getenv("SP_LEAST")) least = atoi(e);
-    p.nsplit = few || tiles(7) * g < cus ? (int)std::max<int64_t>(1, std::min({want / (p.tiles * g), (keys + least - 1) / least, (int64_t)kMaxSplit})) : 1;
-    p.join_inside = few && used == 1 && rows <= 8 && rows * p.nsplit <= (bf16 ? 256 : 128);
-    if (const char *e = getenv("SP_JOIN")) p.join_inside = atoi(e) && few;
+    const int per_cu = !bf16 ? 2 : p.log == 4 ? (window || used == 1 ? 1 : std::min(8, std::max(2, used / 2))) : used == 1 || window ? 2 : p.log == 5 ? std::min(8, used) : 4;
+    const int64_t want = (int64_t)per_cu * cus, least = p.tiles * g >= cus / 2 ? 2048 : p.log == 7 ? 1024 : 256;
+    p.nsplit = p.log == 7 && wide ? 1 : (int)std::max<int64_t>(1, std::min({want / (p.tiles * g), (keys + least - 1) / least, (int64_t)kMaxSplit}));
+    p.join_inside = p.log < 7 && rows <= 8 * used && rows * p.nsplit <= (bf16 ? 256 : 128) * used && p.tiles * g * p.nsplit <= 2 * cus;
     return p;
 }
 

@@ -161,8 +161,9 @@ def test_the_binding_refuses_types_and_shapes():
     import torch
 
     import paper_2512_15550_amd as ck
+    from paper_2512_15550_amd import _marshal
     from paper_2512_15550_amd import binding as B
-    c = types.SimpleNamespace(torch_dtype=torch.bfloat16, _float=torch.float32, device=-1,
+    c = types.SimpleNamespace(torch_dtype=torch.bfloat16, _float=torch.float32, device=-1, _pointer=_marshal.pointer, _rows=_marshal.rows,
                               _formats={torch.bfloat16: ck.KV_PLAIN, torch.int8: ck.KV_INT8, torch.float8_e4m3fn: ck.KV_FP8},
                               _shapes={"pages": (3, 2, 16, 128), "scales": (3, 2, 16)})
     codes, scales = torch.zeros((3, 2, 16, 128), dtype=torch.int8), torch.zeros((3, 2, 16))
@@ -177,3 +178,31 @@ def test_the_binding_refuses_types_and_shapes():
                 (codes[:, :, :, :64], scales, codes, scales), (codes, scales, codes.transpose(0, 1), scales)):
         with pytest.raises(ValueError):
             B._quant_on(c, 1, *bad)
+
+
+def test_tensors_are_checked_as_they_are_described():
+    """The compiled checks against what torch says of the tensors: type, shape, order, device, strides of rows."""
+    import torch
+
+    from paper_2512_15550_amd import _marshal as M
+    t = torch.zeros((6, 4, 16, 128), dtype=torch.bfloat16)
+    assert M.pointer(t, torch.bfloat16, (6, 4, 16, 128), -1) == t.data_ptr() == M.pointer(t, torch.bfloat16, t.shape, -1)
+    assert M.pointer(t[2:], torch.bfloat16, (4, 4, 16, 128), -1) == t[2:].data_ptr()
+    one = t[:, :1].contiguous()
+    assert M.pointer(one.transpose(0, 1), torch.bfloat16, (1, 6, 16, 128), -1) == one.data_ptr()      # (as contiguous as it was)
+    for bad, dtype, shape, device in ((t, torch.float16, t.shape, -1), (t, torch.bfloat16, (6, 4, 16), -1), (t, torch.bfloat16, (6, 4, 16, 127), -1),
+                                      (t, torch.bfloat16, (6, 4, 128, 16), -1), (t, torch.bfloat16, t.shape, 0), (t.transpose(0, 1), torch.bfloat16, (4, 6, 16, 128), -1),
+                                      (t[:, ::2], torch.bfloat16, (6, 2, 16, 128), -1), ([1], torch.bfloat16, (1,), -1), (None, torch.bfloat16, (1,), -1),
+                                      (t, "bf16", t.shape, -1), (t, torch.bfloat16, [6, 4, 16, 128], -1), (t.to_sparse(), torch.bfloat16, t.shape, -1)):
+        assert M.pointer(bad, dtype, shape, device) == -1
+    assert M.pointer(t) == -1
+    empty = torch.zeros((0, 4), dtype=torch.int32)
+    assert M.pointer(empty, torch.int32, (0, 4), -1) == empty.data_ptr()
+    fused = torch.zeros((5, 12 * 128 + 64), dtype=torch.float32)
+    q = fused[:, :1024].view(5, 8, 128)
+    assert M.rows(q, torch.float32, 5, 8, -1) == (q.data_ptr(), 12 * 128 + 64)
+    assert M.rows(q[:1], torch.float32, 1, 8, -1) == (q.data_ptr(), 1024)
+    assert M.rows(q[:0], torch.float32, 0, 8, -1) == (q[:0].data_ptr(), 1024)
+    assert M.rows(fused[:, 64:192].view(5, 1, 128), torch.float32, 5, 1, -1) == (fused[:, 64:].data_ptr(), 12 * 128 + 64)
+    for bad in (q.bfloat16(), q[:4], q[:, :4], q[..., :64], q.flip(1)[:, :, ::2], q.transpose(1, 2), q[:, ::2], q.reshape(5, 1024), None, 7):
+        assert M.rows(bad, torch.float32, 5, 8, -1) is None
