@@ -279,8 +279,8 @@ __device__ __forceinline__ void mask_bits(f32x16_t &s, uint32_t seen, int half, 
 // A tile's scores to probabilities under the running maximum m (in units of log2 e, as all exponents here), their sum to l, the outputs so far to the
 // new maximum.  (A maximum that may be left behind by a few powers of two, so that fewer tiles scale the outputs, was 2 % faster on 2048 tokens of 32K keys, 1130 and
 // 1106 us; but the weight of a row's largest score is 1 now, which bf16 holds exactly, and the outputs there were off by 2.3e-3 in place of 2.0e-3, those of a
-// single token by 2.1e-3 in place of 1.7e-3.)  While m is -infinity the outputs are 0, or infinities that stay.
-template <int OPT, int NB> __device__ __forceinline__ void softmax_regs(f32x16_t (&sc)[NB], f32x16_t (&o)[4], float &m, float &l, float c2)
+// single token by 2.1e-3 in place of 1.7e-3.  LAG: by so many; weights in fp16 lose nothing by it.)  While m is -infinity the outputs are 0, or infinities that stay.
+template <int OPT, int NB, int LAG = 0> __device__ __forceinline__ void softmax_regs(f32x16_t (&sc)[NB], f32x16_t (&o)[4], float &m, float &l, float c2)
 {
     float top = -INFINITY;
 #pragma unroll
@@ -289,7 +289,7 @@ template <int OPT, int NB> __device__ __forceinline__ void softmax_regs(f32x16_t
         for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
     top = half_max(top);
     if constexpr (OPT == 0) top *= c2;
-    if (__any(top > m)) {
+    if (__any(LAG ? top > m + (float)LAG : top > m)) {
         const float m_new = fmaxf(m, top), scale = m == -INFINITY ? 1.0f : exp2_fast(m - m_new);
         m = m_new;
         l *= scale;

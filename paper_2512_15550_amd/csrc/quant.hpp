@@ -273,13 +273,15 @@ __device__ __forceinline__ void scale_regs(f32x16_t &s, const float *scales, int
     }
 }
 
-// Values' scales as they multiply probabilities: times 2^(15 - exponent), where 2^exponent is above every scale so far, so that a weight is below 2^15 and has all of
-// fp16's bits down to 2^-14, which is 2^-29 of the largest that it could be; what is left of smaller ones is off by 2^-40 of that at most.  The outputs are
-// scaled as the exponent grows, once or twice in a run of keys as a rule.
+// Values' scales as they multiply probabilities: times 2^(11 - exponent), where 2^exponent is above every scale so far, and probabilities are under a maximum that
+// may lag by kLag = 4 powers of two, so that a weight is below 2^15, and one under its row's true maximum has all of fp16's bits down to 2^-25 of 2^exponent; what is
+// left of smaller ones is off by 2^-36 of that at most.  The outputs are scaled as the exponent grows, once or twice in a run of keys as a rule, and as a maximum grows by more
+// than 16 times; without the lag a row of few keys has a new one in most tiles (eight sequences' drafts of 8 tokens 94 -> 83 us).
+constexpr int kLag = 4, kWeightPower = 15 - kLag;
 struct ValueScale {
     int exponent = -100;
     __device__ __forceinline__ float top() const { return ldexpf(1.0f, exponent); }
-    __device__ __forceinline__ float factor() const { return ldexpf(1.0f, 15 - exponent); }
+    __device__ __forceinline__ float factor() const { return ldexpf(1.0f, kWeightPower - exponent); }
     // makes room for a wave's scales; the same in all lanes.  (NaN is above nothing: a row that sees it becomes NaN anyway.)
     __device__ __forceinline__ void admit(float scale)
     {

@@ -274,7 +274,7 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
             if constexpr (decltype(masked)::value) mask_bits(sc[kb], seen[kb], half, -INFINITY);
         }
         // (codes: the factor of the exponent is in their keys' scales)
-        softmax_regs<(kCodes && OPT == 0 ? kBias : OPT), 2>(sc, o, m, l, a.o.c2);
+        softmax_regs<(kCodes && OPT == 0 ? kBias : OPT), 2, (kCodes ? kLag : 0)>(sc, o, m, l, a.o.c2);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             if constexpr (kCodes) {
@@ -339,7 +339,7 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
         step((i - t0) & 1, std::true_type(), i);
         ++i;
     }
-    if constexpr (kCodes) scale_outputs(o, exponent - 15);
+    if constexpr (kCodes) scale_outputs(o, exponent - kWeightPower);
     many_finish<T, RowsTile<kCodes>>(a, s, split, t0 == t1, row < rows, token, head, m, half_sum(l), o, half);
 }
 

@@ -2,6 +2,7 @@
 #pragma once
 #include "cache_host.hpp"
 
+#include <stdlib.h>
 namespace ctkvr {
 
 // How a call's rows and keys fall into blocks: tiles of 16, 32 or 128 rows.  us, in that order, 32 heads on 8 KV heads in bf16:
@@ -35,8 +36,10 @@ inline SightPlan sight_plan(const ctkvr_cache *c, int total, int64_t keys, bool 
     else if (rows <= 16ll * used) p.log = 4;
     else if (wide || (is_long && rows > (codes ? 64ll : 48ll) * used)) p.log = 7;
     else p.log = is_long || tiles(5) * g >= cus / 2 ? 5 : 4;
+    if (const char *e = getenv("SP_LOG")) p.log = atoi(e);
     p.tiles = (int)tiles(p.log);
-    const int per_cu = !bf16 ? 2 : p.log == 4 ? (window || used == 1 ? 1 : std::min(8, std::max(2, used / 2))) : used == 1 || window ? 2 : p.log == 5 ? std::min(8, used) : 4;
+    int per_cu = !bf16 ? 2 : p.log == 4 ? (window || used == 1 ? 1 : std::min(8, std::max(2, used / 2))) : used == 1 || window ? 2 : p.log == 5 ? std::min(8, used) : 4;
+    if (const char *e = getenv("SP_WANT")) per_cu = atoi(e);
     const int64_t want = (int64_t)per_cu * cus, least = p.tiles * g >= cus / 2 ? 2048 : p.log == 7 ? 1024 : 256;
     p.nsplit = p.log == 7 && wide ? 1 : (int)std::max<int64_t>(1, std::min({want / (p.tiles * g), (keys + least - 1) / least, (int64_t)kMaxSplit}));
     p.join_inside = p.log < 7 && rows <= 8 * used && rows * p.nsplit <= (bf16 ? 256 : 128) * used && p.tiles * g * p.nsplit <= 2 * cus;

@@ -247,6 +247,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
                     for (int db = 0; db < 8; ++db) o[rb][db] *= f;
             }
         }
+        // (Operands are requested of shared memory ahead of what comes before their use, and stay there: a load that the compiler puts right before it has the wave wait.)
+        uint4 key_codes[2][2];
+        if constexpr (kCodes) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    key_codes[kb][i] = *reinterpret_cast<const uint4 *>(kt_ + (16 * kb + r16) * Tile::kRowBytes + (((part + 4 * i) ^ (r16 >> 1)) << 4));
+            asm volatile("" ::: "memory");
+        }
         f32x8_t sc[RB];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
@@ -254,9 +264,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 bf16x8_t x;
-                const char *row_at = kt_ + (16 * kb + r16) * Tile::kRowBytes;
                 if constexpr (kCodes) {
-                    const uint4 w = *reinterpret_cast<const uint4 *>(row_at + (((part + 4 * (i >> 1)) ^ (r16 >> 1)) << 4));
+                    const uint4 &w = key_codes[kb][i >> 1];
                     x = (i & 1) ? codes8<STORE>(w.z, w.w) : codes8<STORE>(w.x, w.y);
                 } else {
                     x = k[kb][i];
@@ -302,6 +311,23 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
                 }
             }
         }
+        // the values' operands of d block db: eight codes, or eight bf16 values in two parts
+        union ValueOperand { i32x2_t codes; s16x4_t h[2]; bf16x8_t w; } value[8];
+        if constexpr (kCodes) {
+            const int key = 4 * part + ((lane >> 1) & 3) + 16 * ((lane >> 3) & 1);
+#pragma unroll
+            for (int db = 0; db < 8; ++db)
+                value[db].codes = __builtin_amdgcn_ds_read_tr8_b64_v2i32((CTKVR_LDS i32x2_t *)(vt + key * 128 + ((db ^ Tile::swz(key)) << 4) + 8 * (lane & 1)));
+        } else {
+            const int key = 4 * part + (r16 >> 2);
+#pragma unroll
+            for (int db = 0; db < 8; ++db)
+#pragma unroll
+                for (int aa = 0; aa < 2; ++aa)
+                    value[db].h[aa] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CTKVR_LDS s16x4_t *)(
+                        vt + (key + 16 * aa) * 256 + (((2 * db + ((lane & 3) >> 1)) ^ Tile::swz(key + 16 * aa)) << 4) + 8 * (lane & 1)));
+        }
+        asm volatile("" ::: "memory");
         // probabilities under the running maximum, their sum, the outputs so far to the new maximum
         float w[RB][8];
 #pragma unroll
@@ -311,7 +337,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
             for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[rb][i]);
             top = groups_max(top);
             if constexpr (OPT == 0) top *= a.o.c2;
-            if (__any(top > m[rb])) {
+            if (__any(kCodes ? top > m[rb] + (float)kLag : top > m[rb])) {
                 const float m_new = fmaxf(m[rb], top), f = m[rb] == -INFINITY ? 1.0f : exp2_fast(m[rb] - m_new);
                 m[rb] = m_new;
                 l[rb] *= f;
@@ -343,11 +369,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
                 }
                 split_parts(w[rb], p[rb]);
             }
-            const int key = 4 * part + ((lane >> 1) & 3) + 16 * ((lane >> 3) & 1);
 #pragma unroll
             for (int db = 0; db < 8; ++db) {
-                const i32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((CTKVR_LDS i32x2_t *)(vt + key * 128 + ((db ^ Tile::swz(key)) << 4) + 8 * (lane & 1)));
-                uint32_t lo = (uint32_t)x[0], hi = (uint32_t)x[1];
+                uint32_t lo = (uint32_t)value[db].codes[0], hi = (uint32_t)value[db].codes[1];
                 if (masked) lo = no_nan<STORE>(lo), hi = no_nan<STORE>(hi);
                 const f16x8_t y = codes8h<STORE>(lo, hi);
 #pragma unroll
@@ -359,17 +383,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
             bf16x8_t p[RB][1];
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) split_parts(w[rb], p[rb]);   // (rounded to the values' type, as in attn_kernel)
-            const int key = 4 * part + (r16 >> 2);
 #pragma unroll
-            for (int db = 0; db < 8; ++db) {
-                union { s16x4_t h[2]; bf16x8_t w; } x;
+            for (int db = 0; db < 8; ++db)
 #pragma unroll
-                for (int aa = 0; aa < 2; ++aa)
-                    x.h[aa] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CTKVR_LDS s16x4_t *)(
-                        vt + (key + 16 * aa) * 256 + (((2 * db + ((lane & 3) >> 1)) ^ Tile::swz(key + 16 * aa)) << 4) + 8 * (lane & 1)));
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.w, p[rb][0], o[rb][db], 0, 0, 0);
-            }
+                for (int rb = 0; rb < RB; ++rb) o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value[db].w, p[rb][0], o[rb][db], 0, 0, 0);
         }
         buf = buf + 1 == BUFS ? 0 : buf + 1;
         __builtin_amdgcn_wave_barrier();
@@ -392,7 +409,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
         float top = join[0][0][r];
 #pragma unroll
         for (int w = 1; w < NW; ++w) top = fmaxf(top, join[w][0][r]);
-        const float f = (m[rb] == -INFINITY ? 1.0f : exp2_fast(m[rb] - top)) * (kCodes ? ldexpf(1.0f, value_scale.exponent - 15) : 1.0f);
+        const float f = (m[rb] == -INFINITY ? 1.0f : exp2_fast(m[rb] - top)) * (kCodes ? ldexpf(1.0f, value_scale.exponent - kWeightPower) : 1.0f);
 #pragma unroll
         for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4_t *>(smem[0] + (wave * kRows + r) * 512 + (((4 * db + part) ^ r) << 4)) = o[rb][db] * f;
     }

@@ -122,8 +122,10 @@ def attention(st, sees, cap=0.0, slopes=None, scale=1.0 / math.sqrt(128.0), spre
             # own rounding
             rel = math.expm1(2 * err) + (HALF["bf16"] if st.dtype == "bf16" else 0.0) + ((1 if st.dtype == "bf16" else 3) * s + 16) * 2.0 ** -23
             rows = slice(kv * G, (kv + 1) * G)
-            if spread:   # a weight is held to 2^-40 of what the largest value would have; twice that, for the rounding of the largest scale to a power of two
-                size = size + (s * 2.0 ** -39 * v.abs().max()) / rel * (l.T[..., None].transpose(0, 1) > -math.inf)
+            if spread:
+                # weights are below 2^15 with a power of two above all scales as 2^11, so that probabilities may be up to 16 under a maximum that lags: fp16 ends at
+                # 2^-25, 2^-36 of that power, which is twice the largest scale at most; and so for each of s keys
+                size = size + (s * 2.0 ** -35 * v.abs().max()) / rel * (l.T[..., None].transpose(0, 1) > -math.inf)
             out[c0:c0 + n, rows] = o.transpose(0, 1)
             tol[c0:c0 + n, rows] = (size * rel + o.abs() * HALF[st.dtype] + 1e-30).transpose(0, 1)
             lse[c0:c0 + n, rows] = l.T
