@@ -434,7 +434,7 @@ class Cache:
         from . import _marshal   # compiled with the library; missing: build it, as that
         # what every call asks for; a step of one token is a few microseconds, of which looking these up again would be a fair part
         self._lib = load_library()
-        self._pointer, self._rows = _marshal.pointer, _marshal.rows
+        self._pointer, self._pointers, self._rows = _marshal.pointer, _marshal.pointers, _marshal.rows
         self._int, self._float = torch.int32, torch.float32
         self._shapes = {"pages": (p.num_pages, p.n_kv_heads, p.page_size, 128), "cu": (p.batch + 1,), "batch": (p.batch,),
                         "table": (p.batch, p.max_pages), "heads": (p.n_q_heads,), "scales": (p.num_pages, p.n_kv_heads, p.page_size)}
@@ -462,6 +462,12 @@ def _on(cache: Cache, name, t, dtype, shape):
         return p
     raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on device {cache.device}, got "
                      f"{t.dtype}, {tuple(t.shape)}, strides {t.stride()}, {t.device}")
+
+
+def _all_on(cache: Cache, *tensors):
+    """``_on`` of (name, tensor, type, shape) after (name, tensor, type, shape), in one go."""
+    p = cache._pointers(cache.device, *tensors)
+    return p if type(p) is tuple else _on(cache, *tensors[4 * p:4 * p + 4])
 
 
 def _rows_on(cache: Cache, name, t, total, heads):
@@ -574,68 +580,71 @@ def _format_of(cache: Cache, k, plain=False) -> int:
     return f
 
 
-def _quant_on(cache: Cache, format, k, k_scales, v, v_scales):
-    """Format, codes (or plain pages) and scales of K and of V; None passes NULL."""
-    dtype = (k if k is not None else v).dtype
-    return (format, _on(cache, "k", k, dtype, cache._shapes["pages"]), _on(cache, "k_scales", k_scales, cache._float, cache._shapes["scales"]),
-            _on(cache, "v", v, dtype, cache._shapes["pages"]), _on(cache, "v_scales", v_scales, cache._float, cache._shapes["scales"]))
+def _batch_of(cache: Cache, cu_new, cur_lens, block_table):
+    s, i32 = cache._shapes, cache._int
+    return "cu_new", cu_new, i32, s["cu"], "cur_lens", cur_lens, i32, s["batch"], "block_table", block_table, i32, s["table"]
+
+
+def _quant_of(cache: Cache, k, k_scales, v, v_scales):
+    dtype, s, f32 = (k if k is not None else v).dtype, cache._shapes, cache._float
+    return "k", k, dtype, s["pages"], "k_scales", k_scales, f32, s["scales"], "v", v, dtype, s["pages"], "v_scales", v_scales, f32, s["scales"]
 
 
 def ctkvr_cache_quant_append(cache: Cache, q, k, v, cu_new, cur_lens, block_table, q_out, k_codes, k_scales, v_codes, v_scales, positions=None) -> None:
     """As ``ctkvr_cache_append``; the codes are torch.int8 or torch.float8_e4m3fn, the scales fp32 [num_pages][g][page].  q and q_out may be None."""
     p, total = cache.params, k.shape[0]
-    cu, cur, table = _batch_on(cache, cu_new, cur_lens, block_table)
     (qp, qs), (kp, ks) = _rows_on(cache, "q", q, total, p.n_q_heads), _rows_on(cache, "k", k, total, p.n_kv_heads)
     vp, vs = _rows_on(cache, "v", v, total, p.n_kv_heads)
-    _check(cache._lib.ctkvr_cache_quant_append(
-        cache.handle, qp, qs, kp, ks, vp, vs, _on(cache, "positions", positions, cache._int, (cache.n_axes, total)), cu, cur, table, total,
-        _on(cache, "q_out", q_out, cache.torch_dtype, (total, p.n_q_heads, 128)),
-        *_quant_on(cache, _format_of(cache, k_codes), k_codes, k_scales, v_codes, v_scales), cache.stream()))
+    cu, cur, table, pos, out, *codes = _all_on(
+        cache, *_batch_of(cache, cu_new, cur_lens, block_table), "positions", positions, cache._int, (cache.n_axes, total),
+        "q_out", q_out, cache.torch_dtype, (total, p.n_q_heads, 128), *_quant_of(cache, k_codes, k_scales, v_codes, v_scales))
+    _check(cache._lib.ctkvr_cache_quant_append(cache.handle, qp, qs, kp, ks, vp, vs, pos, cu, cur, table, total, out, _format_of(cache, k_codes), *codes,
+                                               cache.stream()))
 
 
 def ctkvr_cache_quant_read(cache: Cache, k_codes, k_scales, v_codes, v_scales, cur_lens, block_table, out_table, k_pages, v_pages, first_tokens=None) -> None:
     """Into plain pages [any number][g][page][128] by out_table int32 [batch][any number]; codes, scales and pages of K, or of V, may be None."""
-    s, some = cache._shapes, k_pages if k_pages is not None else v_pages
-    shape = (some.shape[0],) + s["pages"][1:]
-    _check(cache._lib.ctkvr_cache_quant_read(
-        cache.handle, *_quant_on(cache, _format_of(cache, k_codes if k_codes is not None else v_codes), k_codes, k_scales, v_codes, v_scales),
-        _on(cache, "first_tokens", first_tokens, cache._int, s["batch"]), _on(cache, "cur_lens", cur_lens, cache._int, s["batch"]),
-        _on(cache, "block_table", block_table, cache._int, s["table"]),
-        _on(cache, "out_table", out_table, cache._int, (cache.params.batch, out_table.shape[-1])), out_table.shape[-1], shape[0],
-        _on(cache, "k_pages", k_pages, cache.torch_dtype, shape), _on(cache, "v_pages", v_pages, cache.torch_dtype, shape), cache.stream()))
+    s, i32, some = cache._shapes, cache._int, k_pages if k_pages is not None else v_pages
+    shape, out_shape = (some.shape[0],) + s["pages"][1:], (cache.params.batch, out_table.shape[-1])
+    *codes, first, cur, table, out, k, v = _all_on(
+        cache, *_quant_of(cache, k_codes, k_scales, v_codes, v_scales), "first_tokens", first_tokens, i32, s["batch"], "cur_lens", cur_lens, i32, s["batch"],
+        "block_table", block_table, i32, s["table"], "out_table", out_table, i32, out_shape, "k_pages", k_pages, cache.torch_dtype, shape,
+        "v_pages", v_pages, cache.torch_dtype, shape)
+    _check(cache._lib.ctkvr_cache_quant_read(cache.handle, _format_of(cache, k_codes if k_codes is not None else v_codes), *codes, first, cur, table, out,
+                                             out_shape[1], shape[0], k, v, cache.stream()))
 
 
 def ctkvr_cache_quant_attn(cache: Cache, q, k_codes, k_scales, v_codes, v_scales, cu_new, cur_lens, block_table, out, out_lse=None, slopes=None,
                            prefix_lens=None, first_key=None) -> None:
-    h, total = cache.params.n_q_heads, q.shape[0]
-    cu, cur, table = _batch_on(cache, cu_new, cur_lens, block_table)
+    h, total, s, i32, f32 = cache.params.n_q_heads, q.shape[0], cache._shapes, cache._int, cache._float
     qp, qs = _rows_on(cache, "q", q, total, h)
-    _check(cache._lib.ctkvr_cache_quant_attn(
-        cache.handle, qp, qs, *_quant_on(cache, _format_of(cache, k_codes), k_codes, k_scales, v_codes, v_scales), cu, cur, table, total,
-        *_masks_on(cache, total, slopes, prefix_lens, first_key), _on(cache, "out", out, cache.torch_dtype, (total, h, 128)),
-        _on(cache, "out_lse", out_lse, cache._float, (total, h)), cache.stream()))
+    cu, cur, table, kp, ks, vp, vs, *rest = _all_on(
+        cache, *_batch_of(cache, cu_new, cur_lens, block_table), *_quant_of(cache, k_codes, k_scales, v_codes, v_scales), "slopes", slopes, f32, s["heads"],
+        "prefix_lens", prefix_lens, i32, s["batch"], "first_key", first_key, i32, (total,), "out", out, cache.torch_dtype, (total, h, 128),
+        "out_lse", out_lse, f32, (total, h))
+    _check(cache._lib.ctkvr_cache_quant_attn(cache.handle, qp, qs, _format_of(cache, k_codes), kp, ks, vp, vs, cu, cur, table, total, *rest, cache.stream()))
 
 
 def ctkvr_cache_window_attn(cache: Cache, q, k_pages, v_pages, cu_new, cur_lens, block_table, window, out, n_sink=0, out_lse=None, slopes=None,
                             k_scales=None, v_scales=None) -> None:
     """k_pages and v_pages are plain, or codes with their scales."""
-    h, total = cache.params.n_q_heads, q.shape[0]
-    cu, cur, table = _batch_on(cache, cu_new, cur_lens, block_table)
+    h, total, f32 = cache.params.n_q_heads, q.shape[0], cache._float
     qp, qs = _rows_on(cache, "q", q, total, h)
-    _check(cache._lib.ctkvr_cache_window_attn(
-        cache.handle, qp, qs, *_quant_on(cache, _format_of(cache, k_pages, True), k_pages, k_scales, v_pages, v_scales), cu, cur, table, total, int(window),
-        int(n_sink), _on(cache, "slopes", slopes, cache._float, cache._shapes["heads"]), _on(cache, "out", out, cache.torch_dtype, (total, h, 128)),
-        _on(cache, "out_lse", out_lse, cache._float, (total, h)), cache.stream()))
+    cu, cur, table, kp, ks, vp, vs, *rest = _all_on(
+        cache, *_batch_of(cache, cu_new, cur_lens, block_table), *_quant_of(cache, k_pages, k_scales, v_pages, v_scales),
+        "slopes", slopes, f32, cache._shapes["heads"], "out", out, cache.torch_dtype, (total, h, 128), "out_lse", out_lse, f32, (total, h))
+    _check(cache._lib.ctkvr_cache_window_attn(cache.handle, qp, qs, _format_of(cache, k_pages, True), kp, ks, vp, vs, cu, cur, table, total, int(window),
+                                              int(n_sink), *rest, cache.stream()))
 
 
 def ctkvr_cache_tree_attn(cache: Cache, q, k_pages, v_pages, cu_new, cur_lens, block_table, tree_mask, out, out_lse=None, first_key=None, k_scales=None,
                           v_scales=None) -> None:
     """tree_mask: int32 [total][words], 32 drafted tokens a word; k_pages and v_pages are plain, or codes with their scales."""
-    h, total = cache.params.n_q_heads, q.shape[0]
-    cu, cur, table = _batch_on(cache, cu_new, cur_lens, block_table)
+    h, total, words, i32 = cache.params.n_q_heads, q.shape[0], tree_mask.shape[-1], cache._int
     qp, qs = _rows_on(cache, "q", q, total, h)
-    words = tree_mask.shape[-1]
-    _check(cache._lib.ctkvr_cache_tree_attn(
-        cache.handle, qp, qs, *_quant_on(cache, _format_of(cache, k_pages, True), k_pages, k_scales, v_pages, v_scales), cu, cur, table, total,
-        _on(cache, "tree_mask", tree_mask, cache._int, (total, words)), words, _on(cache, "first_key", first_key, cache._int, (total,)),
-        _on(cache, "out", out, cache.torch_dtype, (total, h, 128)), _on(cache, "out_lse", out_lse, cache._float, (total, h)), cache.stream()))
+    cu, cur, table, kp, ks, vp, vs, mask, *rest = _all_on(
+        cache, *_batch_of(cache, cu_new, cur_lens, block_table), *_quant_of(cache, k_pages, k_scales, v_pages, v_scales),
+        "tree_mask", tree_mask, i32, (total, words), "first_key", first_key, i32, (total,), "out", out, cache.torch_dtype, (total, h, 128),
+        "out_lse", out_lse, cache._float, (total, h))
+    _check(cache._lib.ctkvr_cache_tree_attn(cache.handle, qp, qs, _format_of(cache, k_pages, True), kp, ks, vp, vs, cu, cur, table, total, mask, words, *rest,
+                                            cache.stream()))

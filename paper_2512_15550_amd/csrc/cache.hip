@@ -129,7 +129,6 @@ int ctkvr_cache_create(const ctkvr_cache_params *p, void *hip_stream, ctkvr_cach
             }
         if (most == 1 && (((int64_t)total << c->lg) >> 7) * p->n_kv_heads >= 8ll * c->num_cu) break;   // more tokens are never split again
     }
-    if (const char *e = getenv("SP_ROOM")) part_rows = std::max(part_rows, (size_t)atoll(e)), counts = std::max(counts, (size_t)1 << 20);
     c->part_rows = part_rows;
     c->counts = counts;
     if (part_rows) {

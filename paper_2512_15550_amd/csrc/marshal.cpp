@@ -12,15 +12,47 @@ bool is_a(PyObject *o, PyObject *dtype, long device, const at::Tensor **t)
     return (*t)->layout() == at::kStrided && (*t)->scalar_type() == reinterpret_cast<THPDtype *>(dtype)->scalar_type && (*t)->get_device() == device;
 }
 
-// pointer(tensor, dtype, shape, device): the address of a contiguous tensor of this type and shape on the device (-1: the host's), or -1
+// a contiguous tensor of this type and shape on the device (-1: the host's)
+bool is_whole(PyObject *o, PyObject *dtype, PyObject *shape, long device, const at::Tensor **t)
+{
+    if (!PyTuple_Check(shape) || !is_a(o, dtype, device, t) || (*t)->dim() != PyTuple_GET_SIZE(shape) || !(*t)->is_contiguous()) return false;
+    for (int64_t i = 0; i < (*t)->dim(); ++i)
+        if ((*t)->size(i) != PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i))) return false;
+    return true;
+}
+PyObject *address(const at::Tensor *t) { return PyLong_FromUnsignedLongLong(reinterpret_cast<uintptr_t>(t->data_ptr())); }
+
+// pointer(tensor, dtype, shape, device): the tensor's address, or -1
 PyObject *pointer(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     const at::Tensor *t;
-    if (n != 4 || !PyTuple_Check(args[2])) return PyLong_FromLong(-1);
-    if (!is_a(args[0], args[1], PyLong_AsLong(args[3]), &t) || t->dim() != PyTuple_GET_SIZE(args[2]) || !t->is_contiguous()) return PyLong_FromLong(-1);
-    for (int64_t i = 0; i < t->dim(); ++i)
-        if (t->size(i) != PyLong_AsLongLong(PyTuple_GET_ITEM(args[2], i))) return PyLong_FromLong(-1);
-    return PyLong_FromUnsignedLongLong(reinterpret_cast<uintptr_t>(t->data_ptr()));
+    return n == 4 && is_whole(args[0], args[1], args[2], PyLong_AsLong(args[3]), &t) ? address(t) : PyLong_FromLong(-1);
+}
+
+// pointers(device, name, tensor, dtype, shape, ...): the tensors' addresses, None for None, as a tuple; or the number of the first that is none of these
+PyObject *pointers(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n % 4 != 1) {
+        PyErr_SetString(PyExc_TypeError, "pointers(device, name, tensor, dtype, shape, ...)");
+        return nullptr;
+    }
+    const long device = PyLong_AsLong(args[0]);
+    PyObject *all = PyTuple_New(n / 4);
+    for (Py_ssize_t i = 0; all && i < n / 4; ++i) {
+        PyObject *const *a = args + 1 + 4 * i;
+        const at::Tensor *t;
+        PyObject *p;
+        if (a[1] == Py_None) {
+            Py_INCREF(p = Py_None);
+        } else if (is_whole(a[1], a[2], a[3], device, &t)) {
+            p = address(t);
+        } else {
+            Py_DECREF(all);
+            return PyLong_FromSsize_t(i);
+        }
+        PyTuple_SET_ITEM(all, i, p);
+    }
+    return all;
 }
 
 // rows(tensor, dtype, tokens, heads, device): the address and token stride of [tokens][heads][128], a token's heads contiguous, or None
@@ -34,7 +66,9 @@ PyObject *rows(PyObject *, PyObject *const *args, Py_ssize_t n)
     return Py_BuildValue("(KL)", (unsigned long long)reinterpret_cast<uintptr_t>(t->data_ptr()), (long long)(tokens > 1 ? t->stride(0) : heads * 128));
 }
 
-PyMethodDef methods[] = {{"pointer", (PyCFunction)(void *)pointer, METH_FASTCALL, nullptr}, {"rows", (PyCFunction)(void *)rows, METH_FASTCALL, nullptr}, {}};
+PyMethodDef methods[] = {{"pointer", (PyCFunction)(void *)pointer, METH_FASTCALL, nullptr},
+                         {"pointers", (PyCFunction)(void *)pointers, METH_FASTCALL, nullptr},
+                         {"rows", (PyCFunction)(void *)rows, METH_FASTCALL, nullptr}, {}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods};
 
 }  // namespace

@@ -134,14 +134,15 @@ int ctkvr_cache_quant_append(ctkvr_cache *c, const void *q, int64_t q_stride, co
     a.a.q_out = q_out;
     a.k = QuantRows{(uint8_t *)k_codes, k_scales};
     a.v = QuantRows{(uint8_t *)v_codes, v_scales};
-    const dim3 grid((unsigned)((total + 3) / 4));
+    const int share = total <= 2 * c->num_cu ? 4 : 2;   // (waves a token; of 1024, 2048, 4096, 8192 tokens one, two, four 15.5, 13.7, 13.6; 19.4, 18.0, 20.0; 28.4, 29.2, 30.8; 52, 49, 52 us)
+    const dim3 grid((unsigned)(((int64_t)total * share + 3) / 4));
     hipStream_t st = (hipStream_t)hip_stream;
     if (c->p.dtype == CTKVR_BF16) {
-        if (format == CTKVR_KV_INT8) quant_append_kernel<bf16_t, kInt8><<<grid, 256, 0, st>>>(a);
-        else quant_append_kernel<bf16_t, kFp8><<<grid, 256, 0, st>>>(a);
+        if (format == CTKVR_KV_INT8) quant_append_kernel<bf16_t, kInt8><<<grid, 256, 0, st>>>(a, share);
+        else quant_append_kernel<bf16_t, kFp8><<<grid, 256, 0, st>>>(a, share);
     } else {
-        if (format == CTKVR_KV_INT8) quant_append_kernel<float, kInt8><<<grid, 256, 0, st>>>(a);
-        else quant_append_kernel<float, kFp8><<<grid, 256, 0, st>>>(a);
+        if (format == CTKVR_KV_INT8) quant_append_kernel<float, kInt8><<<grid, 256, 0, st>>>(a, share);
+        else quant_append_kernel<float, kFp8><<<grid, 256, 0, st>>>(a, share);
     }
     return launched("ctkvr_cache_quant_append");
 }

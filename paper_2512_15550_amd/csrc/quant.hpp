@@ -80,38 +80,52 @@ template <int STORE> __device__ __forceinline__ void store_codes(const QuantRows
     if (i8 == 0) to.scales[row] = odd ? __uint_as_float(0x7fc00000u) : amax / kTop<STORE>;
 }
 
-template <typename T, int STORE> __global__ __launch_bounds__(256) void quant_append_kernel(QuantAppendArgs qa)
+// `share` waves have a token, 8 lanes a row of it, the chunks i and i + 8 of 8 elements each.  A wave's first rows are requested before it looks its token up.  Many
+// tokens: reading and writing, a wave each.  Few: loads that wait for each other, so that four waves a token have two rounds of them in place of six.
+template <typename T, int STORE> __global__ __launch_bounds__(256) void quant_append_kernel(QuantAppendArgs qa, int share)
 {
     __shared__ float2 turn[4][64];
     const AppendArgs &a = qa.a;
     const CacheView &v = a.v;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, token = blockIdx.x * 4 + wave;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = blockIdx.x * 4 + wave, token = at / share;
+    if (token >= v.total) return;
+    const int i8 = lane & 7, nq = a.q ? v.h : 0, rows = nq + 2 * v.g, step = 8 * share;
+    auto row = [&](int r) {
+        return r < nq ? (const T *)a.q + (int64_t)token * a.q_stride + r * 128
+               : r < nq + v.g ? (const T *)a.k + (int64_t)token * a.k_stride + (r - nq) * 128
+                              : (const T *)a.val + (int64_t)token * a.v_stride + (r - nq - v.g) * 128;
+    };
+    int r = (at % share) * 8 + (lane >> 3);
+    Chunk<T> lo, hi;
+    if (r < rows) {
+        lo = load_chunk_nt(row(r), i8);
+        hi = load_chunk_nt(row(r), i8 + 8);
+    }
     AppendToken t;
     if (!append_token(a, token, lane, turn[wave], &t)) return;
-    const int i8 = lane & 7, nq = a.q ? v.h : 0, nk = a.k ? v.g : 0, rows = nq + 2 * nk;
-    for (int r = lane >> 3; r < rows; r += 8) {
-        const int kv = r - nq;
-        const T *from = r < nq ? (const T *)a.q + (int64_t)token * a.q_stride + r * 128
-                        : kv < nk ? (const T *)a.k + (int64_t)token * a.k_stride + kv * 128
-                                  : (const T *)a.val + (int64_t)token * a.v_stride + (kv - nk) * 128;
-        if (r >= nq && t.page >= v.num_pages) continue;
-        const Chunk<T> lo = load_chunk_nt(from, i8), hi = load_chunk_nt(from, i8 + 8);
+    while (r < rows) {
+        const int kv = r - nq, next = r + step;
         float x[8], y[8], p[8], q[8];
         unpack(lo, x);
         unpack(hi, y);
+        if (next < rows) {
+            lo = load_chunk_nt(row(next), i8);
+            hi = load_chunk_nt(row(next), i8 + 8);
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            p[i] = kv >= nk ? x[i] : fmaf(x[i], t.cs[i], -(y[i] * t.sn[i]));
-            q[i] = kv >= nk ? y[i] : fmaf(y[i], t.cs[i], x[i] * t.sn[i]);
+            p[i] = kv >= v.g ? x[i] : fmaf(x[i], t.cs[i], -(y[i] * t.sn[i]));
+            q[i] = kv >= v.g ? y[i] : fmaf(y[i], t.cs[i], x[i] * t.sn[i]);
         }
         if (r < nq) {
             T *to = (T *)a.q_out + ((size_t)token * v.h + r) * 128;
             store_chunk(to + 8 * i8, p);
             store_chunk(to + 64 + 8 * i8, q);
-        } else {
-            const int64_t row = (((int64_t)t.page * v.g + (kv < nk ? kv : kv - nk)) << v.page_shift) + (t.slot & ((1 << v.page_shift) - 1));
-            store_codes<STORE>(kv < nk ? qa.k : qa.v, row, i8, p, q);
+        } else if (t.page < v.num_pages) {
+            const int64_t to = (((int64_t)t.page * v.g + (kv < v.g ? kv : kv - v.g)) << v.page_shift) + (t.slot & ((1 << v.page_shift) - 1));
+            store_codes<STORE>(kv < v.g ? qa.k : qa.v, to, i8, p, q);
         }
+        r = next;
     }
 }
 

@@ -2,7 +2,6 @@
 #pragma once
 #include "cache_host.hpp"
 
-#include <stdlib.h>
 namespace ctkvr {
 
 // How a call's rows and keys fall into blocks: tiles of 16, 32 or 128 rows.  us, in that order, 32 heads on 8 KV heads in bf16:
@@ -14,7 +13,7 @@ namespace ctkvr {
 // 34, 57; 500 on as many, 2 KV heads, 13, 16, 35).  Over plain fp32 rows it is 32 or 128, as in ctkvr_cache_attn.
 //   Keys are split into runs where blocks would be too few, to so many blocks a CU: single tokens of one sequence, and in windows, whose runs are alike, one; of
 // several sequences, whose lengths differ, half as many as these, 2 to 8 (up to 64K keys, two sequences 25, 31, 36 with 2, 4, 8; four 63, 65, 69; sixteen 267, 248, 240); tiles
-// of 32 as many as the sequences (eight of 32 rows 110, 99, 93), tiles of 128 four; one sequence's larger tiles, and with fp32 queries, two.  A run has 256 keys at least, 1024
+// of 32 as many as the sequences, up to 6 (eight of 32 rows 96, 93, 94, 109 with 4, 6, 8, 16, of 32 to 100 rows 97, 90, 98, 98), tiles of 128 four; one sequence's larger tiles, and with fp32 queries, two.  A run has 256 keys at least, 1024
 // with tiles of 128, 2048 where the tiles fill half the chip by themselves: the join of the runs costs 4 us and more.  It is done by the block that ends last, without a
 // launch of its own, where that reads little and all blocks run at once (16 sequences in windows of 4096 55.4 -> 54.1, but causal in eight blocks a CU 239 -> 241).
 struct SightPlan {
@@ -36,10 +35,8 @@ inline SightPlan sight_plan(const ctkvr_cache *c, int total, int64_t keys, bool 
     else if (rows <= 16ll * used) p.log = 4;
     else if (wide || (is_long && rows > (codes ? 64ll : 48ll) * used)) p.log = 7;
     else p.log = is_long || tiles(5) * g >= cus / 2 ? 5 : 4;
-    if (const char *e = getenv("SP_LOG")) p.log = atoi(e);
     p.tiles = (int)tiles(p.log);
-    int per_cu = !bf16 ? 2 : p.log == 4 ? (window || used == 1 ? 1 : std::min(8, std::max(2, used / 2))) : used == 1 || window ? 2 : p.log == 5 ? std::min(8, used) : 4;
-    if (const char *e = getenv("SP_WANT")) per_cu = atoi(e);
+    const int per_cu = !bf16 ? 2 : p.log == 4 ? (window || used == 1 ? 1 : std::min(8, std::max(2, used / 2))) : used == 1 || window ? 2 : p.log == 5 ? std::min(6, used) : 4;
     const int64_t want = (int64_t)per_cu * cus, least = p.tiles * g >= cus / 2 ? 2048 : p.log == 7 ? 1024 : 256;
     p.nsplit = p.log == 7 && wide ? 1 : (int)std::max<int64_t>(1, std::min({want / (p.tiles * g), (keys + least - 1) / least, (int64_t)kMaxSplit}));
     p.join_inside = p.log < 7 && rows <= 8 * used && rows * p.nsplit <= (bf16 ? 256 : 128) * used && p.tiles * g * p.nsplit <= 2 * cus;

@@ -163,7 +163,7 @@ def test_the_binding_refuses_types_and_shapes():
     import paper_2512_15550_amd as ck
     from paper_2512_15550_amd import _marshal
     from paper_2512_15550_amd import binding as B
-    c = types.SimpleNamespace(torch_dtype=torch.bfloat16, _float=torch.float32, device=-1, _pointer=_marshal.pointer, _rows=_marshal.rows,
+    c = types.SimpleNamespace(torch_dtype=torch.bfloat16, _float=torch.float32, device=-1, _pointer=_marshal.pointer, _pointers=_marshal.pointers, _rows=_marshal.rows,
                               _formats={torch.bfloat16: ck.KV_PLAIN, torch.int8: ck.KV_INT8, torch.float8_e4m3fn: ck.KV_FP8},
                               _shapes={"pages": (3, 2, 16, 128), "scales": (3, 2, 16)})
     codes, scales = torch.zeros((3, 2, 16, 128), dtype=torch.int8), torch.zeros((3, 2, 16))
@@ -173,11 +173,12 @@ def test_the_binding_refuses_types_and_shapes():
     for x, ok in ((plain, False), (plain.float(), True), (codes.view(torch.uint8), True), (codes.view(torch.float8_e5m2), True)):
         with pytest.raises(ValueError):
             B._format_of(c, x, ok)
-    assert B._quant_on(c, 1, codes, scales, codes, scales)[0] == 1
+    assert B._all_on(c, *B._quant_of(c, codes, scales, codes, scales)) == (codes.data_ptr(), scales.data_ptr()) * 2
+    assert B._all_on(c, *B._quant_of(c, None, None, codes, scales)) == (None, None, codes.data_ptr(), scales.data_ptr())
     for bad in ((codes, scales, codes.view(torch.float8_e4m3fn), scales), (codes, scales.double(), codes, scales), (codes, scales[:2], codes, scales),
                 (codes[:, :, :, :64], scales, codes, scales), (codes, scales, codes.transpose(0, 1), scales)):
-        with pytest.raises(ValueError):
-            B._quant_on(c, 1, *bad)
+        with pytest.raises(ValueError, match="expected a contiguous"):
+            B._all_on(c, *B._quant_of(c, *bad))
 
 
 def test_tensors_are_checked_as_they_are_described():
@@ -195,7 +196,11 @@ def test_tensors_are_checked_as_they_are_described():
                                       (t[:, ::2], torch.bfloat16, (6, 2, 16, 128), -1), ([1], torch.bfloat16, (1,), -1), (None, torch.bfloat16, (1,), -1),
                                       (t, "bf16", t.shape, -1), (t, torch.bfloat16, [6, 4, 16, 128], -1), (t.to_sparse(), torch.bfloat16, t.shape, -1)):
         assert M.pointer(bad, dtype, shape, device) == -1
-    assert M.pointer(t) == -1
+        if bad is not None:
+            assert M.pointers(device, "t", t, torch.bfloat16, t.shape, "none", None, 1, 2, "bad", bad, dtype, shape) == (2 if device == -1 else 0)
+    assert M.pointer(t) == -1 and M.pointers(-1) == ()
+    with pytest.raises(TypeError):
+        M.pointers(-1, "t", t)
     empty = torch.zeros((0, 4), dtype=torch.int32)
     assert M.pointer(empty, torch.int32, (0, 4), -1) == empty.data_ptr()
     fused = torch.zeros((5, 12 * 128 + 64), dtype=torch.float32)
