@@ -196,6 +196,35 @@ template <typename T, int STORE> __global__ __launch_bounds__(256) void quant_re
 }
 
 // ---- attention ----------------------------------------------------------------------------------------------
+// locate_tile with the sequence's span, from the lane that has looked it up: no second trip to memory
+template <int LOG> __device__ __forceinline__ bool locate_span(const CacheView &v, int tile, int *b, int *at, SeqSpan *s)
+{
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int b0 = 0; b0 < v.batch; b0 += 64) {
+        SeqSpan mine{};
+        if (b0 + lane < v.batch) mine = seq_span(v, b0 + lane);
+        const int tiles = ((mine.n << v.lg) + (1 << LOG) - 1) >> LOG;
+        int upto = tiles;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+        }
+        const int all = __builtin_amdgcn_readlane(upto, 63);
+        if (tile < base + all) {
+            const int l = __builtin_ctzll(__ballot(base + upto > tile));
+            *b = b0 + l;
+            *at = tile - base - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(tiles, l));
+            *s = SeqSpan{__builtin_amdgcn_readlane(mine.c0, l), __builtin_amdgcn_readlane(mine.n, l), __builtin_amdgcn_readlane(mine.len, l),
+                         __builtin_amdgcn_readlane(mine.old, l)};
+            return true;
+        }
+        base += all;
+    }
+    return false;
+}
+
 struct QuantAttnArgs {
     AttnArgs a;                         // (k_pages and v_pages are codes)
     const float *k_scales, *v_scales;   // [num_pages][g][page]: a row's number is its scale's

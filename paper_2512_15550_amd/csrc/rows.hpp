@@ -48,8 +48,8 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
     // (a KV head's tiles stay on an XCD where the heads are a multiple of 8; the tiles with most keys go first)
     const int kv = blockIdx.x % v.g, rest = blockIdx.x / v.g, split = rest % a.nsplit;
     int b, at;
-    if (!locate_tile<kRowsLog>(v, a.tiles - 1 - rest / a.nsplit, &b, &at)) return;
-    const SeqSpan s = seq_span(v, b);
+    SeqSpan s;
+    if (!locate_span<kRowsLog>(v, a.tiles - 1 - rest / a.nsplit, &b, &at, &s)) return;
     const int rows = s.n << v.lg, r0 = at << kRowsLog, row = r0 + 32 * wave + (lane & 31);
     const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
     const int token = min(row, rows - 1) >> v.lg, head = (kv << v.lg) + (min(row, rows - 1) & ((1 << v.lg) - 1));

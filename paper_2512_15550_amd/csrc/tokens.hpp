@@ -84,8 +84,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = lane >> 4, r16 = lane & 15;
     const int kv = blockIdx.x % v.g, rest = blockIdx.x / v.g, split = rest % a.nsplit, tile = a.tiles - 1 - rest / a.nsplit;
     int b, at;
-    if (!locate_tile<3 + RB>(v, tile, &b, &at)) return;
-    const SeqSpan s = seq_span(v, b);
+    SeqSpan s;
+    if (!locate_span<3 + RB>(v, tile, &b, &at, &s)) return;
     const int rows = s.n << v.lg, r0 = at * kRows, have = min(kRows, rows - r0);
     const int prefix = a.o.prefix ? min(max(a.o.prefix[b], 0), s.len) : 0;
     int token[RB], head[RB];

@@ -631,6 +631,128 @@ def test_trees_on_pages_that_are_none_and_beyond_the_table(store):
     check(st, (out, lse), sees)
 
 
+# ---- calls of every kind --------------------------------------------------------------------------------------
+KINDS = [("quant", "int8"), ("quant", "fp8")] + [(kind, store) for kind in ("window", "tree") for store in ALL_STORES]
+
+
+def check_kind(st, kind, window=60, sinks=5):
+    if kind == "quant":
+        check_quant(st)
+    elif kind == "window":
+        check_window(st, window, sinks)
+    else:
+        check_tree(st, trees_of(st))
+
+
+@pytest.mark.parametrize("kind,store", KINDS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("batch", [65, 130])
+def test_more_sequences_than_a_wave_has_lanes(kind, store, dtype, batch):
+    """Blocks look their sequence up 64 at a time: sequences without new tokens, single tokens, drafts and a chunk on either side of the 64th."""
+    r = np.random.RandomState(batch)
+    new = [int(x) for x in r.choice([0, 1, 1, 1, 2, 7], size=batch)]
+    new[62:66] = [0, 5, 40, 0][:len(new[62:66])]
+    lens = [int(x) + n for x, n in zip(r.randint(0, 120, size=batch), new)]
+    check_kind(Q.QuantSetup(seed_of(kind, store, dtype, batch), store, dtype, 4, 1, 16, lens, new, behind=3, q_scale=2.0), kind)
+
+
+@pytest.mark.parametrize("kind,store", KINDS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_prompt_s_chunk_beside_single_tokens(kind, store, dtype):
+    st = Q.QuantSetup(seed_of(kind, store, dtype), store, dtype, 8, 2, 16, (90, 600, 33, 1, 257, 512), (1, 400, 1, 1, 1, 2), behind=1, q_scale=2.0)
+    check_kind(st, kind)
+
+
+@pytest.mark.parametrize("kind,store", KINDS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [(1, 1, 1), (130, 1, 64)])
+def test_sequences_that_share_their_first_pages(kind, store, dtype, new):
+    st = Q.QuantSetup(seed_of(kind, store, dtype, new), store, dtype, 8, 2, 16, (300, 200, 250), new, q_scale=2.0)
+    st.table[1, :4] = st.table[2, :4] = st.table[0, :4]
+    check_kind(st, kind, window=100)
+
+
+@pytest.mark.parametrize("kind,store", KINDS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [(1, 1, 1), (20, 1, 3), (150, 40, 1)])
+def test_a_query_that_is_not_finite_is_its_own_row_s_trouble(kind, store, dtype, new):
+    """A head's query of NaN, another's with an infinity, and NaN behind the last sequence."""
+    st = Q.QuantSetup(seed_of(kind, store, dtype), store, dtype, 8, 2, 16, (300, 200, 250), new, behind=4, q_scale=2.0)
+    n = int(st.cu[-1])
+    st.q[n:] = NAN
+    whole = st.q.clone()
+    st.q[0, 3] = NAN
+    st.q[n - 1, 6, 77] = math.inf
+    run = {"quant": lambda: run_quant(st, cache_of(st)), "window": lambda: run_window(st, cache_of(st), 60, 5), "tree": lambda: run_tree(st, cache_of(st), mask)}[kind]
+    mask = trees_of(st)
+    out, lse = run()
+    st.q = whole
+    sees = {"quant": lambda b: Q.sees_range(st, b), "window": lambda b: Q.sees_window(st, b, 60, 5), "tree": lambda b: Q.sees_tree(st, b, mask)}[kind]
+    want, want_lse, tol, tol_lse = Q.attention(st, sees)
+    fine = torch.ones((n, 8), dtype=torch.bool)
+    fine[0, 3] = fine[n - 1, 6] = False
+    near(out[:n].cpu()[fine], want[fine], tol[fine], "out")
+    near(lse[:n].cpu()[fine], want_lse[fine], tol_lse[fine], "lse")
+    assert torch.isnan(out[0, 3]).all() and (out[n:] == 7).all() and (lse[n:] == 7).all()
+
+
+@pytest.mark.parametrize("kind,store", KINDS)
+@pytest.mark.parametrize("new", [(1, 1), (33, 2)])
+def test_without_log_sums_and_without_tokens(kind, store, new):
+    """The same outputs where no log-sum-exp is wanted; a call of no tokens writes nothing."""
+    st = Q.QuantSetup(seed_of(kind, store), store, "bf16", 8, 2, 16, (3000, 70), new, q_scale=2.0)
+    cache, p, mask, q = cache_of(st), pages_of(st), dev(trees_of(st)), dev(st.q)
+
+    def call(cu, q, out, lse, mask):
+        batch = (cu,) + batch_of(st)[1:]
+        if kind == "quant":
+            ck.ctkvr_cache_quant_attn(cache, q, p["k"], p["k_scales"], p["v"], p["v_scales"], *batch, out, out_lse=lse)
+        elif kind == "window":
+            ck.ctkvr_cache_window_attn(cache, q, p["k"], p["v"], *batch, 1000, out, n_sink=5, out_lse=lse, k_scales=p["k_scales"], v_scales=p["v_scales"])
+        else:
+            ck.ctkvr_cache_tree_attn(cache, q, p["k"], p["v"], *batch, mask, out, out_lse=lse, k_scales=p["k_scales"], v_scales=p["v_scales"])
+
+    out, lse = outputs(st)
+    call(dev(st.cu), q, out, lse, mask)
+    alone = torch.full_like(out, 7.0)
+    call(dev(st.cu), q, alone, None, mask)
+    assert torch.equal(out, alone)
+    kept = out.clone()
+    call(torch.zeros_like(dev(st.cu)), q[:0], out[:0], lse[:0], mask[:0])
+    call(torch.zeros_like(dev(st.cu)), q, out, lse, mask)
+    assert torch.equal(out, kept)
+
+
+@pytest.mark.parametrize("store", ALL_STORES)
+@pytest.mark.parametrize("new", [(40, 10), (300, 4)])
+def test_windows_beyond_the_table(store, new):
+    """Tokens beyond the table's slots are no keys; they attend all the same, in a window that ends behind the last key."""
+    st = Q.QuantSetup(seed_of(store, new), store, "bf16", 8, 2, 16, (320, 64), new, spare_cols=0)
+    st.cur = torch.tensor([320 + 30, 64 + 6], dtype=torch.int32)
+    got = run_window(st, cache_of(st), 50, 3)
+    st.lens = [320, 70]
+
+    def sees(b):
+        cur = int(st.cur[b])
+        pos, t = torch.arange(cur - new[b], cur)[:, None], torch.arange(st.lens[b])[None, :]
+        return (t <= pos) & ((t > pos - 50) | (t < 3))
+    check(st, got, sees)
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("h,g,tokens", [(32, 8, 5), (8, 2, 700)])
+def test_append_rotates_queries_in_place(store, dtype, h, g, tokens):
+    st = O.Setup(14, dtype, h, g, 16, (tokens + 20,), (tokens,))
+    q, kn, vn = (torch.randn((tokens, n, 128), generator=st.gen).to(st.td).to(DEV) for n in (h, g, g))
+    there = q.clone()
+    want_q, cache = torch.empty_like(q), cache_of(st)
+    want = run_append(st, store, cache, q, kn, vn, want_q)
+    got = run_append(st, store, cache, there, kn, vn, there)
+    assert torch.equal(there, want_q)
+    assert all(torch.equal(got[name].view(torch.uint8), want[name].view(torch.uint8)) for name in ("k", "v"))
+
+
 # ---- streams, graphs, repetition ------------------------------------------------------------------------------
 @pytest.mark.parametrize("kind,store", [("quant", "int8"), ("quant", "fp8")] + [(kind, store) for kind in ("window", "tree") for store in ALL_STORES])
 @pytest.mark.parametrize("new", [1, 33])
