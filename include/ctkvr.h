@@ -348,8 +348,13 @@ int ctkvr_cache_quant_read(ctkvr_cache *c, int32_t format, const void *k_codes, 
                            const int32_t *first_tokens, const int32_t *cur_lens, const int32_t *block_table, const int32_t *out_table, int32_t out_max_pages,
                            int32_t out_num_pages, void *k_pages, void *v_pages, void *hip_stream);
 
-/* ctkvr_cache_attn over rows of 8 bits (format: INT8 or FP8): the same scores, masks and results, on the values that the codes stand for.  Queries are
- * not rounded; with bf16 data a probability times its value's scale enters the product rounded to bf16.  Errors: EINVAL. */
+/*
+ * ctkvr_cache_attn over rows of 8 bits (format: INT8 or FP8): the same scores, masks and results, on the values that the codes stand for.  Queries are not
+ * rounded (fp32 ones: finite ones, below 2^127).  A probability times its value's scale enters the product in fp16, with fp32 data as the sum of two
+ * such numbers, under a power of two of the row's own: it is off by 2^-11 of itself (2^-22) or, if it is small, by 2^-35 of the largest scale that the row
+ * sees, or of 2^-80 if that is more.  Scales are finite, or NaN for a row that is NaN; scales and codes that no token sees may be anything.
+ * Errors: EINVAL.
+ */
 int ctkvr_cache_quant_attn(ctkvr_cache *c, const void *q, int64_t q_stride, int32_t format, const void *k_codes, const float *k_scales, const void *v_codes,
                            const float *v_scales, const int32_t *cu_new, const int32_t *cur_lens, const int32_t *block_table, int32_t total,
                            const float *slopes, const int32_t *prefix_lens, const int32_t *first_key, void *out, float *out_lse, void *hip_stream);
@@ -357,7 +362,7 @@ int ctkvr_cache_quant_attn(ctkvr_cache *c, const void *q, int64_t q_stride, int3
 /*
  * ctkvr_cache_attn in a sliding window beside the first tokens: the token at pos sees key t where
  *   t <= pos  and  (t > pos - window or t < n_sink),
- * over plain rows (format PLAIN, scales NULL) or rows of 8 bits.  What it costs goes by the window, not by the cache.  Pages that lie before every
+ * over plain rows (format PLAIN, scales NULL) or rows of 8 bits (as in ctkvr_cache_quant_attn).  What it costs goes by the window, not by the cache.  Pages that lie before every
  * window of a sequence and behind its first n_sink tokens are not needed any more: their entries of the table may be -1, or pages of other sequences.
  *   window  1 or more (the token itself counts);  n_sink  0 or more.
  * Errors: EINVAL.
@@ -372,7 +377,7 @@ int ctkvr_cache_window_attn(ctkvr_cache *c, const void *q, int64_t q_stride, int
  *   tree_mask  DEVICE uint32 [total][mask_words]: bit j % 32 of word j / 32 of a token's row says that it sees the j-th new token of its sequence (itself
  *              only with its own bit; tokens beyond 32 * mask_words are not seen).
  *   first_key  DEVICE int32 [total] or NULL: it sees no key, new ones included, in an earlier slot.
- * Over plain rows (format PLAIN, scales NULL) or rows of 8 bits.  The cache was appended to with the draft's own positions (a token's depth in its tree behind the
+ * Over plain rows (format PLAIN, scales NULL) or rows of 8 bits (as in ctkvr_cache_quant_attn).  The cache was appended to with the draft's own positions (a token's depth in its tree behind the
  * tokens before it); the tokens that are kept in the end go to their slots in order by another append, of their k and v, with cur_lens counting them alone.
  * A token that sees no key gets zeros and -infinity.  Errors: EINVAL.
  */

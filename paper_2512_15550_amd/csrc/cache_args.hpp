@@ -92,8 +92,8 @@ template <int SIGHT> __host__ __device__ __forceinline__ uint32_t sight_bits(con
     return seen & low_bits(r.hi - key0);
 }
 
-// The tiles of `keys` keys that a block of rows goes through: n of them, tile i of which is i, from `gap_at` on i + gap.  first and last: what the block's
-// first and last token see (kRange: lo is the least first key of its rows, end what key_range says).
+// The tiles of `keys` keys that a block of rows goes through, whose windows begin at lo or later and whose last key is before hi: numbers from .. to - 1, those from
+// gap_at on `gap` tiles further, behind what lies between the first keys and the windows.
 struct KeyTiles {
     int from, to, gap_at, gap;
     __host__ __device__ __forceinline__ int at(int i) const { return i < gap_at ? i : i + gap; }

@@ -3,7 +3,7 @@
 // A row is 128 codes of one byte, int8 or e4m3, and an fp32 scale: its largest magnitude over the largest code.  Both kinds of code are exact in bf16 and fp16, so that
 // the products take them as they are, two bytes each from the conversion on; a key's scale multiplies its score, a value's its probability.  Such a weight enters the
 // product in fp16, which has three bits more than bf16 (with weights in bf16 the outputs of a single token on 32K keys were 2.5e-3 off, of which their own rounding is
-// 1.6e-3), under a power of two that goes with the largest scale so far (ValueScale).  With fp32 queries a query is three bf16 parts and a weight two of
+// 1.6e-3), under a power of two that goes with the largest scale that its row has seen (kWeightPower).  With fp32 queries a query is three bf16 parts and a weight two of
 // fp16: as exact as fp32 products, at a sixth of their cost.
 #pragma once
 #include "cache.hpp"
@@ -316,26 +316,27 @@ __device__ __forceinline__ void scale_regs(f32x16_t &s, const float *scales, int
     }
 }
 
-// Values' scales as they multiply probabilities: times 2^(11 - exponent), where 2^exponent is above every scale so far, and probabilities are under a maximum that
-// may lag by kLag = 4 powers of two, so that a weight is below 2^15, and one under its row's true maximum has all of fp16's bits down to 2^-25 of 2^exponent; what is
-// left of smaller ones is off by 2^-36 of that at most.  The outputs are scaled as the exponent grows, once or twice in a run of keys as a rule, and as a maximum grows by more
-// than 16 times; without the lag a row of few keys has a new one in most tiles (eight sequences' drafts of 8 tokens 94 -> 83 us).
-constexpr int kLag = 4, kWeightPower = 15 - kLag;
-struct ValueScale {
-    int exponent = -100;
-    __device__ __forceinline__ float top() const { return ldexpf(1.0f, exponent); }
-    __device__ __forceinline__ float factor() const { return ldexpf(1.0f, kWeightPower - exponent); }
-    // makes room for a wave's scales; the same in all lanes.  (NaN is above nothing: a row that sees it becomes NaN anyway.)
-    __device__ __forceinline__ void admit(float scale)
-    {
-        if (!__any(scale > top())) return;
-        uint32_t bits = scale > top() ? __float_as_uint(scale) : 0u;
+// Values' scales as they multiply probabilities: times 2^(11 - exponent) = 2^(kWeightPower - exponent), where 2^exponent is above every scale that the row has seen so
+// far, and probabilities are under a maximum that may lag by kLag = 4 powers of two, so that a weight is below 2^15, and one under its row's true maximum has all of
+// fp16's bits down to 2^-25 of 2^exponent; what is left of smaller ones is off by 2^-36 of that at most.  An exponent is a row's own where rows see different keys: a value
+// that one token sees and its neighbour does not may be any size.  The outputs are scaled as the exponent grows, once or twice in a run of keys as a rule, and as a maximum
+// grows by more than 16 times; without the lag a row of few keys has a new one in most tiles (2048 tokens on 32K keys 1250 -> 1225 us, drafts of 2 to 24 tokens
+// 101 -> 98).
+constexpr int kLag = 4, kWeightPower = 15 - kLag, kLeastExponent = -80;
+// the least power of two above a scale, from kLeastExponent on.  (0 and NaN: kLeastExponent; a row that sees NaN becomes NaN anyway.)
+__device__ __forceinline__ int exponent_above(float scale)
+{
+    return scale > 0.0f ? max((int)(__float_as_uint(scale) >> 23) - 126, kLeastExponent) : kLeastExponent;
+}
+// of a wave's scales together, 0 or more each (NaN: as 0)
+__device__ __forceinline__ int exponent_of_all(float scale)
+{
+    uint32_t bits = scale > 0.0f ? __float_as_uint(scale) : 0u;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) bits = max(bits, (uint32_t)__shfl_xor((int)bits, d));
-        exponent = max(__builtin_amdgcn_readfirstlane((int)(bits >> 23)) - 126, -100);
-    }
-};
-__device__ __forceinline__ void scale_outputs(f32x16_t (&o)[4], int by)   // by 2^by
+    for (int d = 1; d < 64; d <<= 1) bits = max(bits, (uint32_t)__shfl_xor((int)bits, d));
+    return max(__builtin_amdgcn_readfirstlane((int)(bits >> 23)) - 126, kLeastExponent);
+}
+__device__ __forceinline__ void scale_outputs(f32x16_t (&o)[4], int by)   // by 2^by, of the lane's row
 {
     const float f = ldexpf(1.0f, by);
 #pragma unroll

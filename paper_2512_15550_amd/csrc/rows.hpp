@@ -41,7 +41,7 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
     static_assert(kCodes || sizeof(T) == 2, "");
     __shared__ __align__(16) char smem[2][Tile::kBytes];
     __shared__ __align__(16) float scales[2][2][kKeys];   // [buffer][K, V]
-    __shared__ int exponents[2];
+    __shared__ int exponents[2];   // of the values' scales in a buffer
     const AttnArgs &a = qa.a;
     const CacheView &v = a.v;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
@@ -129,7 +129,10 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
     // A wave's share of a tile is 16 rows.  Codes: 8 lanes a row, 16 codes a lane, to registers and from there to shared memory.
     uint4 codes[2][2];
     float scale = 0.0f;
-    ValueScale value_scale;   // (wave 1's; the others follow the exponents that it leaves with the tiles)
+    // A tile that all rows see has its values' scales times 2^(11 - tile_exponent), which wave 1 holds and leaves with the tile; of another they are as they are, since
+    // there every row has an exponent of its own.
+    constexpr int kRowsOwn = INT_MIN, kFar = 80;
+    int tile_exponent = kLeastExponent;
     auto request = [&](uint32_t r) {
         if (wave < 2) scale = (wave ? qa.v_scales : qa.k_scales)[r];
 #pragma unroll
@@ -141,12 +144,11 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
     };
     auto put = [&](auto buf, int i, uint64_t none) {
         if (wave == 0) scales[buf][0][lane] = OPT == 0 ? scale * a.o.c2 : scale;
-        if (wave == 1) {   // (the scales of keys that no row sees are whatever stands there)
-            const int key = tile_of(i) * kKeys + lane;
-            const bool in = key < range.hi && (key >= k_lo || (SIGHT == kWindow && key < a.o.sinks)) && !((none >> lane) & 1);
-            value_scale.admit(in ? scale : 0.0f);
-            scales[buf][1][lane] = scale * value_scale.factor();
-            if (lane == 0) exponents[buf] = value_scale.exponent;
+        if (wave == 1) {
+            const bool all = seen_by_all(i, none);
+            if (all && __any(scale > ldexpf(1.0f, tile_exponent))) tile_exponent = max(tile_exponent, exponent_of_all(scale));
+            scales[buf][1][lane] = all ? scale * ldexpf(1.0f, kWeightPower - tile_exponent) : scale;
+            if (lane == 0) exponents[buf] = all ? tile_exponent : kRowsOwn;
         }
         if (STORE == kFp8 && !seen_by_all(i, none)) {
 #pragma unroll
@@ -191,7 +193,7 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
 
     f32x16_t o[4] = {};
     float m = -INFINITY, l = 0.0f;
-    int exponent = -100;
+    int exponent = kLeastExponent;   // of the row's outputs
     const float slope2 = (OPT & kBias) ? a.o.slopes[head] * kLog2e : 0.0f;
     uint64_t bad_now = 0, bad_next = 0;   // of the tile that is worked on, and of the next
     uint32_t page = 0, r = 0;             // codes: entries of the tile behind the next; plain: the next tile's rows, and those entries
@@ -261,9 +263,33 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
 #pragma unroll
                 for (int p = kParts - 1; p >= 0; --p) sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[j][p], sc[kb], 0, 0, 0);
             }
+        bool own = false;
         if constexpr (kCodes) {
-            if (const int e = __builtin_amdgcn_readfirstlane(exponents[buf]); e != exponent) {
-                scale_outputs(o, exponent - e);
+            const int e = __builtin_amdgcn_readfirstlane(exponents[buf]);
+            own = decltype(masked)::value && e == kRowsOwn;
+            if (own) {
+                float top = 0.0f;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int n = 0; n < 16; ++n) {
+                        const int k = 8 * (n >> 2) + 4 * half + (n & 3);
+                        top = fmaxf(top, (seen[kb] >> k) & 1 ? scales[buf][1][32 * kb + k] : 0.0f);
+                    }
+                const int to = max(exponent, exponent_above(half_max(top)));
+                scale_outputs(o, exponent - to);
+                exponent = to;
+            } else if (__any(exponent != e)) {
+                int by = exponent - e;
+                if (__any(by > kFar)) {
+                    // A row has seen far larger values.  Its outputs, below 2^44 at its exponent with 2^20 keys, have no room at the tile's: what is above 2^kFar goes to
+                    // its maximum and its sum (by 2^122 at most, which leaves that a normal number).
+                    const int far = max(by - kFar, 0);
+                    m += (float)far;
+                    l = ldexpf(l, -far);
+                    by -= far;
+                }
+                scale_outputs(o, by);
                 exponent = e;
             }
         }
@@ -279,6 +305,11 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
         for (int kb = 0; kb < 2; ++kb) {
             if constexpr (kCodes) {
                 scale_regs(sc[kb], scales[buf][1] + 32 * kb, half);
+                if (own) {
+                    const float by = ldexpf(1.0f, kWeightPower - exponent);
+#pragma unroll
+                    for (int n = 0; n < 16; ++n) sc[kb][n] *= by;
+                }
                 if constexpr (decltype(masked)::value) mask_bits(sc[kb], seen[kb], half, 0.0f);   // (a hidden row's scale may be anything)
             }
 #pragma unroll

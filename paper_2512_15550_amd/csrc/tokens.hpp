@@ -200,7 +200,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
         l[rb] = 0.0f;
         slope2[rb] = (OPT & kBias) ? a.o.slopes[head[rb]] * kLog2e : 0.0f;
     }
-    ValueScale value_scale;
+    int exponent[RB], least = kLeastExponent;   // of the rows' weights; a bound of all from below
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) exponent[rb] = kLeastExponent;
+    auto raise = [&](int rb, int to) {
+        const float f = ldexpf(1.0f, exponent[rb] - to);
+        exponent[rb] = to;
+#pragma unroll
+        for (int db = 0; db < 8; ++db) o[rb][db] *= f;
+    };
     uint32_t bads[BUFS] = {};   // (of the tiles on their way, the next one first)
     uint32_t r = t0 < t1 ? rows_of(tile_of(t0)) : 0;
     loads_landed<0>();   // (of all that the compiler knows of: it would wait for these, and for all that it does not know of, in every turn)
@@ -233,18 +241,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
         bads[BUFS - 2] = bad;
         char *kt_ = smem[wave] + buf * Tile::kBytes, *vt = kCodes ? kt_ + Tile::kHalf : kt_;
         float *scales = reinterpret_cast<float *>(kt_ + 2 * Tile::kHalf);
-        if constexpr (kCodes) {   // (the scales of keys that no row sees are whatever stands there)
+        const bool masked = key0 + 32 > range.all_hi || (key0 < all_lo && !(SIGHT == kWindow && key0 + 32 <= a.o.sinks)) || bad_now != 0;
+        if constexpr (kCodes) {
             const float scale = scales[lane];
-            const int key = key0 + (lane & 31);
-            const bool in = key < range.hi && (key >= k_lo || (SIGHT == kWindow && key < a.o.sinks)) && !((bad_now >> (lane & 31)) & 1);
-            const int before = value_scale.exponent;
-            value_scale.admit(in && lane >= 32 ? scale : 0.0f);
-            if (value_scale.exponent != before) {
-                const float f = ldexpf(1.0f, before - value_scale.exponent);
+            if (!masked && __any(lane >= 32 && scale > ldexpf(1.0f, least))) {
+                least = max(least, exponent_of_all(lane >= 32 ? scale : 0.0f));
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-                    for (int db = 0; db < 8; ++db) o[rb][db] *= f;
+                for (int rb = 0; rb < RB; ++rb) raise(rb, max(exponent[rb], least));
             }
         }
         // (Operands are requested of shared memory ahead of what comes before their use, and stay there: a load that the compiler puts right before it has the wave wait.)
@@ -293,7 +296,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
         }
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) score_regs<OPT, 8, 16>(sc[rb], a.o, slope2[rb], sight[rb].pos - key0, part);
-        const bool masked = key0 + 32 > range.all_hi || (key0 < all_lo && !(SIGHT == kWindow && key0 + 32 <= a.o.sinks)) || bad_now != 0;
         uint32_t seen[RB];   // by the lane's rows, a bit for each key
         if (masked) {
 #pragma unroll
@@ -302,7 +304,21 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sc[rb][i] = (seen[rb] >> (4 * part + 16 * (i >> 2) + (i & 3))) & 1 ? sc[rb][i] : -INFINITY;
             }
-            if constexpr (!kCodes) {
+            if constexpr (kCodes) {   // (the scales of keys that no row sees are whatever stands there)
+                float top[RB] = {};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int n = 4 * part + 16 * (i >> 2) + (i & 3);
+                    const float x = scales[32 + n];
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) top[rb] = fmaxf(top[rb], (seen[rb] >> n) & 1 ? x : 0.0f);
+                }
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                    const int to = max(exponent[rb], exponent_above(groups_max(top[rb])));
+                    if (__any(to != exponent[rb])) raise(rb, to);
+                }
+            } else {
                 if (__any(OddValues<bf16_t, 32, 64>::any(vt, lane))) {
                     add_odd(o, vt, part, [&](int rb, int n) { return (bool)((seen[rb] >> n) & 1); });
                     __builtin_amdgcn_wave_barrier();
@@ -354,11 +370,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
         if constexpr (kCodes) {
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                const f32x4_t x = *reinterpret_cast<const f32x4_t *>(scales + 32 + 16 * kb + 4 * part) * value_scale.factor();
+                const f32x4_t x = *reinterpret_cast<const f32x4_t *>(scales + 32 + 16 * kb + 4 * part);
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
+                for (int rb = 0; rb < RB; ++rb) {
+                    const float by = ldexpf(1.0f, kWeightPower - exponent[rb]);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) w[rb][4 * kb + c] *= x[c];
+                    for (int c = 0; c < 4; ++c) w[rb][4 * kb + c] *= x[c] * by;
+                }
             }
             f16x8_t p[RB][kWeights];
 #pragma unroll
@@ -409,7 +427,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
         float top = join[0][0][r];
 #pragma unroll
         for (int w = 1; w < NW; ++w) top = fmaxf(top, join[w][0][r]);
-        const float f = (m[rb] == -INFINITY ? 1.0f : exp2_fast(m[rb] - top)) * (kCodes ? ldexpf(1.0f, value_scale.exponent - kWeightPower) : 1.0f);
+        const float f = (m[rb] == -INFINITY ? 1.0f : exp2_fast(m[rb] - top)) * (kCodes ? ldexpf(1.0f, exponent[rb] - kWeightPower) : 1.0f);
 #pragma unroll
         for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4_t *>(smem[0] + (wave * kRows + r) * 512 + (((4 * db + part) ^ r) << 4)) = o[rb][db] * f;
     }

@@ -431,6 +431,56 @@ def test_values_of_very_different_sizes(store, dtype, powers, shape):
     check(st, run_quant(st, cache_of(st)), lambda b: Q.sees_range(st, b), spread=True)
 
 
+LARGE = {
+    "few": ((90, 300, 64), (16, 4, 1)),
+    "drafts": ((90, 300), (40, 33)),
+    "split": ((6000,), (3,)),
+    "rows": ((400, 2000), (400, 150)),
+    "rows_split": ((6000,), (150,)),
+}
+
+
+@pytest.mark.parametrize("kind", ["quant", "docs", "window", "tree"])
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", LARGE)
+@pytest.mark.parametrize("power,others", [(30, 0), (110, 0), (190, -70)])
+def test_large_values_that_other_tokens_see(kind, store, dtype, shape, power, others):
+    """Values up to 2^190 times as large as the others (times 2^`others`), which some tokens see and their neighbours do not: these are as exact as without them."""
+    lens, new = LARGE[shape]
+    st = Q.QuantSetup(seed_of(kind, store, dtype, shape), store, dtype, 16, 2, 16, lens, new, behind=1, q_scale=2.0)
+    n, first, mask = int(st.cu[-1]), None, trees_of(st)
+    sees = {"quant": lambda b: Q.sees_range(st, b), "docs": lambda b: Q.sees_range(st, b, None, first), "window": lambda b: Q.sees_window(st, b, 70, 3),
+            "tree": lambda b: Q.sees_tree(st, b, mask)}[kind]
+    if kind == "docs":
+        first = torch.randint(0, 2, (st.total,), generator=st.gen).int() * 45
+    large = []
+    st.v_scales *= 2.0 ** others
+    for b, (s, m) in enumerate(zip(lens, new)):
+        large.append({"docs": 31, "window": max(s - m - 40, 0)}.get(kind, s - m // 2 - 1))     # before the others' first key, in some windows, half of the new tokens on
+        for part in (power // 2, power - power // 2):     # (2^190 is no fp32 number)
+            st.v_scales[int(st.table[b, large[b] // 16]), :, large[b] % 16] *= 2.0 ** part
+    assert torch.isfinite(st.v_scales).all()
+    if kind == "quant":
+        got = run_quant(st, cache_of(st))
+    elif kind == "docs":
+        got = run_quant(st, cache_of(st), first=first)
+    elif kind == "window":
+        got = run_window(st, cache_of(st), 70, 3)
+    else:
+        got = run_tree(st, cache_of(st), mask)
+    out, lse = (x[:n].cpu() for x in got)
+    hit = torch.cat([sees(b)[:, large[b]] for b in range(st.batch)])
+    want, want_lse, tol, tol_lse = Q.attention(st, sees, spread=True)
+    near(out[hit], want[hit], tol[hit], "tokens that see it")
+    near(lse, want_lse, tol_lse, "lse")
+    for b in range(st.batch):
+        st.v_scales[int(st.table[b, large[b] // 16]), :, large[b] % 16] = 1.0
+    want, _, tol, _ = Q.attention(st, sees)
+    assert (~hit).any() or shape in ("few", "split")
+    near(out[~hit], want[~hit], tol[~hit], "tokens that do not")
+
+
 @pytest.mark.parametrize("store", STORES)
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_views_of_a_fused_projection_and_a_scale_of_ones_own(store, dtype):
