@@ -52,7 +52,8 @@ template <typename T, int SIGHT> int plain_launch(const ctkvr_cache *c, QuantAtt
         if constexpr (sizeof(T) == 2) {
             if (log == 4) tokens_kernel<kPlain, T, kOpt, SIGHT, 1><<<dim3(grid), 256, 0, st>>>(qa);
             if (log == 5) tokens_kernel<kPlain, T, kOpt, SIGHT, 2><<<dim3(grid), 256, 0, st>>>(qa);
-            if (log == 7) rows_kernel<kPlain, T, kOpt, SIGHT><<<dim3(grid), 256, 0, st>>>(qa);
+            if (log == 7) rows_kernel<kPlain, T, kOpt, SIGHT, 4><<<dim3(grid), 256, 0, st>>>(qa);
+            if (log == 8) rows_kernel<kPlain, T, kOpt, SIGHT, 8><<<dim3(grid), 512, 0, st>>>(qa);
         } else {
             if (log == 5) attn_few_kernel<T, kOpt, 2, SIGHT><<<dim3(grid), 128, 0, st>>>(a);
             if (log == 7) attn_kernel<T, kOpt, 4, SIGHT><<<dim3(grid), 256, 0, st>>>(a);

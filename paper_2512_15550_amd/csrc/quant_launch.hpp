@@ -15,8 +15,11 @@ template <typename T, int STORE, int SIGHT> void quant_attn_form(QuantAttnArgs &
     with_opts(SIGHT == kTree ? opt & kCap : opt, [&](auto o) {
         constexpr int kOpt = decltype(o)::value & (SIGHT == kTree ? kCap : ~0);   // (drafted tokens have no distance)
         if (log == 4) tokens_kernel<STORE, T, kOpt, SIGHT, 1><<<dim3(grid), 256, 0, st>>>(q);
-        else if (log == 7) rows_kernel<STORE, T, kOpt, SIGHT><<<dim3(grid), 256, 0, st>>>(q);
-        else if constexpr (sizeof(T) == 2) tokens_kernel<STORE, T, kOpt, SIGHT, 2><<<dim3(grid), 256, 0, st>>>(q);
+        else if (log == 7) rows_kernel<STORE, T, kOpt, SIGHT, 4><<<dim3(grid), 256, 0, st>>>(q);
+        else if constexpr (sizeof(T) == 2) {
+            if (log == 5) tokens_kernel<STORE, T, kOpt, SIGHT, 2><<<dim3(grid), 256, 0, st>>>(q);
+            else rows_kernel<STORE, T, kOpt, SIGHT, 8><<<dim3(grid), 512, 0, st>>>(q);
+        }
         return 0;
     });
 }

@@ -1,4 +1,4 @@
-// Attention of many rows: tiles of 128 rows, over plain bf16 rows and rows of 8 bits.
+// Attention of many rows: tiles of 128 and 256 rows, over plain bf16 rows and rows of 8 bits.
 #pragma once
 #include "quant.hpp"
 
@@ -31,14 +31,16 @@ template <bool CODES> struct RowsTile {
     }
 };
 
-// One block a tile of 128 rows of a unit and, where the keys are split, one of nsplit runs of them; a wave has 32 rows.  While a tile of 64 keys is worked on the
-// next one is put into shared memory (codes: turned into bf16 and fp16 by the block, each once for all four waves) and the one behind it requested.
-template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void rows_kernel(QuantAttnArgs qa)
+// One block a tile of 32 NW rows of a unit and, where the keys are split, one of nsplit runs of them; a wave has 32 rows.  While a tile of 64 keys is worked on the
+// next one is put into shared memory (codes: turned into bf16 and fp16 by the block, each once for all its waves) and the one behind it requested.  Two waves a SIMD: two blocks of four
+// a CU, or one of eight, which does half of that work for a row (2048 tokens on 32K codes 1243 -> 1146 us, 930 TFLOP/s).  Products and the vector instructions of softmax, scales and
+// conversion bound it, which two waves of a SIMD hardly overlap.
+template <int STORE, typename T, int OPT, int SIGHT, int NW> __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void rows_kernel(QuantAttnArgs qa)
 {
     constexpr bool kCodes = STORE != kPlain;
     using Tile = RowsTile<kCodes>;
-    constexpr int NW = 4, kRowsLog = 7, kKeys = 64, kParts = sizeof(T) == 2 ? 1 : 3, kWeights = sizeof(T) == 2 ? 1 : 2;
-    static_assert(kCodes || sizeof(T) == 2, "");
+    constexpr int kRowsLog = NW == 8 ? 8 : 7, kKeys = 64, kShare = kKeys / NW, kParts = sizeof(T) == 2 ? 1 : 3, kWeights = sizeof(T) == 2 ? 1 : 2;
+    static_assert((kCodes || sizeof(T) == 2) && (NW == 4 || (NW == 8 && sizeof(T) == 2)), "");
     __shared__ __align__(16) char smem[2][Tile::kBytes];
     __shared__ __align__(16) float scales[2][2][kKeys];   // [buffer][K, V]
     __shared__ int exponents[2];   // of the values' scales in a buffer
@@ -126,8 +128,8 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
         return (t + 1) * kKeys <= range.all_hi && (t * kKeys >= all_lo || (SIGHT == kWindow && (t + 1) * kKeys <= a.o.sinks)) && none == 0;
     };
 
-    // A wave's share of a tile is 16 rows.  Codes: 8 lanes a row, 16 codes a lane, to registers and from there to shared memory.
-    uint4 codes[2][2];
+    // A wave's share of a tile is kShare rows.  Codes: 8 lanes a row, 16 codes a lane, to registers and from there to shared memory.
+    uint4 codes[2][kShare / 8];
     float scale = 0.0f;
     // A tile that all rows see has its values' scales times 2^(11 - tile_exponent), which wave 1 holds and leaves with the tile; of another they are as they are, since
     // there every row has an exponent of its own.
@@ -136,8 +138,8 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
     auto request = [&](uint32_t r) {
         if (wave < 2) scale = (wave ? qa.v_scales : qa.k_scales)[r];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int64_t from = (int64_t)(uint32_t)__shfl((int)r, wave * 16 + 8 * j + (lane >> 3)) * 128 + 16 * (lane & 7);
+        for (int j = 0; j < kShare / 8; ++j) {
+            const int64_t from = (int64_t)(uint32_t)__shfl((int)r, wave * kShare + 8 * j + (lane >> 3)) * 128 + 16 * (lane & 7);
             codes[0][j] = *reinterpret_cast<const uint4 *>((const char *)a.k_pages + from);
             codes[1][j] = *reinterpret_cast<const uint4 *>((const char *)a.v_pages + from);
         }
@@ -152,14 +154,14 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
         }
         if (STORE == kFp8 && !seen_by_all(i, none)) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            for (int j = 0; j < kShare / 8; ++j) {
                 uint4 &w = codes[1][j];
                 w = make_uint4(no_nan<STORE>(w.x), no_nan<STORE>(w.y), no_nan<STORE>(w.z), no_nan<STORE>(w.w));
             }
         }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int key = wave * 16 + 8 * j + (lane >> 3);
+        for (int j = 0; j < kShare / 8; ++j) {
+            const int key = wave * kShare + 8 * j + (lane >> 3);
             char *k_to = smem[buf] + key * Tile::kKeyRow + 16 * (lane & 7), *v_to = smem[buf] + Tile::kKeyBytes + key * Tile::kValueRow + 16 * (lane & 7);
             *reinterpret_cast<bf16x8_t *>(k_to) = codes8<STORE>(codes[0][j].x, codes[0][j].y);
             *reinterpret_cast<bf16x8_t *>(k_to + 128) = codes8<STORE>(codes[0][j].z, codes[0][j].w);
@@ -167,25 +169,25 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
             *reinterpret_cast<f16x8_t *>(v_to + 128) = codes8h<STORE>(codes[1][j].z, codes[1][j].w);
         }
     };
-    // Plain rows: four a load, straight to shared memory.  Where a wave's 16 are in one page the address of the first is the wave's, not a lane's.
+    // Plain rows: four a load, straight to shared memory.  Where a wave's are in one page the address of the first is the wave's, not a lane's.
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_at(smem));
-    const bool one_page = (1 << v.page_shift) >= 16;
+    const bool one_page = (1 << v.page_shift) >= kShare;
     const int in4 = lane >> 4, c16 = lane & 15;
     auto load = [&](auto buf, uint32_t r, bool whole) {
-        const uint32_t to = lds0 + buf * Tile::kBytes + wave * 16 * 256;
+        const uint32_t to = lds0 + buf * Tile::kBytes + wave * kShare * 256;
         if (one_page && whole) {
-            const int64_t from = (int64_t)(uint32_t)__builtin_amdgcn_readlane(r, wave * 16) * 256;
+            const int64_t from = (int64_t)(uint32_t)__builtin_amdgcn_readlane(r, wave * kShare) * 256;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                load_to_lds(to + j * 1024, (const char *)a.k_pages + from, (4 * j + in4) * 256 + 16 * (c16 ^ (4 * j + in4)));
+            for (int j = 0; j < kShare / 4; ++j) {
+                load_to_lds(to + j * 1024, (const char *)a.k_pages + from, (4 * j + in4) * 256 + 16 * (c16 ^ ((wave * kShare + 4 * j + in4) & 15)));
                 load_to_lds(to + Tile::kKeyBytes + j * 1024, (const char *)a.v_pages + from, (4 * j + in4) * 256 + 16 * (c16 ^ (in4 << 2)));
             }
             return;
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t from = (int64_t)(uint32_t)__shfl((int)r, wave * 16 + 4 * j + in4) * 256;
-            row_to_lds(to + j * 1024, (const char *)a.k_pages + from + 16 * (c16 ^ (4 * j + in4)));
+        for (int j = 0; j < kShare / 4; ++j) {
+            const int64_t from = (int64_t)(uint32_t)__shfl((int)r, wave * kShare + 4 * j + in4) * 256;
+            row_to_lds(to + j * 1024, (const char *)a.k_pages + from + 16 * (c16 ^ ((wave * kShare + 4 * j + in4) & 15)));
             row_to_lds(to + Tile::kKeyBytes + j * 1024, (const char *)a.v_pages + from + 16 * (c16 ^ (in4 << 2)));
         }
     };
@@ -228,8 +230,8 @@ template <int STORE, typename T, int OPT, int SIGHT> __global__ __launch_bounds_
                 const u32x4_t *w = reinterpret_cast<const u32x4_t *>(tile + Tile::kKeyBytes) + threadIdx.x;
                 uint32_t odd = 0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const u32x4_t x = w[j * 256];
+                for (int j = 0; j < 16 / NW; ++j) {
+                    const u32x4_t x = w[j * 64 * NW];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) odd |= ((x[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
                 }
