@@ -681,6 +681,70 @@ def test_trees_on_pages_that_are_none_and_beyond_the_table(store):
     check(st, (out, lse), sees)
 
 
+# ---- many rows in wide tables ---------------------------------------------------------------------------------
+def wide(seed, store, page, lens=(300, 200, 700, 64), new=(100, 70, 129, 64), h=8, g=2, **more):
+    """Tables with room for more than 4096 tokens: rows are taken 256 at a time."""
+    return Q.QuantSetup(seed, store, "bf16", h, g, page, lens, new, spare_cols=4096 // page, behind=2, **more)
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("page", [1, 8, 64])
+@pytest.mark.parametrize("cap", [0.0, 5.0])
+@pytest.mark.parametrize("kinds", [(), ("bias",), ("prefix",), ("docs",), ("bias", "prefix", "docs")], ids="+".join)
+def test_wide_tables(store, page, cap, kinds):
+    st = wide(seed_of(store, page, kinds), store, page, q_scale=2.0)
+    check_quant(st, cap=cap, **masks_of(st, kinds))
+
+
+@pytest.mark.parametrize("store", ALL_STORES)
+@pytest.mark.parametrize("page", [1, 4, 8, 64])
+@pytest.mark.parametrize("cap", [0.0, 5.0])
+def test_wide_tables_of_drafts(store, page, cap):
+    """Any bits, a first key besides; pages that are none."""
+    st = wide(seed_of(store, page), store, page, q_scale=2.0)
+    mask = torch.randint(-2 ** 31, 2 ** 31, (st.total, 5), generator=st.gen).int()
+    mask[3:9] = 0
+    first = torch.randint(-10, 200, (st.total,), generator=st.gen).int()
+    check_tree(st, mask, cap)
+    check_tree(st, mask, cap, first)
+    for b, c in ((0, 1), (0, 100 // page), (1, 0), (2, 650 // page), (3, 63 // page)):
+        st.table[b, c] = st.num_pages if b % 2 else -1
+    check_tree(st, mask, cap, first)
+
+
+@pytest.mark.parametrize("store", ALL_STORES)
+@pytest.mark.parametrize("page", [1, 8, 16])
+def test_wide_tables_what_is_not_seen_does_not_matter(store, page):
+    """A drafted token's row of NaN, for those that do not see it; bytes that nobody wrote behind the last key and on pages that are free."""
+    st = wide(seed_of(store, page), store, page, q_scale=2.0)
+    mask, bad = trees_of(st), 20
+    spoil(st, sorted(set(range(st.num_pages)) - set(st.table[st.table >= 0].tolist())), slice(None))
+    sees = torch.zeros(int(st.cu[-1]), dtype=torch.bool)
+    for b, (s, n) in enumerate(zip(st.lens, st.new)):
+        if s % page:
+            spoil(st, int(st.table[b, (s - 1) // page]), slice(s % page, page))
+        t = s - n + bad
+        spoil(st, int(st.table[b, t // page]), t % page)
+        rows = slice(int(st.cu[b]), int(st.cu[b + 1]))
+        sees[rows] = (mask[rows, 0] >> bad & 1).bool()
+    out, lse = run_tree(st, cache_of(st), mask)
+    want, want_lse, tol, tol_lse = Q.attention(st, lambda b: Q.sees_tree(st, b, torch.where((mask[:, 0] >> bad & 1).bool()[:, None], 0, mask)))
+    n = int(st.cu[-1])
+    assert torch.isnan(out[:n][sees.to(DEV)]).all()
+    near(out[:n].cpu()[~sees], want[~sees], tol[~sees], "out")
+    near(lse[:n].cpu()[~sees], want_lse[~sees], tol_lse[~sees], "lse")
+    assert (out[n:] == 7).all() and (lse[n:] == 7).all()
+
+
+@pytest.mark.parametrize("store", ALL_STORES)
+@pytest.mark.parametrize("page", [1, 8, 16])
+@pytest.mark.parametrize("sinks", [0, 100])
+def test_wide_tables_of_windows(store, page, sinks):
+    st = wide(seed_of(store, page, sinks), store, page, (4500, 4300), (150, 129), q_scale=2.0)
+    check_window(st, 4100, sinks)
+    check_window(st, 4097, sinks, cap=5.0, slopes=masks_of(st, ("bias",))["slopes"])
+
+
 # ---- calls of every kind --------------------------------------------------------------------------------------
 KINDS = [("quant", "int8"), ("quant", "fp8")] + [(kind, store) for kind in ("window", "tree") for store in ALL_STORES]
 
