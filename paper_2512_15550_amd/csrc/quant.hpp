@@ -81,7 +81,8 @@ template <int STORE> __device__ __forceinline__ void store_codes(const QuantRows
 }
 
 // `share` waves have a token, 8 lanes a row of it, the chunks i and i + 8 of 8 elements each.  A wave's first rows are requested before it looks its token up.  Many
-// tokens: reading and writing, a wave each.  Few: loads that wait for each other, so that four waves a token have two rounds of them in place of six.
+// tokens: reading and writing, a wave each.  Few: loads that wait for each other, so that four waves a token have two rounds of them in place of six
+// (16 tokens 7.3 -> 5.6 us).  Memory bounds it: 8192 tokens in 38 us, 4.8 TB/s, as a copy.
 template <typename T, int STORE> __global__ __launch_bounds__(256) void quant_append_kernel(QuantAppendArgs qa, int share)
 {
     __shared__ float2 turn[4][64];
@@ -151,6 +152,7 @@ template <int STORE> __device__ __forceinline__ f32x4_t decode(uint32_t w, float
     }
 }
 // A block takes runs of 64 tokens of a unit: 16 lanes a row, 8 codes a lane, so that a row's values are written in a line, and four rows a lane on their way at once.
+// Memory bounds it: 32K tokens in 44 us, 4.6 TB/s, where a copy reaches 4.8.
 template <typename T, int STORE> __global__ __launch_bounds__(256) void quant_read_kernel(QuantReadArgs a)
 {
     constexpr int kRun = 64, kEach = 4;

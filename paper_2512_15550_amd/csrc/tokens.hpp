@@ -68,7 +68,9 @@ template <int RB, typename F> __device__ __forceinline__ void add_odd(f32x4_t (&
 
 // One block a tile of 16 RB rows and a run of their keys, which its waves share out, 32 at a time; no wave waits for another before the end.  Keys and values go straight
 // to shared memory, BUFS - 1 tiles ahead of the one that is worked on.  Scores come as S^T = K Q^T on 16 x 16 x 32 products: a lane has one row (lane % 16) of each 16 and, of
-// each 16 keys, those from 4 (lane / 16) on, and its probabilities of 32 keys are, where they stand, an operand of O^T = V^T P^T.  What it reads bounds it.
+// each 16 keys, those from 4 (lane / 16) on, and its probabilities of 32 keys are, where they stand, an operand of O^T = V^T P^T.  What it reads bounds tiles of 16 rows: 5.4 TB/s for
+// 16 sequences of 8K to 64K keys (238 us), one token on 32K 21 us, 9 of them launch, dependent loads and the runs' join; tiles of 32 the conversion of codes and the softmax
+// (vector instructions half of the cycles, matrix cores 11 %; drafts of 8 to 25 tokens of 8 sequences 90 us).
 template <int STORE, typename T, int OPT, int SIGHT, int RB>
 __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens_kernel(QuantAttnArgs qa)
 {
