@@ -81,7 +81,7 @@ template <int STORE> __device__ __forceinline__ void store_codes(const QuantRows
 }
 
 // `share` waves have a token, 8 lanes a row of it, the chunks i and i + 8 of 8 elements each.  A wave's first rows are requested before it looks its token up.  Many
-// tokens: reading and writing, a wave each.  Few: loads that wait for each other, so that four waves a token have two rounds of them in place of six
+// tokens: reading and writing, two waves each.  Few: loads that wait for each other, so that four waves a token have two rounds of them in place of six
 // (16 tokens 7.3 -> 5.6 us).  Memory bounds it: 8192 tokens in 38 us, 4.8 TB/s, as a copy.
 template <typename T, int STORE> __global__ __launch_bounds__(256) void quant_append_kernel(QuantAppendArgs qa, int share)
 {
