@@ -868,6 +868,35 @@ def test_append_rotates_queries_in_place(store, dtype, h, g, tokens):
 
 
 # ---- streams, graphs, repetition ------------------------------------------------------------------------------
+@pytest.mark.parametrize("kind,store", KINDS)
+def test_two_handles_on_two_streams_at_once(kind, store):
+    """Split calls, each with a workspace of its own, that run beside each other."""
+    sts = [Q.QuantSetup(seed, store, "bf16", 8, 2, 16, (6000, 5000), new, q_scale=2.0) for seed, new in ((81, (1, 2)), (82, (60, 40)))]
+    calls = []
+    for st in sts:
+        cache, p, batch, q, mask = cache_of(st), pages_of(st), batch_of(st), dev(st.q), dev(trees_of(st))
+
+        def call(out, lse, cache=cache, p=p, batch=batch, q=q, mask=mask):
+            if kind == "quant":
+                ck.ctkvr_cache_quant_attn(cache, q, p["k"], p["k_scales"], p["v"], p["v_scales"], *batch, out, out_lse=lse)
+            elif kind == "window":
+                ck.ctkvr_cache_window_attn(cache, q, p["k"], p["v"], *batch, 4500, out, n_sink=5, out_lse=lse, k_scales=p["k_scales"], v_scales=p["v_scales"])
+            else:
+                ck.ctkvr_cache_tree_attn(cache, q, p["k"], p["v"], *batch, mask, out, out_lse=lse, k_scales=p["k_scales"], v_scales=p["v_scales"])
+        calls.append(call)
+    alone, beside = [outputs(st) for st in sts], [outputs(st) for st in sts]
+    for call, outs in zip(calls, alone):
+        call(*outs)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sts]
+    for _ in range(5):
+        for stream, call, outs in zip(streams, calls, beside):
+            with torch.cuda.stream(stream):
+                call(*outs)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for x, y in zip(alone, beside) for a, b in zip(x, y))
+
+
 @pytest.mark.parametrize("kind,store", [("quant", "int8"), ("quant", "fp8")] + [(kind, store) for kind in ("window", "tree") for store in ALL_STORES])
 @pytest.mark.parametrize("new", [1, 33])
 def test_the_same_call_gives_the_same_bits_on_any_stream_and_in_graphs(kind, store, new):
