@@ -3,7 +3,28 @@
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <memory>
+
 namespace {
+
+// What torch throws becomes an error of the interpreter, which calls these functions directly: a tensor without storage (inside torch.vmap or torch.func.grad, say) has no
+// address, and asking for it throws.
+template <typename F> PyObject *guarded(F f) noexcept
+{
+    try {
+        return f();
+    } catch (const c10::Error &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what_without_backtrace());
+    } catch (const std::exception &e) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+        PyErr_SetString(PyExc_RuntimeError, "unknown exception");
+    }
+    return nullptr;
+}
+struct Decref {
+    void operator()(PyObject *o) const { Py_DECREF(o); }
+};
 
 bool is_a(PyObject *o, PyObject *dtype, long device, const at::Tensor **t)
 {
@@ -25,8 +46,10 @@ PyObject *address(const at::Tensor *t) { return PyLong_FromUnsignedLongLong(rein
 // pointer(tensor, dtype, shape, device): the tensor's address, or -1
 PyObject *pointer(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
-    const at::Tensor *t;
-    return n == 4 && is_whole(args[0], args[1], args[2], PyLong_AsLong(args[3]), &t) ? address(t) : PyLong_FromLong(-1);
+    return guarded([&] {
+        const at::Tensor *t;
+        return n == 4 && is_whole(args[0], args[1], args[2], PyLong_AsLong(args[3]), &t) ? address(t) : PyLong_FromLong(-1);
+    });
 }
 
 // pointers(device, name, tensor, dtype, shape, ...): the tensors' addresses, None for None, as a tuple; or the number of the first that is none of these
@@ -36,34 +59,34 @@ PyObject *pointers(PyObject *, PyObject *const *args, Py_ssize_t n)
         PyErr_SetString(PyExc_TypeError, "pointers(device, name, tensor, dtype, shape, ...)");
         return nullptr;
     }
-    const long device = PyLong_AsLong(args[0]);
-    PyObject *all = PyTuple_New(n / 4);
-    for (Py_ssize_t i = 0; all && i < n / 4; ++i) {
-        PyObject *const *a = args + 1 + 4 * i;
-        const at::Tensor *t;
-        PyObject *p;
-        if (a[1] == Py_None) {
-            Py_INCREF(p = Py_None);
-        } else if (is_whole(a[1], a[2], a[3], device, &t)) {
-            p = address(t);
-        } else {
-            Py_DECREF(all);
-            return PyLong_FromSsize_t(i);
+    return guarded([&]() -> PyObject * {
+        const long device = PyLong_AsLong(args[0]);
+        std::unique_ptr<PyObject, Decref> all(PyTuple_New(n / 4));
+        if (!all) return nullptr;
+        for (Py_ssize_t i = 0; i < n / 4; ++i) {
+            PyObject *const *a = args + 1 + 4 * i;
+            const at::Tensor *t;
+            PyObject *p;
+            if (a[1] == Py_None) Py_INCREF(p = Py_None);
+            else if (is_whole(a[1], a[2], a[3], device, &t)) p = address(t);
+            else return PyLong_FromSsize_t(i);
+            PyTuple_SET_ITEM(all.get(), i, p);
         }
-        PyTuple_SET_ITEM(all, i, p);
-    }
-    return all;
+        return all.release();
+    });
 }
 
 // rows(tensor, dtype, tokens, heads, device): the address and token stride of [tokens][heads][128], a token's heads contiguous, or None
 PyObject *rows(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
-    const at::Tensor *t;
-    if (n != 5 || !is_a(args[0], args[1], PyLong_AsLong(args[4]), &t) || t->dim() != 3) Py_RETURN_NONE;
-    const int64_t tokens = PyLong_AsLongLong(args[2]), heads = PyLong_AsLongLong(args[3]);
-    if (t->size(0) != tokens || t->size(1) != heads || t->size(2) != 128) Py_RETURN_NONE;
-    if (tokens && (t->stride(2) != 1 || (heads != 1 && t->stride(1) != 128))) Py_RETURN_NONE;
-    return Py_BuildValue("(KL)", (unsigned long long)reinterpret_cast<uintptr_t>(t->data_ptr()), (long long)(tokens > 1 ? t->stride(0) : heads * 128));
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *t;
+        if (n != 5 || !is_a(args[0], args[1], PyLong_AsLong(args[4]), &t) || t->dim() != 3) Py_RETURN_NONE;
+        const int64_t tokens = PyLong_AsLongLong(args[2]), heads = PyLong_AsLongLong(args[3]);
+        if (t->size(0) != tokens || t->size(1) != heads || t->size(2) != 128) Py_RETURN_NONE;
+        if (tokens && (t->stride(2) != 1 || (heads != 1 && t->stride(1) != 128))) Py_RETURN_NONE;
+        return Py_BuildValue("(KL)", (unsigned long long)reinterpret_cast<uintptr_t>(t->data_ptr()), (long long)(tokens > 1 ? t->stride(0) : heads * 128));
+    });
 }
 
 PyMethodDef methods[] = {{"pointer", (PyCFunction)(void *)pointer, METH_FASTCALL, nullptr},
