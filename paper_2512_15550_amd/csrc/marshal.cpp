@@ -26,7 +26,16 @@ struct Decref {
     void operator()(PyObject *o) const { Py_DECREF(o); }
 };
 
-bool is_a(PyObject *o, PyObject *dtype, long device, const at::Tensor **t)
+// a whole number, or the least one, which is no size and no device; what is none leaves no error behind
+int64_t whole_number(PyObject *o)
+{
+    const int64_t n = PyLong_AsLongLong(o);
+    if (n != -1 || !PyErr_Occurred()) return n;
+    PyErr_Clear();
+    return INT64_MIN;
+}
+
+bool is_a(PyObject *o, PyObject *dtype, int64_t device, const at::Tensor **t)
 {
     if (!THPVariable_Check(o) || !THPDtype_Check(dtype)) return false;
     *t = &THPVariable_Unpack(o);
@@ -34,11 +43,11 @@ bool is_a(PyObject *o, PyObject *dtype, long device, const at::Tensor **t)
 }
 
 // a contiguous tensor of this type and shape on the device (-1: the host's)
-bool is_whole(PyObject *o, PyObject *dtype, PyObject *shape, long device, const at::Tensor **t)
+bool is_whole(PyObject *o, PyObject *dtype, PyObject *shape, int64_t device, const at::Tensor **t)
 {
     if (!PyTuple_Check(shape) || !is_a(o, dtype, device, t) || (*t)->dim() != PyTuple_GET_SIZE(shape) || !(*t)->is_contiguous()) return false;
     for (int64_t i = 0; i < (*t)->dim(); ++i)
-        if ((*t)->size(i) != PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i))) return false;
+        if ((*t)->size(i) != whole_number(PyTuple_GET_ITEM(shape, i))) return false;
     return true;
 }
 PyObject *address(const at::Tensor *t) { return PyLong_FromUnsignedLongLong(reinterpret_cast<uintptr_t>(t->data_ptr())); }
@@ -48,7 +57,7 @@ PyObject *pointer(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     return guarded([&] {
         const at::Tensor *t;
-        return n == 4 && is_whole(args[0], args[1], args[2], PyLong_AsLong(args[3]), &t) ? address(t) : PyLong_FromLong(-1);
+        return n == 4 && is_whole(args[0], args[1], args[2], whole_number(args[3]), &t) ? address(t) : PyLong_FromLong(-1);
     });
 }
 
@@ -60,7 +69,7 @@ PyObject *pointers(PyObject *, PyObject *const *args, Py_ssize_t n)
         return nullptr;
     }
     return guarded([&]() -> PyObject * {
-        const long device = PyLong_AsLong(args[0]);
+        const int64_t device = whole_number(args[0]);
         std::unique_ptr<PyObject, Decref> all(PyTuple_New(n / 4));
         if (!all) return nullptr;
         for (Py_ssize_t i = 0; i < n / 4; ++i) {
@@ -81,8 +90,8 @@ PyObject *rows(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     return guarded([&]() -> PyObject * {
         const at::Tensor *t;
-        if (n != 5 || !is_a(args[0], args[1], PyLong_AsLong(args[4]), &t) || t->dim() != 3) Py_RETURN_NONE;
-        const int64_t tokens = PyLong_AsLongLong(args[2]), heads = PyLong_AsLongLong(args[3]);
+        if (n != 5 || !is_a(args[0], args[1], whole_number(args[4]), &t) || t->dim() != 3) Py_RETURN_NONE;
+        const int64_t tokens = whole_number(args[2]), heads = whole_number(args[3]);
         if (t->size(0) != tokens || t->size(1) != heads || t->size(2) != 128) Py_RETURN_NONE;
         if (tokens && (t->stride(2) != 1 || (heads != 1 && t->stride(1) != 128))) Py_RETURN_NONE;
         return Py_BuildValue("(KL)", (unsigned long long)reinterpret_cast<uintptr_t>(t->data_ptr()), (long long)(tokens > 1 ? t->stride(0) : heads * 128));

@@ -42,3 +42,19 @@ print("ok")
 def test_a_tensor_without_storage_is_refused(call, transform):
     r = subprocess.run([sys.executable, "-c", WITHOUT_STORAGE % (call, transform, call)], cwd=ROOT, capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and r.stdout == "ok\n", f"status {r.returncode}\n" + r.stdout + r.stderr
+
+
+def test_a_shape_of_no_whole_numbers_is_no_tensor_s_shape():
+    """An answer, and no error left behind for the next call to trip over."""
+    import torch
+
+    from paper_2512_15550_amd import _marshal as M
+    t, rows = torch.zeros((2, 3)), torch.zeros((2, 3, 128))
+    for bad in ("3", 2 ** 70, None, 3.5):
+        assert M.pointer(t, torch.float32, (2, bad), -1) == -1
+        assert M.pointers(-1, "t", t, torch.float32, (2, 3), "t", t, torch.float32, (2, bad)) == 1
+        assert M.rows(rows, torch.float32, 2, bad, -1) is None and M.rows(rows, torch.float32, bad, 3, -1) is None
+        for device in ("cuda", 2 ** 70, None):
+            assert M.pointer(t, torch.float32, (2, 3), device) == -1 and M.pointers(device, "t", t, torch.float32, (2, 3)) == 0
+            assert M.rows(rows, torch.float32, 2, 3, device) is None
+    assert M.pointer(t, torch.float32, (2, 3), -1) == t.data_ptr()
