@@ -325,15 +325,16 @@ __device__ __forceinline__ void scale_regs(f32x16_t &s, const float *scales, int
 // grows by more than 16 times; without the lag a row of few keys has a new one in most tiles (2048 tokens on 32K keys 1250 -> 1225 us, drafts of 2 to 24 tokens
 // 101 -> 98).
 constexpr int kLag = 4, kWeightPower = 15 - kLag, kLeastExponent = -80;
-// the least power of two above a scale, from kLeastExponent on.  (0 and NaN: kLeastExponent; a row that sees NaN becomes NaN anyway.)
+// (Scales may have either sign: what counts is their magnitude.)
+// the least power of two above a magnitude, from kLeastExponent on.  (0 and NaN: kLeastExponent; a row that sees NaN becomes NaN anyway.)
 __device__ __forceinline__ int exponent_above(float scale)
 {
     return scale > 0.0f ? max((int)(__float_as_uint(scale) >> 23) - 126, kLeastExponent) : kLeastExponent;
 }
-// of a wave's scales together, 0 or more each (NaN: as 0)
+// above a wave's scales together (NaN: as 0)
 __device__ __forceinline__ int exponent_of_all(float scale)
 {
-    uint32_t bits = scale > 0.0f ? __float_as_uint(scale) : 0u;
+    uint32_t bits = fabsf(scale) > 0.0f ? __float_as_uint(fabsf(scale)) : 0u;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) bits = max(bits, (uint32_t)__shfl_xor((int)bits, d));
     return max(__builtin_amdgcn_readfirstlane((int)(bits >> 23)) - 126, kLeastExponent);

@@ -148,7 +148,7 @@ template <int STORE, typename T, int OPT, int SIGHT, int NW> __global__ __launch
         if (wave == 0) scales[buf][0][lane] = OPT == 0 ? scale * a.o.c2 : scale;
         if (wave == 1) {
             const bool all = seen_by_all(i, none);
-            if (all && __any(scale > ldexpf(1.0f, tile_exponent))) tile_exponent = max(tile_exponent, exponent_of_all(scale));
+            if (all && __any(fabsf(scale) > ldexpf(1.0f, tile_exponent))) tile_exponent = max(tile_exponent, exponent_of_all(scale));
             scales[buf][1][lane] = all ? scale * ldexpf(1.0f, kWeightPower - tile_exponent) : scale;
             if (lane == 0) exponents[buf] = all ? tile_exponent : kRowsOwn;
         }
@@ -276,7 +276,7 @@ template <int STORE, typename T, int OPT, int SIGHT, int NW> __global__ __launch
 #pragma unroll
                     for (int n = 0; n < 16; ++n) {
                         const int k = 8 * (n >> 2) + 4 * half + (n & 3);
-                        top = fmaxf(top, (seen[kb] >> k) & 1 ? scales[buf][1][32 * kb + k] : 0.0f);
+                        top = fmaxf(top, (seen[kb] >> k) & 1 ? fabsf(scales[buf][1][32 * kb + k]) : 0.0f);
                     }
                 const int to = max(exponent, exponent_above(half_max(top)));
                 scale_outputs(o, exponent - to);

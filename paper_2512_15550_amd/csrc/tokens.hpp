@@ -245,7 +245,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
         float *scales = reinterpret_cast<float *>(kt_ + 2 * Tile::kHalf);
         const bool masked = key0 + 32 > range.all_hi || (key0 < all_lo && !(SIGHT == kWindow && key0 + 32 <= a.o.sinks)) || bad_now != 0;
         if constexpr (kCodes) {
-            const float scale = scales[lane];
+            const float scale = fabsf(scales[lane]);
             if (!masked && __any(lane >= 32 && scale > ldexpf(1.0f, least))) {
                 least = max(least, exponent_of_all(lane >= 32 ? scale : 0.0f));
 #pragma unroll
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || RB == 1 ? 2 : 1) void tokens
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int n = 4 * part + 16 * (i >> 2) + (i & 3);
-                    const float x = scales[32 + n];
+                    const float x = fabsf(scales[32 + n]);
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb) top[rb] = fmaxf(top[rb], (seen[rb] >> n) & 1 ? x : 0.0f);
                 }
