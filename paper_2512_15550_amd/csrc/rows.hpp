@@ -44,6 +44,7 @@ template <int STORE, typename T, int OPT, int SIGHT, int NW> __global__ __launch
     __shared__ __align__(16) char smem[2][Tile::kBytes];
     __shared__ __align__(16) float scales[2][2][kKeys];   // [buffer][K, V]
     __shared__ int exponents[2];   // of the values' scales in a buffer
+    __shared__ __align__(8) uint8_t far_rows[2][NW];   // [step % 2][wave]
     const AttnArgs &a = qa.a;
     const CacheView &v = a.v;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
@@ -133,6 +134,8 @@ template <int STORE, typename T, int OPT, int SIGHT, int NW> __global__ __launch
     float scale = 0.0f;
     // A tile that all rows see has its values' scales times 2^(11 - tile_exponent), which wave 1 holds and leaves with the tile; of another they are as they are, since
     // there every row has an exponent of its own.
+    //   A row that has seen values more than 2^kFar times as large as such a tile's keeps its exponent there, since its outputs, below 2^44 at that with 2^20 keys, have no
+    // room at the tile's; the tile's weights are next to nothing to it.  While a block has such rows, or may have, it takes its tiles one at a time.
     constexpr int kRowsOwn = INT_MIN, kFar = 80;
     int tile_exponent = kLeastExponent;
     auto request = [&](uint32_t r) {
@@ -265,34 +268,35 @@ template <int STORE, typename T, int OPT, int SIGHT, int NW> __global__ __launch
 #pragma unroll
                 for (int p = kParts - 1; p >= 0; --p) sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[j][p], sc[kb], 0, 0, 0);
             }
-        bool own = false;
+        int e = 0;
         if constexpr (kCodes) {
-            const int e = __builtin_amdgcn_readfirstlane(exponents[buf]);
-            own = decltype(masked)::value && e == kRowsOwn;
-            if (own) {
-                float top = 0.0f;
+            e = __builtin_amdgcn_readfirstlane(exponents[buf]);
+            if constexpr (decltype(masked)::value) {
+                int to = e;
+                if (e == kRowsOwn) {
+                    float top = 0.0f;
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
+                    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                    for (int n = 0; n < 16; ++n) {
-                        const int k = 8 * (n >> 2) + 4 * half + (n & 3);
-                        top = fmaxf(top, (seen[kb] >> k) & 1 ? fabsf(scales[buf][1][32 * kb + k]) : 0.0f);
-                    }
-                const int to = max(exponent, exponent_above(half_max(top)));
-                scale_outputs(o, exponent - to);
-                exponent = to;
-            } else if (__any(exponent != e)) {
-                int by = exponent - e;
-                if (__any(by > kFar)) {
-                    // A row has seen far larger values.  Its outputs, below 2^44 at its exponent with 2^20 keys, have no room at the tile's: what is above 2^kFar goes to
-                    // its maximum and its sum (by 2^122 at most, which leaves that a normal number).
-                    const int far = max(by - kFar, 0);
-                    m += (float)far;
-                    l = ldexpf(l, -far);
-                    by -= far;
+                        for (int n = 0; n < 16; ++n) {
+                            const int k = 8 * (n >> 2) + 4 * half + (n & 3);
+                            top = fmaxf(top, (seen[kb] >> k) & 1 ? fabsf(scales[buf][1][32 * kb + k]) : 0.0f);
+                        }
+                    to = max(exponent, exponent_above(half_max(top)));
+                } else if (exponent - e > kFar) {
+                    to = exponent;
                 }
-                scale_outputs(o, by);
-                exponent = e;
+                if (__any(to != exponent)) {
+                    scale_outputs(o, exponent - to);
+                    exponent = to;
+                }
+                const bool is_far = __any(exponent - max(e, kLeastExponent) > kFar);
+                if (lane == 0) far_rows[i & 1][wave] = is_far;
+            } else {
+                if (__any(exponent != e)) {
+                    scale_outputs(o, exponent - e);
+                    exponent = e;
+                }
             }
         }
 #pragma unroll
@@ -307,8 +311,8 @@ template <int STORE, typename T, int OPT, int SIGHT, int NW> __global__ __launch
         for (int kb = 0; kb < 2; ++kb) {
             if constexpr (kCodes) {
                 scale_regs(sc[kb], scales[buf][1] + 32 * kb, half);
-                if (own) {
-                    const float by = ldexpf(1.0f, kWeightPower - exponent);
+                if (decltype(masked)::value && __any(exponent != e)) {   // (some rows' weights take a power of their own)
+                    const float by = ldexpf(1.0f, (e == kRowsOwn ? kWeightPower : e) - exponent);
 #pragma unroll
                     for (int n = 0; n < 16; ++n) sc[kb][n] *= by;
                 }
@@ -362,7 +366,12 @@ template <int STORE, typename T, int OPT, int SIGHT, int NW> __global__ __launch
     int i = t0;
     while (i < t1) {
         // (two at a time: where a tile is in shared memory is then part of the instructions)
-        if (((i - t0) & 1) == 0)
+        bool pairs = ((i - t0) & 1) == 0;
+        if (kCodes && pairs && i > t0 && i + 1 < t1 && seen_by_all(i, bad_now) && seen_by_all(i + 1, bad_next)) {
+            using Waves = std::conditional_t<NW == 8, uint64_t, uint32_t>;
+            pairs = !__any(*reinterpret_cast<const Waves *>(far_rows[(i - 1) & 1]) != 0);
+        }
+        if (pairs)
             while (i + 1 < t1 && seen_by_all(i, bad_now) && seen_by_all(i + 1, bad_next)) {
                 step(Zero(), std::false_type(), i);
                 step(std::integral_constant<int, 1>(), std::false_type(), i + 1);

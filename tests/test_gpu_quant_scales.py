@@ -54,3 +54,30 @@ def test_scales_below_zero(kind, store, dtype, shape, signs):
             x[below] *= 2.0 ** 40
     got, sees = run_kind(st, kind)
     check(st, got, sees, spread=signs == "large")
+
+
+# ---- sizes ----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("power,others", [(120, 0.0), (120, 2.0 ** -100), (127, 0.0), (60, 2.0 ** -60)])
+def test_the_sum_of_a_row_that_sees_a_far_larger_value(store, dtype, shape, power, others):
+    """Some tokens' documents begin before a value of 2^power beside ones of 0 or next to it.  What makes most of every row's sum are many keys whose probabilities are
+    2^-7 of the largest: none of them may be lost."""
+    st = setup(seed_of(store, dtype, shape, power), store, dtype, shape)
+    one, half = (127, 64) if store == "int8" else (1.0, 0.5)
+    st.k_scales[:] = 1.0 / 127.0 if store == "int8" else 1.0
+    st.q = torch.zeros_like(st.q)
+    st.q[:, :, 0] = 110.0
+    k = torch.zeros(st.k.shape)
+    k[..., 0] = half
+    st.v_scales[:] = others
+    first = torch.randint(0, 2, (st.total,), generator=st.gen).int() * 8
+    first[0], first[int(st.cu[-1]) - 1] = 0, 8
+    for b in range(st.batch):
+        k[int(st.table[b, 0]), :, 9:12, 0] = one                # the largest scores, seen by all
+        st.v_scales[int(st.table[b, 0]), :, 5] = 2.0 ** power   # ... and seen from 0 on
+    st.k = k.to(Q.CODES[store])
+    st.v = (torch.randint(-1, 2, st.v.shape, generator=st.gen).float()).to(Q.CODES[store])
+    got = run_quant(st, cache_of(st), first=first)
+    check(st, got, lambda b: Q.sees_range(st, b, None, first), spread=True)
