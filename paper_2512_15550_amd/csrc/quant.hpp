@@ -317,6 +317,16 @@ __device__ __forceinline__ void scale_regs(f32x16_t &s, const float *scales, int
         for (int c = 0; c < 4; ++c) s[4 * i + c] *= x[c];
     }
 }
+// ... times their scales times `by`, which brings scales that probabilities above 1 would take beyond fp32 into range first
+__device__ __forceinline__ void scale_regs_by(f32x16_t &s, const float *scales, float by, int half)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(scales + 8 * i + 4 * half);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[4 * i + c] *= x[c] * by;
+    }
+}
 
 // Values' scales as they multiply probabilities: times 2^(11 - exponent) = 2^(kWeightPower - exponent), where 2^exponent is above every scale that the row has seen so
 // far, and probabilities are under a maximum that may lag by kLag = 4 powers of two, so that a weight is below 2^15, and one under its row's true maximum has all of

@@ -310,11 +310,10 @@ template <int STORE, typename T, int OPT, int SIGHT, int NW> __global__ __launch
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             if constexpr (kCodes) {
-                scale_regs(sc[kb], scales[buf][1] + 32 * kb, half);
                 if (decltype(masked)::value && __any(exponent != e)) {   // (some rows' weights take a power of their own)
-                    const float by = ldexpf(1.0f, (e == kRowsOwn ? kWeightPower : e) - exponent);
-#pragma unroll
-                    for (int n = 0; n < 16; ++n) sc[kb][n] *= by;
+                    scale_regs_by(sc[kb], scales[buf][1] + 32 * kb, ldexpf(1.0f, (e == kRowsOwn ? kWeightPower : e) - exponent), half);
+                } else {
+                    scale_regs(sc[kb], scales[buf][1] + 32 * kb, half);
                 }
                 if constexpr (decltype(masked)::value) mask_bits(sc[kb], seen[kb], half, 0.0f);   // (a hidden row's scale may be anything)
             }

@@ -81,3 +81,23 @@ def test_the_sum_of_a_row_that_sees_a_far_larger_value(store, dtype, shape, powe
     st.v = (torch.randint(-1, 2, st.v.shape, generator=st.gen).float()).to(Q.CODES[store])
     got = run_quant(st, cache_of(st), first=first)
     check(st, got, lambda b: Q.sees_range(st, b, None, first), spread=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_scales_next_to_the_largest_number(dtype, shape):
+    """Scales of 2^126 under codes of 2^-9 and none, in tiles of which a page is missing; scores that grow by less than 16 times, under a maximum that lags."""
+    st = setup(seed_of(dtype, shape), "fp8", dtype, shape)
+    st.k_scales[:] = 1.0
+    st.q = torch.zeros_like(st.q)
+    st.q[:, :, 0] = 31.0
+    k = torch.zeros(st.k.shape)
+    for b, s in enumerate(st.lens):
+        for c in range(-(-s // 16)):
+            k[int(st.table[b, c]), :, :, 0] = min(c // 4, 7) / 8     # (31 / sqrt(128) / 8 is half a power of two)
+    st.k = k.to(Q.CODES["fp8"])
+    st.v = (torch.randint(-1, 2, st.v.shape, generator=st.gen).float() * 2.0 ** -9).to(Q.CODES["fp8"])
+    st.v_scales[:] = 2.0 ** 126
+    for b, s in enumerate(st.lens):
+        st.table[b, 1:-(-s // 16):2] = -1
+    check(st, run_quant(st, cache_of(st)), lambda b: Q.sees_range(st, b), spread=True)
