@@ -46,7 +46,7 @@ struct ScoreOpts {
     const int32_t *first;     // [total] or null
     float c2;                 // scale * log2 e
     float cap_in, cap_out, cap_105, cap_945;   // scale / cap, cap * log2 e, the latter times 105 and 945 (cap != 0)
-    int window, sinks;        // kWindow: the last keys that a row sees, its own among them (2^21 at most), and the first ones
+    int window, sinks;        // kWindow: the last keys that a row sees, its own among them (2^30 at most), and the first ones
     const uint32_t *drafts;   // kTree: [total][words], bit j of a token: it sees the j-th new token of its sequence
     int words;
 };

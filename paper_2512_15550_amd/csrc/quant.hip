@@ -218,7 +218,7 @@ int ctkvr_cache_window_attn(ctkvr_cache *c, const void *q, int64_t q_stride, int
     const AttnCall x{q, q_stride, format, k_pages, k_scales, v_pages, v_scales, cu_new, cur_lens, block_table, total, out, out_lse};
     TRY(check_attn(c, x));
     ScoreOpts o = score_opts(c, slopes, nullptr, nullptr);
-    o.window = std::min(window, 1 << 21);   // (no two tokens are that far apart)
+    o.window = std::min(window, 1 << 30);   // (slots are below that, also those beyond the table)
     o.sinks = std::min(n_sink, 1 << 20);
     return attend<kWindow>(c, x, o, (hipStream_t)hip_stream);
 }

@@ -101,3 +101,22 @@ def test_scales_next_to_the_largest_number(dtype, shape):
     for b, s in enumerate(st.lens):
         st.table[b, 1:-(-s // 16):2] = -1
     check(st, run_quant(st, cache_of(st)), lambda b: Q.sees_range(st, b), spread=True)
+
+
+# ---- windows --------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("store", ["plain"] + STORES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [(1, 1), (40, 10), (300, 4)])
+@pytest.mark.parametrize("cur,window", [(1 << 22, (1 << 22) - 100), (1 << 22, 1 << 22), (1 << 29, 2 ** 31 - 1), ((1 << 30) - 1, 1 << 30)])
+def test_wide_windows_far_beyond_the_table(store, dtype, new, cur, window):
+    """Tokens millions of slots beyond the table's, in windows that reach back into it."""
+    st = Q.QuantSetup(seed_of(store, dtype, new, cur), store, dtype, 8, 2, 16, (320, 64), new, spare_cols=0)
+    st.cur = torch.tensor([cur, cur - 30], dtype=torch.int32)
+    got = run_window(st, cache_of(st), window, 3)
+
+    def sees(b):
+        last = int(st.cur[b])
+        pos, t = torch.arange(last - new[b], last)[:, None], torch.arange(st.cols * 16)[None, :]
+        return (t <= pos) & ((t > pos - window) | (t < 3))
+    st.lens = [320, 320]
+    check(st, got, sees)
