@@ -110,35 +110,24 @@ int ctkvr_cache_create(const ctkvr_cache_params *p, void *hip_stream, ctkvr_cach
         c->axes = std::max(c->axes, c->rope.axis[i] + 1);
     }
     // for the largest product of rows and runs that a call may take, and its tiles
-    size_t part_rows = 0, counts = 0;
+    Room room = sight_room(c);
     for (int total = 1; total <= p->max_new; ++total) {
-        int most = 1;
-        auto room = [&](int nsplit, int tiles) {
-            most = std::max(most, nsplit);
-            if (nsplit == 1) return;
-            part_rows = std::max(part_rows, (size_t)nsplit * total * p->n_q_heads);
-            counts = std::max(counts, (size_t)tiles * p->n_kv_heads);
-        };
         const AttnPlan plan = attn_plan(c, total);
-        room(plan.nsplit, plan.tiles);
-        const int64_t slots = (int64_t)p->max_pages * p->page_size;
-        for (const int64_t keys : {slots, std::min<int64_t>(slots, 4095)})   // (fewer are split less, in the form that they get)
-            for (const int form : {0, 1, 2, 3}) {
-                const SightPlan sight = sight_plan(c, total, keys, form & 1, form & 2);
-                room(sight.nsplit, sight.tiles);
-            }
-        if (most == 1 && (((int64_t)total << c->lg) >> 7) * p->n_kv_heads >= 8ll * c->num_cu) break;   // more tokens are never split again
+        if (plan.nsplit == 1 && (((int64_t)total << c->lg) >> 7) * p->n_kv_heads >= 8ll * c->num_cu) break;   // more tokens are never split again
+        if (plan.nsplit == 1) continue;
+        room.rows = std::max(room.rows, (size_t)plan.nsplit * total * p->n_q_heads);
+        room.counts = std::max(room.counts, (size_t)plan.tiles * p->n_kv_heads);
     }
-    c->part_rows = part_rows;
-    c->counts = counts;
-    if (part_rows) {
-        int rc = pool_get(c->dev, (part_rows * 129 + counts) * 4, 4, &c->mem);
+    c->part_rows = room.rows;
+    c->counts = room.counts;
+    if (room.rows) {
+        int rc = pool_get(c->dev, (room.rows * 129 + room.counts) * 4, 4, &c->mem);
         if (rc == CTKVR_OK) {
             c->part_o = (float *)c->mem.base;
-            c->part_lse = c->part_o + part_rows * 128;
-            c->done = (uint32_t *)(c->part_lse + part_rows);
+            c->part_lse = c->part_o + room.rows * 128;
+            c->done = (uint32_t *)(c->part_lse + room.rows);
             hipStream_t st = (hipStream_t)hip_stream;
-            cache_clear_kernel<<<dim3((unsigned)((counts + 255) / 256)), 256, 0, st>>>(c->done, counts);
+            cache_clear_kernel<<<dim3((unsigned)((room.counts + 255) / 256)), 256, 0, st>>>(c->done, room.counts);
             rc = launched("ctkvr_cache_create");
             const hipError_t e = hipStreamSynchronize(st);
             if (rc == CTKVR_OK && e != hipSuccess) rc = fail(CTKVR_EHIP, "ctkvr_cache_create: %s", hipGetErrorString(e));

@@ -83,10 +83,9 @@ template <int SIGHT> int attend(const ctkvr_cache *c, const AttnCall &x, const S
     qa.k_scales = x.k_scales;
     qa.v_scales = x.v_scales;
     const int64_t slots = (int64_t)c->p.max_pages * c->p.page_size;
-    const SightPlan plan = sight_plan(c, x.total, SIGHT == kWindow ? std::min<int64_t>(slots, (int64_t)o.window + o.sinks + x.total) : slots,
-                                      x.format != CTKVR_KV_PLAIN, SIGHT == kWindow);
-    if (plan.nsplit > 1 && ((size_t)plan.nsplit * x.total * c->p.n_q_heads > c->part_rows || (size_t)plan.tiles * c->p.n_kv_heads > c->counts))
-        return fail(CTKVR_EHIP, "%d runs of %d tokens: beyond the workspace", plan.nsplit, x.total);
+    SightPlan plan = sight_plan(c, x.total, SIGHT == kWindow ? std::min<int64_t>(slots, (int64_t)o.window + o.sinks + x.total) : slots,
+                                x.format != CTKVR_KV_PLAIN, SIGHT == kWindow);
+    fit_plan(c, x.total, Room{c->part_rows, c->counts}, plan);
     a.tiles = plan.tiles;
     a.nsplit = plan.nsplit;
     a.done = plan.join_inside ? c->done : nullptr;

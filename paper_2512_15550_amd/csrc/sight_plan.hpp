@@ -59,4 +59,32 @@ inline SightPlan sight_plan(const ctkvr_cache *c, int total, int64_t keys, bool 
     return p;
 }
 
+// What a workspace has room for: rows of partial outputs, and counts of the tiles whose runs are joined by the block that ends last
+struct Room {
+    size_t rows, counts;
+};
+// ... that every call of up to max_new tokens finds room in.  Plans are looked up at a number of tokens and a sixteenth more, and what lies between is taken to have as many
+// runs as either, so that a handle's creation does not go through all numbers (one KV head, two sequences, 32768 tokens: 7.8 ms -> 0.3); it makes the workspace larger by a
+// sixteenth at most.  A call with more runs all the same gets as many as there is room for (fit_plan).
+inline Room sight_room(const ctkvr_cache *c)
+{
+    const int64_t slots = (int64_t)c->p.max_pages * c->p.page_size, spans[2] = {slots, std::min<int64_t>(slots, 4095)};   // (fewer keys are split less, in the form that they get)
+    Room room{0, 0};
+    for (int total = 1, upto; total <= c->p.max_new; total = upto + 1) {
+        upto = std::min(c->p.max_new, total + total / 16);
+        int most = 1;
+        for (int at = total; at <= upto; at += std::max(1, upto - total))
+            for (int span = 0; span < (slots > 4095 ? 2 : 1); ++span)
+                for (const int form : {0, 1, 2, 3}) most = std::max(most, sight_plan(c, at, spans[span], form & 1, form & 2).nsplit);
+        if (most > 1) room = Room{std::max(room.rows, (size_t)most * upto * c->p.n_q_heads), (size_t)c->num_cu};   // (runs are joined inside in up to two blocks a CU: a tile has two at least)
+        else if ((((int64_t)total << c->lg) >> 7) * c->p.n_kv_heads >= 8ll * c->num_cu) break;   // more tokens are never split again
+    }
+    return room;
+}
+inline void fit_plan(const ctkvr_cache *c, int total, const Room &room, SightPlan &p)
+{
+    p.nsplit = (int)std::max<size_t>(1, std::min<size_t>(p.nsplit, room.rows / ((size_t)total * c->p.n_q_heads)));
+    if ((size_t)p.tiles * c->p.n_kv_heads > room.counts) p.join_inside = false;
+}
+
 }  // namespace ctkvr
