@@ -47,19 +47,24 @@ template <typename T, int SIGHT> int plain_launch(const ctkvr_cache *c, QuantAtt
 {
     AttnArgs &a = qa.a;
     const unsigned grid = (unsigned)((int64_t)a.tiles * c->p.n_kv_heads * a.nsplit);
-    with_opts(opt, [&](auto o) {
+    TRY(with_opts(opt, [&](auto o) {
         constexpr int kOpt = decltype(o)::value & (SIGHT == kTree ? kCap : ~0);   // (drafted tokens have no distance)
         if constexpr (sizeof(T) == 2) {
+            constexpr bool kWide = SIGHT == kTree;   // (tiles of 256 plain rows are slower in windows)
             if (log == 4) tokens_kernel<kPlain, T, kOpt, SIGHT, 1><<<dim3(grid), 256, 0, st>>>(qa);
-            if (log == 5) tokens_kernel<kPlain, T, kOpt, SIGHT, 2><<<dim3(grid), 256, 0, st>>>(qa);
-            if (log == 7) rows_kernel<kPlain, T, kOpt, SIGHT, 4><<<dim3(grid), 256, 0, st>>>(qa);
-            if (log == 8) rows_kernel<kPlain, T, kOpt, SIGHT, 8><<<dim3(grid), 512, 0, st>>>(qa);
+            else if (log == 5) tokens_kernel<kPlain, T, kOpt, SIGHT, 2><<<dim3(grid), 256, 0, st>>>(qa);
+            else if (log == 7) rows_kernel<kPlain, T, kOpt, SIGHT, 4><<<dim3(grid), 256, 0, st>>>(qa);
+            else if (!kWide || log != 8) return no_kernel(log);
+            if constexpr (kWide) {
+                if (log == 8) rows_kernel<kPlain, T, kOpt, SIGHT, 8><<<dim3(grid), 512, 0, st>>>(qa);
+            }
         } else {
             if (log == 5) attn_few_kernel<T, kOpt, 2, SIGHT><<<dim3(grid), 128, 0, st>>>(a);
-            if (log == 7) attn_kernel<T, kOpt, 4, SIGHT><<<dim3(grid), 256, 0, st>>>(a);
+            else if (log == 7) attn_kernel<T, kOpt, 4, SIGHT><<<dim3(grid), 256, 0, st>>>(a);
+            else return no_kernel(log);
         }
-        return 0;
-    });
+        return (int)CTKVR_OK;
+    }));
     join_launch<T>(c, a, st);
     return launched(SIGHT == kWindow ? "ctkvr_cache_window_attn" : "ctkvr_cache_tree_attn");
 }
@@ -95,7 +100,7 @@ template <int SIGHT> int attend(const ctkvr_cache *c, const AttnCall &x, const S
         return bf16 ? quant_attn_launch<bf16_t>(c, qa, plan, x.format, SIGHT, opt, st) : quant_attn_launch<float>(c, qa, plan, x.format, SIGHT, opt, st);
     if constexpr (SIGHT != kRange)
         return bf16 ? plain_launch<bf16_t, SIGHT>(c, qa, plan.log, opt, st) : plain_launch<float, SIGHT>(c, qa, plan.log, opt, st);
-    return CTKVR_OK;
+    return fail(CTKVR_EINVAL, "plain rows are ctkvr_cache_attn's");   // (refused before)
 }
 
 }  // namespace

@@ -59,6 +59,9 @@ inline SightPlan sight_plan(const ctkvr_cache *c, int total, int64_t keys, bool 
     return p;
 }
 
+// A plan's tiles that a launch has no kernel for
+inline int no_kernel(int log) { return fail(CTKVR_EHIP, "no kernel for tiles of 2^%d rows", log); }
+
 // What a workspace has room for: rows of partial outputs, and counts of the tiles whose runs are joined by the block that ends last
 struct Room {
     size_t rows, counts;
