@@ -120,3 +120,61 @@ def test_wide_windows_far_beyond_the_table(store, dtype, new, cur, window):
         return (t <= pos) & ((t > pos - window) | (t < 3))
     st.lens = [320, 320]
     check(st, got, sees)
+
+
+# ---- weights --------------------------------------------------------------------------------------------------
+def pairs(store, dtype, shape, negative=False):
+    """Keys of which two, of nearly the same score, have nearly all of a row's probability, and values of equal size and opposite sign: what is left of their difference is small
+    beside what a rounding of either weight makes.  Queries have three elements, so that scores are nearly exact."""
+    st = setup(seed_of(store, dtype, shape, negative), store, dtype, shape, h=8, g=2)
+    st.q = torch.zeros_like(st.q)
+    st.q[:, :, 0] = 60.0
+    st.q[:, :, 1:3] = 2.0 * torch.randn((st.total, 8, 2), generator=st.gen).to(st.td)
+    one = 127.0 if store == "int8" else 448.0
+    k = torch.zeros(st.k.shape)
+    k[..., 0] = -one
+    k[..., 1:3] = (torch.randn(k[..., 1:3].shape, generator=st.gen) * one / 8).clamp(-one, one)
+    v = torch.randn(st.v.shape, generator=st.gen) * one / 8
+    st.k_scales = (0.9 + 0.2 * torch.rand(st.k_scales.shape, generator=st.gen)) / one
+    st.v_scales = (1.0 + torch.rand(st.v_scales.shape, generator=st.gen)) / one
+    for b, s in enumerate(st.lens):
+        at = (s - st.new[b]) // 2
+        for i, sign in enumerate((1.0, -1.0)):
+            page, row = int(st.table[b, (at + i) // 16]), (at + i) % 16
+            k[page, :, row, 0] = one
+            st.k_scales[page, :, row] = 1.0 / one
+            v[page, :, row] = sign * torch.where(torch.arange(128) % 2 == 0, one, -one / 2)
+            st.v_scales[page, :, row] = 1.37 / one
+    st.k, st.v = ((x.round() if store == "int8" else x).to(Q.CODES[store]) for x in (k, v))
+    return st
+
+
+def weights_bound(st, sees, half):
+    """Outputs, and how far off they may be if weights are off by `half` of themselves, scores by a step for each product, factor and sum, and sums by one for each key."""
+    out, _, _, _ = Q.attention(st, sees)
+    size, tol = torch.zeros_like(out), torch.zeros_like(out)
+    G = st.h // st.g
+    for b in range(st.batch):
+        s, n, c0 = st.lens[b], st.new[b], int(st.cu[b])
+        seen = sees(b)
+        for kv in range(st.g):
+            k, v = st.held("k", b, kv, s)[0], st.held("v", b, kv, s)[0]
+            q = st.q[c0:c0 + n].to(O.F8).view(n, st.g, G, 128)[:, kv].transpose(0, 1)
+            z = (torch.matmul(q, k.T) / math.sqrt(128.0)).masked_fill(~seen, -math.inf)
+            err = float((torch.matmul(q.abs(), k.abs().T) / math.sqrt(128.0)).max()) * (8 if st.dtype == "bf16" else 16) * 2.0 ** -23 + 2.0 ** -20
+            size = torch.matmul(torch.softmax(z, dim=-1), v.abs())
+            rel = math.expm1(2 * err) + half + ((1 if st.dtype == "bf16" else 3) * s + 16) * 2.0 ** -23
+            tol[c0:c0 + n, kv * G:(kv + 1) * G] = (size * rel).transpose(0, 1)
+    return out, tol + out.abs() * O.HALF[st.dtype]
+
+
+@pytest.mark.parametrize("kind", ["quant", "window", "tree"])
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_weights_are_off_by_half_a_step_of_fp16(kind, store, dtype, shape):
+    """... in bf16, by 2^-22 of themselves in fp32: not by the 2^-8 that bf16 weights would be off by, which the same bound refuses."""
+    st = pairs(store, dtype, shape)
+    got, sees = run_kind(st, kind, window=5000, sinks=0)
+    want, tol = weights_bound(st, sees, 2.0 ** -11 if dtype == "bf16" else 2.0 ** -22)
+    near(got[0][:int(st.cu[-1])], want, tol, "out")
