@@ -574,9 +574,10 @@ def ctkvr_cache_evict(cache: Cache, weights_in, k_pages, v_pages, cur_lens, bloc
 # ---- the paged KV cache in 8 bits, in a window, with drafted tokens ---------------
 def _format_of(cache: Cache, k, plain=False) -> int:
     """What rows of k's type are: int8 or e4m3 codes, or plain rows where those are taken."""
-    f = cache._formats.get(k.dtype, -1)
+    dtype = getattr(k, "dtype", None)
+    f = cache._formats.get(dtype, -1)
     if f < 0 or (f == KV_PLAIN and not plain):
-        raise ValueError(f"rows of {k.dtype}: expected torch.int8 or torch.float8_e4m3fn codes" + (f", or plain rows of {cache.torch_dtype}" if plain else ""))
+        raise ValueError(f"rows of {dtype}: expected torch.int8 or torch.float8_e4m3fn codes" + (f", or plain rows of {cache.torch_dtype}" if plain else ""))
     return f
 
 
@@ -586,12 +587,15 @@ def _batch_of(cache: Cache, cu_new, cur_lens, block_table):
 
 
 def _quant_of(cache: Cache, k, k_scales, v, v_scales):
-    dtype, s, f32 = (k if k is not None else v).dtype, cache._shapes, cache._float
+    # (of neither: refused by _format_of)
+    dtype, s, f32 = getattr(k if k is not None else v, "dtype", None), cache._shapes, cache._float
     return "k", k, dtype, s["pages"], "k_scales", k_scales, f32, s["scales"], "v", v, dtype, s["pages"], "v_scales", v_scales, f32, s["scales"]
 
 
 def ctkvr_cache_quant_append(cache: Cache, q, k, v, cu_new, cur_lens, block_table, q_out, k_codes, k_scales, v_codes, v_scales, positions=None) -> None:
     """As ``ctkvr_cache_append``; the codes are torch.int8 or torch.float8_e4m3fn, the scales fp32 [num_pages][g][page].  q and q_out may be None."""
+    if k is None:
+        raise ValueError("k: expected a tensor, got None")
     p, total = cache.params, k.shape[0]
     (qp, qs), (kp, ks) = _rows_on(cache, "q", q, total, p.n_q_heads), _rows_on(cache, "k", k, total, p.n_kv_heads)
     vp, vs = _rows_on(cache, "v", v, total, p.n_kv_heads)
@@ -605,6 +609,8 @@ def ctkvr_cache_quant_append(cache: Cache, q, k, v, cu_new, cur_lens, block_tabl
 def ctkvr_cache_quant_read(cache: Cache, k_codes, k_scales, v_codes, v_scales, cur_lens, block_table, out_table, k_pages, v_pages, first_tokens=None) -> None:
     """Into plain pages [any number][g][page][128] by out_table int32 [batch][any number]; codes, scales and pages of K, or of V, may be None."""
     s, i32, some = cache._shapes, cache._int, k_pages if k_pages is not None else v_pages
+    if some is None:
+        raise ValueError("neither k_pages nor v_pages")
     shape, out_shape = (some.shape[0],) + s["pages"][1:], (cache.params.batch, out_table.shape[-1])
     *codes, first, cur, table, out, k, v = _all_on(
         cache, *_quant_of(cache, k_codes, k_scales, v_codes, v_scales), "first_tokens", first_tokens, i32, s["batch"], "cur_lens", cur_lens, i32, s["batch"],
