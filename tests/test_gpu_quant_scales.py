@@ -123,10 +123,10 @@ def test_wide_windows_far_beyond_the_table(store, dtype, new, cur, window):
 
 
 # ---- weights --------------------------------------------------------------------------------------------------
-def pairs(store, dtype, shape, negative=False):
+def pairs(store, dtype, shape):
     """Keys of which two, of nearly the same score, have nearly all of a row's probability, and values of equal size and opposite sign: what is left of their difference is small
     beside what a rounding of either weight makes.  Queries have three elements, so that scores are nearly exact."""
-    st = setup(seed_of(store, dtype, shape, negative), store, dtype, shape, h=8, g=2)
+    st = setup(seed_of(store, dtype, shape), store, dtype, shape, h=8, g=2)
     st.q = torch.zeros_like(st.q)
     st.q[:, :, 0] = 60.0
     st.q[:, :, 1:3] = 2.0 * torch.randn((st.total, 8, 2), generator=st.gen).to(st.td)
@@ -178,3 +178,25 @@ def test_weights_are_off_by_half_a_step_of_fp16(kind, store, dtype, shape):
     got, sees = run_kind(st, kind, window=5000, sinks=0)
     want, tol = weights_bound(st, sees, 2.0 ** -11 if dtype == "bf16" else 2.0 ** -22)
     near(got[0][:int(st.cu[-1])], want, tol, "out")
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [shape for shape in SHAPES if max(SHAPES[shape][1]) > 1])
+@pytest.mark.parametrize("power", [20, 60, 120])
+def test_weights_beside_large_values_are_as_exact(store, dtype, shape, power):
+    """The last token of a sequence brings a value 2^power times as large as the others: those before it, which do not see it, are as exact as without."""
+    st = pairs(store, dtype, shape)
+    for b, (s, n) in enumerate(zip(st.lens, st.new)):
+        if n > 1:
+            st.v_scales[int(st.table[b, (s - 1) // 16]), :, (s - 1) % 16] *= 2.0 ** power
+    out = run_quant(st, cache_of(st))[0][:int(st.cu[-1])].cpu()
+    hit = [int(st.cu[b + 1]) - 1 for b, n in enumerate(st.new) if n > 1]
+    assert torch.isfinite(out[hit]).all() and (out[hit].abs().amax(dim=-1) > 1e-7 * 2.0 ** power).all()     # (a hundred times e^-10 of it, at least, in some element)
+    for b, (s, n) in enumerate(zip(st.lens, st.new)):
+        if n > 1:
+            st.v_scales[int(st.table[b, (s - 1) // 16]), :, (s - 1) % 16] *= 2.0 ** -power
+    want, tol = weights_bound(st, lambda b: Q.sees_range(st, b), 2.0 ** -11 if dtype == "bf16" else 2.0 ** -22)
+    keep = torch.ones(len(out), dtype=torch.bool)
+    keep[hit] = False
+    near(out[keep], want[keep], tol[keep], "out")
