@@ -23,8 +23,12 @@ SHAPES = {
 }
 
 
+#: many rows of 128 at a time
+CROWD = ((300,) * 48, (200,) * 48, True)
+
+
 def setup(seed, store, dtype, shape, h=8, g=2, **more):
-    lens, new, wide = SHAPES[shape]
+    lens, new, wide = SHAPES.get(shape, CROWD)
     return Q.QuantSetup(seed, store, dtype, h, g, 16, lens, new, spare_cols=256 if wide else 1, behind=1, **more)
 
 
@@ -200,3 +204,14 @@ def test_weights_beside_large_values_are_as_exact(store, dtype, shape, power):
     keep = torch.ones(len(out), dtype=torch.bool)
     keep[hit] = False
     near(out[keep], want[keep], tol[keep], "out")
+
+
+@pytest.mark.parametrize("kind", ["quant", "window", "tree"])
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_weights_of_a_crowd(kind, store, dtype):
+    """77 thousand rows: a weight in some ten thousand lies, rounded to fp32, half way between two numbers of fp16.  Its parts with fp32 queries have to be of one rounding."""
+    st = pairs(store, dtype, "crowd")
+    got, sees = run_kind(st, kind, window=5000, sinks=0)
+    want, tol = weights_bound(st, sees, 2.0 ** -11 if dtype == "bf16" else 2.0 ** -22)
+    near(got[0][:int(st.cu[-1])], want, tol, "out")
