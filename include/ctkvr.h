@@ -350,9 +350,10 @@ int ctkvr_cache_quant_read(ctkvr_cache *c, int32_t format, const void *k_codes, 
 
 /*
  * ctkvr_cache_attn over rows of 8 bits (format: INT8 or FP8): the same scores, masks and results, on the values that the codes stand for.  Queries are not
- * rounded (fp32 ones: finite ones, below 2^127).  A probability times its value's scale enters the product in fp16, with fp32 data as the sum of two
- * such numbers, under a power of two of the row's own: it is off by 2^-11 of itself (2^-22) or, if it is small, by 2^-35 of the largest magnitude of a scale that
- * the row sees, or of 2^-80 if that is more.  Scales are finite, of either sign, or NaN for a row that is NaN; scales and codes that no token sees may be anything.
+ * rounded; their products with a row's codes, which the row's scale multiplies afterwards, are fp32 sums (finite for queries below 2^112, whatever the scales).  A probability
+ * times its value's scale enters the product in fp16, with fp32 data as the sum of two such numbers, under a power of two of the row's own: it is off by 2^-11 of itself (2^-22)
+ * or, if it is small, by 2^-35 of the largest magnitude of a scale that the row sees, or of 2^-80 if that is more.  Scales are finite, of either sign, or NaN for a row that is
+ * NaN; scales and codes that no token sees may be anything.
  * Errors: EINVAL.
  */
 int ctkvr_cache_quant_attn(ctkvr_cache *c, const void *q, int64_t q_stride, int32_t format, const void *k_codes, const float *k_scales, const void *v_codes,

@@ -4,7 +4,7 @@
 // the products take them as they are, two bytes each from the conversion on; a key's scale multiplies its score, a value's its probability.  Such a weight enters the
 // product in fp16, which has three bits more than bf16 (with weights in bf16 the outputs of a single token on 32K keys were 2.5e-3 off, of which their own rounding is
 // 1.6e-3), under a power of two that goes with the largest scale that its row has seen (kWeightPower).  With fp32 queries a query is three bf16 parts and a weight two of
-// fp16: as exact as fp32 products, at a sixth of their cost.
+// fp16: as exact as fp32 products (outputs 4e-7 to 9e-7 off, elementary operations in fp32 8e-7 to 2.6e-6), at a sixth of their cost.
 #pragma once
 #include "cache.hpp"
 

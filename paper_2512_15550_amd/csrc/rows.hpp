@@ -33,7 +33,7 @@ template <bool CODES> struct RowsTile {
 
 // One block a tile of 32 NW rows of a unit and, where the keys are split, one of nsplit runs of them; a wave has 32 rows.  While a tile of 64 keys is worked on the
 // next one is put into shared memory (codes: turned into bf16 and fp16 by the block, each once for all its waves) and the one behind it requested.  Two waves a SIMD: two blocks of four
-// a CU, or one of eight, which does half of that work for a row (2048 tokens on 32K codes 1243 -> 1146 us, 926 to 954 TFLOP/s; 8192 plain rows in a window of 1024 take 185 us in blocks of four, 199 in blocks of eight).  Products and the vector instructions of softmax, scales and
+// a CU, or one of eight, which does half of that work for a row (2048 tokens on 32K codes 1243 -> 1146 us, 903 to 952 TFLOP/s; 8192 plain rows in a window of 1024 take 185 us in blocks of four, 199 in blocks of eight).  Products and the vector instructions of softmax, scales and
 // conversion bound it, which two waves of a SIMD hardly overlap.
 template <int STORE, typename T, int OPT, int SIGHT, int NW> __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void rows_kernel(QuantAttnArgs qa)
 {

@@ -14,7 +14,7 @@ namespace ctkvr {
 // 512 353 -> 319, 33 62 -> 54, 4096 on themselves 199 -> 176, four sequences of 300 on 8K to 64K 1555 -> 652, split, eight drafts of 64 on 32K 443 -> 366, plain ones 398 -> 361;
 // but one plain draft of 64 61 -> 63, 2048 and 1024 on themselves 73 -> 80 and 41 -> 46, 8192 plain rows in windows of 1024 and 128 185 -> 199 and 82 -> 94, and 20 tokens of
 // eight sequences, 80 rows, 142 -> 198).  Runs are as many as use all CUs to the end (five drafts of 27 on 8K, 450 blocks and 250: 94 -> 79).
-//   With fp32 queries a tile of 32 rows has more registers than two waves a SIMD: 16 or 128 rows (100 / 512 tokens on 8192 keys 70, 83, 62 / 220, 266, 194; 8 on 32K 32,
+//   With fp32 queries a tile of 32 rows has more registers than two waves a SIMD: 16 or 128 rows (100 / 512 tokens on 8192 keys 70, 83, 62 / 220, 266, 203; 8 on 32K 32,
 // 34, 57; 500 on as many, 2 KV heads, 13, 16, 35).  Over plain fp32 rows it is 32 or 128, as in ctkvr_cache_attn.
 //   Keys are split into runs where blocks would be too few, to so many blocks a CU: single tokens of one sequence, and in windows, whose runs are alike, one; of
 // several sequences, whose lengths differ, half as many as these, 2 to 8 (up to 64K keys, two sequences 25, 31, 36 with 2, 4, 8; four 63, 65, 69; sixteen 267, 248, 240); tiles
