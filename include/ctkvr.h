@@ -366,7 +366,7 @@ int ctkvr_cache_quant_attn(ctkvr_cache *c, const void *q, int64_t q_stride, int3
  * over plain rows (format PLAIN, scales NULL) or rows of 8 bits (as in ctkvr_cache_quant_attn).  What it costs goes by the window, not by the cache.  Pages that lie before every
  * window of a sequence and behind its first n_sink tokens are not needed any more: their entries of the table may be -1, or pages of other sequences.
  *   window  1 or more (the token itself counts);  n_sink  0 or more.
- * Errors: EINVAL.
+ * Roundings and sums as there: over plain bf16 rows the probabilities enter the product with V rounded to bf16.  Errors: EINVAL.
  */
 int ctkvr_cache_window_attn(ctkvr_cache *c, const void *q, int64_t q_stride, int32_t format, const void *k_pages, const float *k_scales, const void *v_pages,
                             const float *v_scales, const int32_t *cu_new, const int32_t *cur_lens, const int32_t *block_table, int32_t total, int32_t window,
@@ -380,7 +380,7 @@ int ctkvr_cache_window_attn(ctkvr_cache *c, const void *q, int64_t q_stride, int
  *   first_key  DEVICE int32 [total] or NULL: it sees no key, new ones included, in an earlier slot.
  * Over plain rows (format PLAIN, scales NULL) or rows of 8 bits (as in ctkvr_cache_quant_attn).  The cache was appended to with the draft's own positions (a token's depth in its tree behind the
  * tokens before it); the tokens that are kept in the end go to their slots in order by another append, of their k and v, with cur_lens counting them alone.
- * A token that sees no key gets zeros and -infinity.  Errors: EINVAL.
+ * A token that sees no key gets zeros and -infinity.  Roundings and sums as in ctkvr_cache_attn, over 8-bit rows as in ctkvr_cache_quant_attn.  Errors: EINVAL.
  */
 int ctkvr_cache_tree_attn(ctkvr_cache *c, const void *q, int64_t q_stride, int32_t format, const void *k_pages, const float *k_scales, const void *v_pages,
                           const float *v_scales, const int32_t *cu_new, const int32_t *cur_lens, const int32_t *block_table, int32_t total,
